@@ -459,6 +459,134 @@ int misat_overload_observe(misat_overload* ov, const int64_t* hit_tokens, const 
 int misat_recheck_delays(int32_t n, const uint64_t* group, const uint8_t* held, int64_t base_delay_us,
                          int64_t min_delay_us, int64_t* delay_out);
 
+/* ---- KV blocks of an inference instance: rotary positions, append, attention ----
+ * The router counts 16-token KV blocks and says how many of a prompt's leading blocks the
+ * chosen instance already holds (hit_blocks).  These calls are the instance's side of that
+ * decision: the tokens after the hit are rotated to their positions, put into blocks of the
+ * instance's cache, and attend over the cached prefix and each other.  The paper has no
+ * counterpart (it uses an existing engine).
+ *
+ * Conventions beyond the ones above:
+ *   - Each call runs on the stream it is given ([async]; none allocates, waits or keeps
+ *     anything of a call for the next, so all of them can be captured into a CUDA graph).
+ *     A pool's calls share its workspace: calls on two streams must be ordered by the caller.
+ *   - A tensor of heads is [n_tokens][heads][head_dim] with the elements of a head next to
+ *     each other and any non-negative strides between tokens and heads, given in elements.
+ *     Rows at 16-byte boundaries are moved 16 bytes at a time, others an element at a time.
+ *   - Whole numbers found malformed on the device (offsets out of order, a length beyond its
+ *     block table, a block outside the pool) are sticky errors of the pool, returned by
+ *     misat_kv_sync; the sequences concerned are skipped, and nothing outside the buffers
+ *     passed is read or written. */
+#define MISAT_BF16 0
+#define MISAT_F16 1
+#define MISAT_F32 2
+
+/* Rotary position embedding.  The first rot_dim elements of a head are rot_dim / 2 pairs;
+ * pair i of a token at position p is turned by the angle p f_i and scaled by attn_factor:
+ *   (a, b) -> attn_factor (a cos - b sin, a sin + b cos)
+ * f_i = base^(-2i / rot_dim), then by `scaling`:
+ *   LINEAR    f_i / factor
+ *   BY_PARTS  f_i (g + (1 - g) / factor) with g = clamp((r_i - beta_slow) /
+ *             (beta_fast - beta_slow), 0, 1) and r_i = orig_len f_i / (2 pi), the turns that
+ *             the pair makes over the original length: slow pairs are interpolated, fast ones
+ *             kept. */
+#define MISAT_ROPE_HALF 0        /* pair i = elements i and i + rot_dim / 2 */
+#define MISAT_ROPE_INTERLEAVED 1 /* pair i = elements 2i and 2i + 1 */
+#define MISAT_ROPE_SCALE_NONE 0
+#define MISAT_ROPE_SCALE_LINEAR 1
+#define MISAT_ROPE_SCALE_BY_PARTS 2
+typedef struct misat_rope misat_rope;
+typedef struct misat_rope_config {
+  int32_t rot_dim;      /* even, 2..1024 */
+  int32_t layout;       /* MISAT_ROPE_HALF / INTERLEAVED */
+  int32_t scaling;      /* MISAT_ROPE_SCALE_* */
+  double base;          /* > 1 (10000) */
+  double factor;        /* > 0; read with LINEAR and BY_PARTS */
+  double orig_len;      /* > 0, 0 <= beta_slow < beta_fast: read with BY_PARTS */
+  double beta_slow, beta_fast;
+  double attn_factor;   /* finite, > 0 (1) */
+} misat_rope_config;
+
+/* Frequencies on the current device.  [sync]  Errors: INVALID_ARG, OOM, CUDA. */
+int misat_rope_create(const misat_rope_config* cfg, misat_rope** out);
+/* Frees them; no call that uses them, nor a pool made with them, may be pending.  [sync] */
+int misat_rope_destroy(misat_rope* rope);
+/* out = rotation of x (n_tokens x n_heads heads of head_dim >= rot_dim elements, at most 1024)
+ * at positions[token]; the elements past rot_dim are copied.  backward != 0: the gradient of x
+ * given the gradient of out, i.e. the transposed map (the turn the other way).  dtype:
+ * MISAT_BF16, F16 or F32; computed in 32 bits and rounded once.  out may be x itself (same
+ * pointer and strides) but not overlap it otherwise.  Errors: INVALID_ARG, CUDA. */
+int misat_rotary(const misat_rope* rope, int32_t dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                 const void* x, int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions, void* out,
+                 int64_t out_token_stride, int64_t out_head_stride, int32_t backward, void* cuda_stream);
+
+/* A pool of KV blocks.  k_blocks and v_blocks (device, 16-byte aligned, owned by the caller)
+ * are [n_blocks][n_kv_heads][16][head_dim]: the 16 tokens of a block and head are contiguous. */
+typedef struct misat_kv misat_kv;
+typedef struct misat_kv_config {
+  int32_t n_blocks;    /* >= 1, n_blocks * n_kv_heads < 2^31 */
+  int32_t n_kv_heads;  /* >= 1 */
+  int32_t n_q_heads;   /* a multiple of n_kv_heads, at most 128 per kv head */
+  int32_t head_dim;    /* a multiple of 8, 8..128 */
+  int32_t dtype;       /* MISAT_BF16 or MISAT_F16: of the blocks and of every q, k, v, out */
+  int32_t max_batch;   /* largest n of a misat_kv_batch, 1..2^20 */
+  float scale;         /* factor on q.k, > 0; 0: 1 / sqrt(head_dim) */
+  const misat_rope* rope; /* rotation of appended keys and queries (rot_dim <= head_dim), or NULL;
+                             must outlive the pool */
+  void* k_blocks;
+  void* v_blocks;
+} misat_kv_config;
+
+/* The new tokens of n sequences, device pointers.  Sequence b has q_off[b+1] - q_off[b] new
+ * tokens, the last of its kv_len[b] tokens: new token i is at position kv_len[b] -
+ * (q_off[b+1] - q_off[b]) + i, and position p is in slot p % 16 of block
+ * block_table[b * table_stride + p / 16].  Entries past the sequence's last block are not
+ * read. */
+typedef struct misat_kv_batch {
+  int32_t n;                  /* sequences, 0..max_batch */
+  int32_t n_tokens;           /* q_off[n] */
+  int32_t max_q;              /* at least the new tokens of any sequence */
+  const int32_t* q_off;       /* [n+1], q_off[0] = 0, non-decreasing */
+  const int32_t* kv_len;      /* [n] tokens of the sequence, the new ones included */
+  const int32_t* block_table; /* [n][table_stride] */
+  int64_t table_stride;       /* blocks per row, kv_len <= 16 table_stride */
+} misat_kv_batch;
+
+/* [sync]  Errors: INVALID_ARG, OOM, CUDA. */
+int misat_kv_create(const misat_kv_config* cfg, misat_kv** out);
+/* Frees the pool's workspace, not the blocks; no call may be pending.  [sync] */
+int misat_kv_destroy(misat_kv* kv);
+
+/* Append: k (rotated, if the pool has a rotation) and v of every new token go into its
+ * sequence's blocks; q, rotated the same way, into q_out.  q may be NULL (then q_out is
+ * ignored); q_out may be q.  Values are rounded once, to the pool's dtype.  Two tokens of a
+ * batch must not share a slot.  A sequence with kv_len below its new tokens is an error.
+ * [async]  Errors: INVALID_ARG, CUDA; INVALID_ARG later (see above). */
+int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, int64_t k_token_stride,
+                    int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                    const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                    int64_t qo_token_stride, int64_t qo_head_stride, void* cuda_stream);
+
+/* Attention of the new tokens over the cached tokens: for the token at position p and query
+ * head h, over the keys j <= p (with window > 0 only p - window < j) of kv head
+ * h / (n_q_heads / n_kv_heads):
+ *   out = sum_j softmax_j(scale q.k_j) v_j,   lse = log sum_j exp(scale q.k_j)
+ * lse is optional, [n_tokens][n_q_heads] 32-bit.  Scores, maxima, sums and the output's sum
+ * are held in 32 bits; the weights are rounded to the pool's dtype for the product with v.
+ * A token that sees no key (a position below zero) gets zeros, and -infinity in lse.  Slots
+ * past kv_len are never used, whatever they hold; a key that only some new tokens of a
+ * sequence see has to be finite for all of them (0 times infinity is NaN).
+ * The result does not depend on timing: the same call gives the same bits.  [async]
+ * Errors: INVALID_ARG, CUDA; INVALID_ARG later (see above; what the skipped sequences' rows
+ * of out and lse then hold is not specified). */
+int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, int64_t q_token_stride,
+                    int64_t q_head_stride, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                    int32_t window, void* cuda_stream);
+
+/* Wait for the stream and return the pool's sticky device error (0 if none), then clear it.
+ * [sync] */
+int misat_kv_sync(misat_kv* kv, void* cuda_stream);
+
 /* Wait for the stream and return the sticky device error (0 if none), then clear it and
  * drop any pending route.  A batch rejected on the device changes no persistent state;
  * after TABLE_FULL during a commit the index of the affected instance may hold part of

@@ -1,0 +1,74 @@
+// Internal definitions of the KV block operators: handles and the launches behind the C ABI.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+// Frequencies of a rotation as fractions of a turn in 64-bit fixed point: the angle at position p
+// is (p * freq[i] mod 2^64) / 2^64 turns.  The product wraps at whole turns, so the angle is exact
+// to 2^-44 turns at any position below 2^20, where a 32-bit product of position and frequency has
+// lost all but a few bits.
+struct misat_rope {
+  int device, num_sms;
+  int32_t rot, layout;
+  float attn;
+  uint64_t* freq;  // device [rot / 2]
+};
+
+struct misat_kv {
+  int device, num_sms;
+  int32_t n_blocks, hkv, hq, d, dtype, max_batch;
+  float scale;
+  const misat_rope* rope;
+  void* kb;
+  void* vb;
+  int32_t* err;  // device, sticky
+};
+
+namespace misat {
+
+// A tensor of heads; strides in elements.
+struct Heads {
+  void* p;
+  int64_t ts, hs;
+};
+
+// Device view of a misat_kv_batch.
+struct KvBatch {
+  int32_t n, n_tokens, max_q;
+  const int32_t* q_off;
+  const int32_t* kv_len;
+  const int32_t* table;
+  int64_t stride;
+};
+
+// Checks of the arguments that both pool calls share.  A tensor's pointer has to be aligned to its
+// elements; strides may be anything non-negative.
+inline bool heads_ok(const void* p, int64_t ts, int64_t hs, int elem) {
+  return p && ts >= 0 && hs >= 0 && (reinterpret_cast<uintptr_t>(p) % elem) == 0;
+}
+inline bool batch_ok(const misat_kv* kv, const misat_kv_batch* b) {
+  if (!kv || !b || b->n < 0 || b->n > kv->max_batch || b->n_tokens < 0 || b->max_q < 0 || b->table_stride < 0)
+    return false;
+  if (b->n_tokens > 0 && b->n == 0) return false;
+  return b->n_tokens == 0 || (b->q_off && b->kv_len && b->block_table);
+}
+inline KvBatch batch_view(const misat_kv_batch* b) {
+  return {b->n, b->n_tokens, b->max_q, b->q_off, b->kv_len, b->block_table, b->table_stride};
+}
+
+// The handle's device is the current one.
+inline bool on_device(int device) {
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess && d == device;
+}
+
+// Return code of the launches just made.
+inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA; }
+
+void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,
+                   cudaStream_t st);
+
+}  // namespace misat

@@ -29,6 +29,10 @@ ERR_INVALID_ARG, ERR_OOM, ERR_CUDA, ERR_STATE, ERR_TABLE_FULL, ERR_BATCH_TOO_LAR
 ERR_INTERNAL = -7
 MODE_MISA_T, MODE_MISA, MODE_SESSION_ADMISSION, MODE_PLACEMENT_ONLY = 0, 1, 2, 3
 PREFIX_GLOBAL, PREFIX_PER_INSTANCE = 0, 1
+BF16, F16, F32 = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BY_PARTS = 0, 1, 2
+BLOCK_TOKENS = 16
 ADMIT_CONT, ADMIT_NEW, ADMIT_FOLLOW = 1, 2, 3
 HOLD_GLOBAL_CAP, HOLD_CLASS_CAP, HOLD_NO_ELIGIBLE, HOLD_PREFER_CACHE, HOLD_LEADER_HELD = 16, 17, 18, 19, 20
 
@@ -82,6 +86,23 @@ PHASES = ("prologue", "hash", "caps", "probe_first", "probe_search", "select", "
           "evict_shift")
 
 
+class misat_rope_config(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("orig_len", C.c_double), ("beta_slow", C.c_double),
+                ("beta_fast", C.c_double), ("attn_factor", C.c_double)]
+
+
+class misat_kv_config(C.Structure):
+    _fields_ = [("n_blocks", C.c_int32), ("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("max_batch", C.c_int32), ("scale", C.c_float),
+                ("rope", _p), ("k_blocks", _p), ("v_blocks", _p)]
+
+
+class misat_kv_batch(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_tokens", C.c_int32), ("max_q", C.c_int32), ("q_off", _p), ("kv_len", _p),
+                ("block_table", _p), ("table_stride", C.c_int64)]
+
+
 _SIG = {
     "misat_create": [C.POINTER(misat_config), _p, C.POINTER(_p)],
     "misat_destroy": [_p],
@@ -120,6 +141,16 @@ _SIG = {
     "misat_overload_destroy": [_p],
     "misat_overload_observe": [_p, _p, _p, _p, _p, _p],
     "misat_recheck_delays": [C.c_int32, _p, _p, C.c_int64, C.c_int64, _p],
+    "misat_rope_create": [C.POINTER(misat_rope_config), C.POINTER(_p)],
+    "misat_rope_destroy": [_p],
+    "misat_rotary": [_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _p, C.c_int64, C.c_int64, _p, _p, C.c_int64,
+                     C.c_int64, C.c_int32, _p],
+    "misat_kv_create": [C.POINTER(misat_kv_config), C.POINTER(_p)],
+    "misat_kv_destroy": [_p],
+    "misat_kv_append": [_p, _p, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p,
+                        C.c_int64, C.c_int64, _p],
+    "misat_kv_attend": [_p, _p, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, C.c_int32, _p],
+    "misat_kv_sync": [_p, _p],
 }
 NOALLOC_MAX_REQUESTS = 65536
 
@@ -509,3 +540,216 @@ def recheck_delays(group, held, base_delay_us: int, min_delay_us: int) -> np.nda
     _ck(_lib.misat_recheck_delays(int(g.shape[0]), _np_ptr(g), _np_ptr(h), int(base_delay_us), int(min_delay_us),
                                   _np_ptr(out)), "misat_recheck_delays")
     return out
+
+
+# ---- KV blocks of an inference instance: rotary positions, append, attention ----
+
+
+def _dtype_code(dtype):
+    import torch
+
+    code = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}.get(dtype)
+    if code is None:
+        raise ValueError(f"dtype {dtype}: bfloat16, float16 or float32 expected")
+    return code
+
+
+def _heads(t, name, dtype, device, n_heads=None, head_dim=None):
+    """Checks a [tokens, heads, head_dim] tensor whose heads are contiguous."""
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: {dtype} on {device} expected, got {t.dtype} on {t.device}")
+    if t.dim() != 3 or (n_heads is not None and (t.shape[1] != n_heads or t.shape[2] != head_dim)):
+        raise ValueError(f"{name}: [tokens, {n_heads or 'heads'}, {head_dim or 'head_dim'}] expected, "
+                         f"got {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: the elements of a head must be contiguous")
+    return t
+
+
+def _ints(t, name, shape, device):
+    import torch
+
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: int32 {list(shape)} on {device} expected, got {t.dtype} {list(t.shape)} on "
+                         f"{t.device}")
+    return t
+
+
+class Rope:
+    """Rotary position embedding on the current CUDA device (misat_rope_*, misat_rotary)."""
+
+    def __init__(self, rot_dim, *, base=10000.0, layout=ROPE_HALF, scaling=ROPE_SCALE_NONE, factor=1.0, orig_len=0.0,
+                 beta_slow=1.0, beta_fast=32.0, attn_factor=1.0):
+        import torch
+
+        self._torch = torch
+        self.rot_dim = int(rot_dim)
+        self._h = None
+        cfg = misat_rope_config(self.rot_dim, layout, scaling, base, factor, orig_len, beta_slow, beta_fast,
+                                attn_factor)
+        h = _p()
+        _ck(_lib.misat_rope_create(C.byref(cfg), C.byref(h)), "misat_rope_create")
+        self._h = h
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.misat_rope_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _apply(self, x, positions, out, backward):
+        torch = self._torch
+        _heads(x, "x", x.dtype, self.device)
+        n, heads, d = x.shape
+        _ints(positions, "positions", (n,), self.device)
+        if n > 1 and positions.stride(0) != 1:
+            raise ValueError("positions: a contiguous tensor expected")
+        if out is None:
+            out = torch.empty((n, heads, d), dtype=x.dtype, device=self.device)
+        else:
+            _heads(out, "out", x.dtype, self.device, heads, d)
+            if out.shape[0] != n:
+                raise ValueError(f"out: {n} tokens expected, got {out.shape[0]}")
+        xs, os_ = x.stride(), out.stride()
+        _ck(_lib.misat_rotary(self._h, _dtype_code(x.dtype), n, heads, d, x.data_ptr(), xs[0], xs[1],
+                              positions.data_ptr(), out.data_ptr(), os_[0], os_[1], backward,
+                              torch.cuda.current_stream().cuda_stream), "misat_rotary")
+        return out
+
+    def rotate(self, x, positions, out=None):
+        """x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); out may be x."""
+        return self._apply(x, positions, out, 0)
+
+    def backward(self, grad, positions, out=None):
+        """Gradient of rotate()'s x, given the gradient of its result."""
+        return self._apply(grad, positions, out, 1)
+
+
+class KvBatch:
+    """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer."""
+
+    def __init__(self, pool, q_off, kv_len, block_table, n_tokens, max_q):
+        n = kv_len.shape[0]
+        _ints(q_off, "q_off", (n + 1,), pool.device)
+        _ints(kv_len, "kv_len", (n,), pool.device)
+        if block_table.dim() != 2:
+            raise ValueError("block_table: [sequences, blocks] expected")
+        _ints(block_table, "block_table", (n, block_table.shape[1]), pool.device)
+        if not (q_off.is_contiguous() and kv_len.is_contiguous()):
+            raise ValueError("q_off and kv_len: contiguous tensors expected")
+        if block_table.shape[1] > 1 and block_table.stride(1) != 1:
+            raise ValueError("block_table: the blocks of a sequence must be contiguous")
+        if n > 1 and block_table.stride(0) < block_table.shape[1]:
+            raise ValueError("block_table: rows must not overlap")
+        self.n, self.n_tokens = n, int(n_tokens)
+        self._keep = (q_off, kv_len, block_table)
+        stride = block_table.stride(0) if n > 1 else block_table.shape[1]
+        self._c = misat_kv_batch(n, self.n_tokens, int(max_q), q_off.data_ptr(), kv_len.data_ptr(),
+                                 block_table.data_ptr(), stride)
+        self._ref = C.addressof(self._c)
+
+
+class KvPool:
+    """A pool of 16-token KV blocks on the current CUDA device (misat_kv_*).
+
+    k_blocks, v_blocks: [n_blocks, n_kv_heads, 16, head_dim], contiguous, bfloat16 or float16; the
+    caller's memory.  rope: a Rope that append() applies, or None.  scale: factor on q.k
+    (1 / sqrt(head_dim)).  Calls run on the current stream; the pool orders its own calls when that
+    stream changes."""
+
+    def __init__(self, k_blocks, v_blocks, *, n_q_heads, rope=None, scale=0.0, max_batch=1 << 20):
+        import torch
+
+        self._torch = torch
+        self._h = None
+        if k_blocks.dim() != 4 or k_blocks.shape[2] != BLOCK_TOKENS or v_blocks.shape != k_blocks.shape:
+            raise ValueError(f"k_blocks, v_blocks: one shape [blocks, kv heads, {BLOCK_TOKENS}, head_dim] expected")
+        if not (k_blocks.is_contiguous() and v_blocks.is_contiguous()):
+            raise ValueError("k_blocks, v_blocks: contiguous tensors expected")
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        if k_blocks.device != self.device or v_blocks.device != self.device or v_blocks.dtype != k_blocks.dtype:
+            raise ValueError(f"k_blocks, v_blocks: one dtype on {self.device} expected")
+        self.dtype = k_blocks.dtype
+        self.n_blocks, self.n_kv_heads, _, self.head_dim = k_blocks.shape
+        self.n_q_heads = int(n_q_heads)
+        self.k_blocks, self.v_blocks, self.rope = k_blocks, v_blocks, rope
+        cfg = misat_kv_config(self.n_blocks, self.n_kv_heads, self.n_q_heads, self.head_dim, _dtype_code(self.dtype),
+                              int(max_batch), float(scale), rope._h if rope is not None else None,
+                              k_blocks.data_ptr(), v_blocks.data_ptr())
+        h = _p()
+        _ck(_lib.misat_kv_create(C.byref(cfg), C.byref(h)), "misat_kv_create")
+        self._h = h
+        self._last = None  # stream of the last call
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.misat_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def batch(self, q_off, kv_len, block_table, *, n_tokens, max_q):
+        """Describe a step: int32 device tensors q_off [n+1] (offsets of the sequences' new
+        tokens), kv_len [n] (tokens after the append), block_table [n, blocks]."""
+        return KvBatch(self, q_off, kv_len, block_table, n_tokens, max_q)
+
+    def _stream(self):
+        st = self._torch.cuda.current_stream()
+        last = self._last
+        if last is None or last.cuda_stream != st.cuda_stream:
+            if self._torch.cuda.is_current_stream_capturing():
+                return st.cuda_stream  # whoever replays the graph orders it with the pool's other calls
+            if last is not None:
+                st.wait_stream(last)
+            self._last = st
+        return st.cuda_stream
+
+    def append(self, batch, k, v, q=None, q_out=None):
+        """Put the new tokens' k (rotated) and v, [n_tokens, kv heads, head_dim], into their
+        blocks; returns the rotated q [n_tokens, q heads, head_dim] (None without q).  q_out may be q."""
+        T, d, hkv, hq, dt, dev = batch.n_tokens, self.head_dim, self.n_kv_heads, self.n_q_heads, self.dtype, self.device
+        if _heads(k, "k", dt, dev, hkv, d).shape[0] != T or _heads(v, "v", dt, dev, hkv, d).shape[0] != T:
+            raise ValueError(f"k, v: {T} tokens expected")
+        ks, vs = k.stride(), v.stride()
+        if q is None:
+            qp, qs, op, os_ = None, (0, 0), None, (0, 0)
+            q_out = None
+        else:
+            if q_out is None:
+                q_out = self._torch.empty((T, hq, d), dtype=dt, device=dev)
+            if _heads(q, "q", dt, dev, hq, d).shape[0] != T or _heads(q_out, "q_out", dt, dev, hq, d).shape[0] != T:
+                raise ValueError(f"q, q_out: {T} tokens expected")
+            qp, qs, op, os_ = q.data_ptr(), q.stride(), q_out.data_ptr(), q_out.stride()
+        _ck(_lib.misat_kv_append(self._h, batch._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], qp,
+                                 qs[0], qs[1], op, os_[0], os_[1], self._stream()), "misat_kv_append")
+        return q_out
+
+    def attend(self, batch, q, out=None, window=0, return_lse=False):
+        """Attention of the new tokens' q [n_tokens, q heads, head_dim] over the cached tokens up to
+        and including each; window > 0: over the last `window` of them.  Returns out, or (out, lse)."""
+        torch = self._torch
+        T, d, hq, dt, dev = batch.n_tokens, self.head_dim, self.n_q_heads, self.dtype, self.device
+        if out is None:
+            out = torch.empty((T, hq, d), dtype=dt, device=dev)
+        if _heads(q, "q", dt, dev, hq, d).shape[0] != T or _heads(out, "out", dt, dev, hq, d).shape[0] != T:
+            raise ValueError(f"q, out: {T} tokens expected")
+        lse = torch.empty((T, hq), dtype=torch.float32, device=dev) if return_lse else None
+        qs, os_ = q.stride(), out.stride()
+        _ck(_lib.misat_kv_attend(self._h, batch._ref, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
+                                 lse.data_ptr() if return_lse else None, int(window), self._stream()),
+            "misat_kv_attend")
+        return (out, lse) if return_lse else out
+
+    def sync(self):
+        """Wait for the current stream and raise the pool's sticky device error, if there is one."""
+        _ck(_lib.misat_kv_sync(self._h, self._stream()), "misat_kv_sync")
