@@ -1,86 +1,939 @@
-// Attention of new tokens over a paged cache: a warp per (token, query head), one key at a time.
+// Attention of new tokens over a paged cache (one token, or a chunk), on the tensor cores.
+//
+//   out_r = sum_j p_rj v_j / l_r,  p_rj = 2^(c (s_rj - m_r)),  s = q k^T,  c = scale log2 e,  l_r = sum_j p_rj
+//
+// One pass over the keys.  A tile is 128 rows: 128 / group tokens times the `group` query heads that
+// share a kv head, so the keys and values are read once for all of them.  Per 128 keys the matrix
+// instructions form S = Q K^T in tensor memory, a thread per row reads its 128 scores, takes them to
+// weights and writes these back as the 16-bit operand of O += P V, which stays in tensor memory.
+// The running maximum m is a reference, not the maximum: O and l are rescaled only when a score
+// passes it by more than 2^8 (a weight is then at most 256, and the sums are in 32 bits).
+//
+// Two streams of such tiles share a CTA, so that one's matrix products run under the other's
+// exponentials.  An item of more than 128 rows gives each stream half of its rows, and both read the same
+// keys; a smaller item (a step of single tokens) gives each stream every other block of 128 keys, and
+// the first stream joins the two at the end.
+//
+// One CTA per SM.  The blocks of all items, in order, are dealt out in equal contiguous runs, so
+// long and short sequences, and the triangle of a chunk, load every SM alike.  An item that
+// crosses runs leaves partial sums (O, m, l in 32 bits) in the workspace; the last CTA to arrive
+// adds them, always in the order of the keys, so the result has the same bits on every call.
+//
+// Warps: 0-3 and 4-7 softmax of stream 0 and 1; 8 loads keys and values (a page of 16 tokens is one
+// or two boxes, 2 KB each); 9 issues the matrix instructions; 10-11 load queries.
+#include <type_traits>
+
 #include "kv.h"
+#include "tensor.cuh"
 
 using namespace misat;
 
 namespace {
 
+constexpr int kKeys = 128;     // keys of a block
+constexpr int kTile = 128;     // rows of a stream's tile
+constexpr int kThreads = 384;
+constexpr int kRing = 160 * 1024;  // bytes of the ring of key and value tiles
+constexpr float kRescale = 8.f;    // log2 of the largest weight before a rescale
+constexpr int kRegsIssue = 88, kRegsSoftmax = 208;  // 128 * 88 + 256 * 208 = 384 * 168 registers
+
 struct AttendArgs {
   KvBatch b;
   Heads q, out;
-  const void* kb;
-  const void* vb;
   float* lse;
-  float scale;
-  int32_t hq, group, hkv, d, n_blocks, window;
+  float scale, c;  // c = scale * log2(e)
+  int32_t group, hkv, d, n_blocks, window, tok;  // tok: tokens of a stream's tile
+  bool vec_q, vec_out;  // rows at 16-byte boundaries
+  float4* ws_o;  // [slots][DP / 4][128 rows]
+  float2* ws_ml; // [slots][128 rows]: m, l
+  unsigned* ctr; // [2 x CTAs] arrivals of split items, zero between calls
   int32_t* err;
 };
 
-__device__ __forceinline__ float ldf(const __half* p) { return __half2float(*p); }
-__device__ __forceinline__ float ldf(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void stf(__half* p, float x) { *p = __float2half_rn(x); }
-__device__ __forceinline__ void stf(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+// ---- what there is to do ----
 
-template <class T>
-__global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendArgs a) {
-  const int lane = threadIdx.x & 31;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  chain_wait();
-  if (id >= (int64_t)a.b.n_tokens * a.hq) return;
-  const int t = (int)(id / a.hq), h = (int)(id % a.hq), hk = h / a.group;
-  int lo = 0, hi = a.b.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.b.q_off[mid] <= t) lo = mid;
-    else hi = mid;
-  }
-  const int begin = a.b.q_off[lo], end = a.b.q_off[lo + 1], len = a.b.kv_len[lo];
-  const bool ok = begin <= t && t < end && end - begin <= a.b.max_q && len >= 0 && len <= a.b.stride * kBlockTokens;
-  if (!ok && lane == 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
-  const int64_t pos = ok ? (int64_t)len - end + t : -1;
-  const int64_t from = a.window > 0 && pos + 1 > a.window ? pos + 1 - a.window : 0;
-  const T* q = static_cast<const T*>(a.q.p) + (int64_t)t * a.q.ts + (int64_t)h * a.q.hs;
-  float qr[4], o[4] = {0, 0, 0, 0};
-  for (int i = 0; i < 4; ++i) qr[i] = lane + 32 * i < a.d ? ldf(q + lane + 32 * i) * a.scale : 0.f;
-  float m = -INFINITY, l = 0.f;
-  for (int64_t j = from; j <= pos; ++j) {
-    const int blk = a.b.table[(int64_t)lo * a.b.stride + j / kBlockTokens];
-    if (blk < 0 || blk >= a.n_blocks) {
-      if (lane == 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
-      continue;
+struct Seq {
+  int begin, n, len;  // first new token, new tokens, tokens in all
+};
+
+__device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b) {
+  const int begin = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
+  const bool ok = begin >= 0 && end >= begin && end <= a.b.n_tokens && end - begin <= a.b.max_q && len >= 0 &&
+                  len <= a.b.stride * kBlockTokens;
+  if (!ok) set_error(a.err, MISAT_ERR_INVALID_ARG);
+  return {begin, ok ? end - begin : 0, len};
+}
+
+// Keys of the item of a sequence's tokens [t0, t0 + nt), in blocks.
+struct Span {
+  int from, to;    // keys [from, to) that some row sees
+  int jb, blocks;  // first block, number of blocks (0: no row sees a key)
+};
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const Seq& s, int t0, int nt) {
+  const int p0 = s.len - s.n + t0, to = max(p0 + nt, 0);
+  const int from = a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0;
+  const int jb = from / kKeys;
+  return {from, to, jb, to > 0 ? (to + kKeys - 1) / kKeys - jb : 0};
+}
+__device__ __forceinline__ int item_cost(const AttendArgs& a, const Seq& s, int tile) {
+  const int t0 = tile * 2 * a.tok;
+  return max(span_of(a, s, t0, min(2 * a.tok, s.n - t0)).blocks, 1);
+}
+__device__ __forceinline__ int n_items(const AttendArgs& a, const Seq& s) {
+  return (s.n + 2 * a.tok - 1) / (2 * a.tok);
+}
+
+// A CTA's part of one item.
+struct Segment {
+  Seq s;
+  Span k;
+  int b, h;
+  int t0, nt;          // tokens of the item
+  int j0, nb;          // first block (of the sequence) and blocks of this part
+  bool pair;           // both streams have rows of their own
+  bool whole;          // the part is the item
+  int64_t first, last; // the item's blocks in the order of all blocks
+  __device__ __forceinline__ int stream_blocks(int st) const { return pair ? nb : (nb + 1 - st) / 2; }
+};
+
+// The run of blocks of one CTA, item by item.
+struct Walk {
+  int b, h, tile, off;
+  int64_t left, at;
+  Seq s;
+  __device__ __forceinline__ bool next(const AttendArgs& a, Segment& g) {
+    if (left <= 0) return false;
+    g.s = s;
+    g.b = b;
+    g.h = h;
+    g.t0 = tile * 2 * a.tok;
+    g.nt = min(2 * a.tok, s.n - g.t0);
+    g.pair = g.nt > a.tok;
+    g.k = span_of(a, s, g.t0, g.nt);
+    const int cost = max(g.k.blocks, 1);
+    const int take = (int)min(left, (int64_t)(cost - off));
+    g.j0 = g.k.jb + off;
+    g.nb = g.k.blocks ? take : 0;
+    g.whole = take == cost;
+    g.first = at - off;
+    g.last = g.first + cost;
+    at += take;
+    left -= take;
+    off = 0;
+    if (++tile * 2 * a.tok >= s.n) {
+      tile = 0;
+      if (++h == a.hkv) {
+        h = 0;
+        if (left > 0) {
+          do {
+            s = load_seq(a, ++b);
+          } while (s.n == 0 && b + 1 < a.b.n);
+        }
+      }
     }
-    const int64_t at = (((int64_t)blk * a.hkv + hk) * kBlockTokens + j % kBlockTokens) * a.d;
-    const T* kr = static_cast<const T*>(a.kb) + at;
-    const T* vr = static_cast<const T*>(a.vb) + at;
-    float s = 0.f;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 32 * i < a.d) s += qr[i] * ldf(kr + lane + 32 * i);
-    for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-    const float mn = fmaxf(m, s);
-    const float c = m == -INFINITY ? 0.f : __expf(m - mn), p = __expf(s - mn);
-    l = l * c + p;
-    for (int i = 0; i < 4; ++i)
-      if (lane + 32 * i < a.d) o[i] = o[i] * c + p * ldf(vr + lane + 32 * i);
-    m = mn;
+    return true;
   }
-  T* out = static_cast<T*>(a.out.p) + (int64_t)t * a.out.ts + (int64_t)h * a.out.hs;
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < a.d) stf(out + lane + 32 * i, l > 0 ? o[i] / l : 0.f);
-  if (a.lse && lane == 0) a.lse[id] = l > 0 ? m + logf(l) : -INFINITY;
+};
+
+// ---- shared memory ----
+
+template <int DP>
+struct Layout {
+  static constexpr int kHalf = kKeys * 128;                 // 128 rows of 64 elements
+  static constexpr int kStage = kHalf * (DP / 64);          // a tile of keys, values or queries
+  static constexpr int kStages = kRing / kStage;
+  static constexpr int kQ = 0;                              // two tiles of queries
+  static constexpr int kKv = 2 * kStage;
+  static constexpr int kCtl = kKv + kStages * kStage;
+};
+
+struct Control {
+  uint64_t kv_full[10], kv_empty[10];
+  uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t ml_full, ml_free, wg[2], drain;
+  float2 ml[kTile];  // m and l of stream 1 for the join
+  int64_t sum[kThreads / 32];
+  int64_t total, per;
+  int b, h, tile, off;
+  int last[2];
+  int abort;
+  uint32_t tmem;
+};
+template <int DP>
+constexpr int smem_bytes() { return 1024 + Layout<DP>::kCtl + (int)sizeof(Control); }
+static_assert(smem_bytes<128>() <= 227 * 1024, "shared memory of a CTA");
+static_assert(Layout<64>::kStages <= 10 && Layout<128>::kStages <= 10, "ring barriers");
+
+// A counter through a ring or a pair of phases.
+struct Ring {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int n) {
+    if (++at == n) {
+      at = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+// ---- the run of each CTA ----
+// Total of all items' blocks and the place where this CTA's run begins; every thread takes part.
+__device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Walk& w) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto seq_cost = [&](int b) -> int64_t {
+    if (b >= a.b.n) return 0;
+    const Seq s = load_seq(a, b);
+    int64_t sum = 0;
+    for (int t = 0, k = n_items(a, s); t < k; ++t) sum += item_cost(a, s, t);
+    return sum * a.hkv;
+  };
+  const int64_t first = seq_cost(tid);
+  int64_t sum = first;
+  for (int b = tid + kThreads; b < a.b.n; b += kThreads) sum += seq_cost(b);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) c->sum[warp] = sum;
+  __syncthreads();
+  int64_t total = 0;
+  for (int i = 0; i < kThreads / 32; ++i) total += c->sum[i];
+  const int64_t per = (total + gridDim.x - 1) / gridDim.x, lo = per * blockIdx.x;
+  if (lo >= total) return false;
+  int64_t base = 0;
+  for (int b0 = 0; base <= lo; b0 += kThreads) {
+    const int64_t v = b0 == 0 ? first : seq_cost(b0 + tid);
+    int64_t inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    __syncthreads();
+    if (lane == 31) c->sum[warp] = inc;
+    __syncthreads();
+    int64_t before = base;
+    for (int i = 0; i < kThreads / 32; ++i) {
+      if (i < warp) before += c->sum[i];
+      base += c->sum[i];
+    }
+    before += inc - v;
+    if (before <= lo && lo < before + v) {
+      const Seq s = load_seq(a, b0 + tid);
+      const int64_t head = v / a.hkv;
+      int64_t rest = lo - before;
+      c->b = b0 + tid;
+      c->h = (int)(rest / head);
+      rest -= c->h * head;
+      int t = 0;
+      for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
+      c->tile = t;
+      c->off = (int)rest;
+      c->per = per;
+    }
+  }
+  __syncthreads();
+  w.b = c->b;
+  w.h = c->h;
+  w.tile = c->tile;
+  w.off = c->off;
+  w.at = lo;
+  w.left = min(per, total - lo);
+  w.s = load_seq(a, w.b);
+  return true;
+}
+
+// ---- keys and values ----
+template <int DP>
+struct Loader {
+  using L = Layout<DP>;
+  const AttendArgs& a;
+  const CUtensorMap* map_k;
+  const CUtensorMap* map_v;
+  Control* c;
+  uint32_t kv;
+  Ring ring;
+
+  // The block of this lane's page (lanes 2i, 2i + 1 share page i of 8 where a head has two halves).
+  __device__ __forceinline__ int page(const Segment& g, int j) const {
+    const int i = (threadIdx.x & 31) / (DP / 64);
+    const int p = j * (kKeys / kBlockTokens) + i;
+    if (i >= kKeys / kBlockTokens || p * kBlockTokens >= g.k.to || (p + 1) * kBlockTokens <= g.k.from) return -1;
+    int blk = *(const volatile int32_t*)(a.b.table + (int64_t)g.b * a.b.stride + p);
+    if (blk < 0 || blk >= a.n_blocks) {
+      set_error(a.err, MISAT_ERR_INVALID_ARG);
+      blk = a.n_blocks;  // past the tensor: the box is filled with zeros
+    }
+    return blk;
+  }
+  __device__ __forceinline__ bool load(const Segment& g, const CUtensorMap* map, int blk) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t full = smem_u32(&c->kv_full[ring.at]);
+    if (!mbar_wait(smem_u32(&c->kv_empty[ring.at]), ring.phase ^ 1, &c->abort)) return false;
+    const int boxes = __popc(__ballot_sync(0xffffffffu, blk >= 0));
+    if (lane == 0) mbar_expect(full, boxes * kBlockTokens * 128);
+    __syncwarp();
+    if (blk >= 0) {
+      const int i = lane / (DP / 64), half = lane % (DP / 64);
+      const int row = blk < a.n_blocks ? blk * a.hkv + g.h : a.n_blocks * a.hkv;
+      tma_load_3d(kv + ring.at * L::kStage + half * L::kHalf + i * kBlockTokens * 128, map, full, half * 64, 0, row);
+    }
+    ring.step(L::kStages);
+    return true;
+  }
+  __device__ __forceinline__ void run(Walk w) {
+    Segment g;
+    while (w.next(a, g)) {
+      if (g.nb == 0) continue;
+      int cur = page(g, g.j0), ahead = g.nb > 1 ? page(g, g.j0 + 1) : -1;
+      if (!load(g, map_k, cur)) return;
+      if (!g.pair && g.nb > 1 && !load(g, map_k, ahead)) return;
+      for (int j = 0; j < g.nb; ++j) {
+        const int ahead2 = j + 2 < g.nb ? page(g, g.j0 + j + 2) : -1;
+        if (!load(g, map_v, cur)) return;
+        if (g.pair) {
+          if (j + 1 < g.nb && !load(g, map_k, ahead)) return;
+        } else {
+          if (j + 2 < g.nb && !load(g, map_k, ahead2)) return;
+        }
+        cur = ahead;
+        ahead = ahead2;
+      }
+    }
+  }
+  // After a wait that ran out: the copies still in flight are waited for, again for a bounded time.
+  __device__ __forceinline__ void drain() {
+    int go_on = 0;
+    for (int i = 0; i < L::kStages; ++i)
+      mbar_wait(smem_u32(&c->kv_full[i]), i < ring.at ? ring.phase : ring.phase ^ 1, &go_on);
+  }
+};
+
+// ---- queries ----
+// Which of the two query tiles a stream of a segment uses: both streams of a pair their own, else
+// the one tile that was not used last, so that the next item's queries load early.
+struct QuerySlots {
+  uint32_t phase[2] = {0, 0};
+  int turn = 0;
+  __device__ __forceinline__ int slot(const Segment& g, int st) const { return g.pair ? st : turn; }
+  __device__ __forceinline__ void step(const Segment& g) {
+    if (g.pair) {
+      phase[0] ^= 1;
+      phase[1] ^= 1;
+    } else {
+      phase[turn] ^= 1;
+      turn ^= 1;
+    }
+  }
+};
+
+template <class T, int DP>
+__device__ __forceinline__ void load_queries(const AttendArgs& a, Walk w, char* smem, Control* c) {
+  using L = Layout<DP>;
+  constexpr int kLoaders = 64, kChunks = DP / 8;  // 16-byte pieces of a row
+  const int tid = threadIdx.x - 320;
+  QuerySlots qs;
+  Segment g;
+  while (w.next(a, g)) {
+    if (g.nb == 0) continue;
+    for (int st = 0; st < (g.pair ? 2 : 1); ++st) {
+      const int slot = qs.slot(g, st);
+      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase[slot] ^ 1, &c->abort)) return;
+      const int t0 = st * a.tok, rows = min(a.tok, g.nt - t0) * a.group;
+      char* dst = smem + L::kQ + slot * L::kStage;
+      const T* src = static_cast<const T*>(a.q.p) + (int64_t)(g.s.begin + g.t0 + t0) * a.q.ts +
+                     (int64_t)g.h * a.group * a.q.hs;
+      const int n = rows * kChunks;
+      for (int i0 = tid; i0 < n; i0 += kLoaders * 4) {
+        uint4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + u * kLoaders, r = i / kChunks, ch = i % kChunks;
+          v[u] = make_uint4(0, 0, 0, 0);
+          if (i < n && ch * 8 < a.d) {
+            const int t = r / a.group;
+            const T* p = src + (int64_t)t * a.q.ts + (int64_t)(r - t * a.group) * a.q.hs + ch * 8;
+            if (a.vec_q) {
+              v[u] = *reinterpret_cast<const uint4*>(p);
+            } else {
+              const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
+              v[u] = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16,
+                                e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+            }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + u * kLoaders, r = i / kChunks, ch = i % kChunks;
+          if (i < n)
+            *reinterpret_cast<uint4*>(dst + (ch / 8) * L::kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[u];
+        }
+      }
+      fence_async_shared();
+      __syncwarp();
+      if ((tid & 31) == 0) mbar_arrive(smem_u32(&c->q_full[slot]));
+    }
+    qs.step(g);
+  }
+}
+
+// ---- matrix instructions ----
+// Tensor memory: S of stream 0 and 1 (128 columns each; the weights replace the scores in the first
+// 64), O of stream 0 and 1 (DP columns each).  Instructions of one thread execute in order, so S of
+// the next block may be issued right behind the product that reads the weights in its place.
+__device__ __forceinline__ uint32_t col_s(int st) { return st * 128; }
+template <int DP>
+__device__ __forceinline__ uint32_t col_o(int st) { return 256 + st * DP; }
+
+template <class T, int DP>
+struct Issuer {
+  using L = Layout<DP>;
+  static constexpr bool kBf16 = std::is_same_v<T, __nv_bfloat16>;
+  const AttendArgs& a;
+  Control* c;
+  char* smem;
+  uint32_t base, tmem;
+  Ring ring;
+  uint32_t p_phase[2] = {0, 0};
+
+  // Stage of the next tile, once it has landed (-1: gave up).
+  __device__ __forceinline__ int take() {
+    const int at = ring.at;
+    const bool ok = mbar_wait(smem_u32(&c->kv_full[at]), ring.phase, &c->abort);
+    ring.step(L::kStages);
+    return ok ? at : -1;
+  }
+  __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
+  __device__ __forceinline__ bool lead() const { return (threadIdx.x & 31) == 0; }
+
+  __device__ __forceinline__ void scores(int st, int slot, int stage, bool last_use) {
+    if (!lead()) return;
+    const uint32_t q = base + L::kQ + slot * L::kStage, k = base + L::kKv + stage * L::kStage;
+    const uint32_t id = mma_desc(kBf16, 128, kKeys, false);
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const uint32_t at = (i / 4) * L::kHalf + (i % 4) * 32;
+      mma_ss(tmem + col_s(st), smem_desc(q + at, 16, 1024), smem_desc(k + at, 16, 1024), id, i > 0);
+    }
+    mma_commit(smem_u32(&c->s_full[st]));
+    if (last_use) release(stage);
+  }
+  // O of the stream (+)= weights times the values of block j; rows of V that no row of the item may
+  // see (past the sequence's end they hold anything) are cleared first.
+  __device__ __forceinline__ bool product(const Segment& g, int st, int stage, int j, bool clear, bool fresh,
+                                          bool last_use, bool last) {
+    if (clear) {
+      const int lo = max(g.k.from - j * kKeys, 0), hi = min(g.k.to - j * kKeys, kKeys);
+      if (lo > 0 || hi < kKeys) {
+        char* v = smem + L::kKv + stage * L::kStage;
+        const int lane = threadIdx.x & 31, gone = lo + kKeys - hi;
+        for (int i = lane; i < gone * (DP / 8); i += 32) {
+          const int r = i / (DP / 8), ch = i % (DP / 8), row = r < lo ? r : hi + r - lo;
+          *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async_shared();
+        __syncwarp();
+      }
+    }
+    if (!mbar_wait(smem_u32(&c->p_full[st]), p_phase[st], &c->abort)) return false;
+    p_phase[st] ^= 1;
+    tc_fence_after();
+    if (!lead()) return true;
+    const uint32_t v = base + L::kKv + stage * L::kStage;
+    const uint32_t id = mma_desc(kBf16, 128, DP, true);
+#pragma unroll
+    for (int i = 0; i < kKeys / 16; ++i)
+      mma_ts(tmem + col_o<DP>(st), tmem + col_s(st) + i * 8, smem_desc(v + i * 16 * 128, L::kHalf, 1024), id,
+             !fresh || i > 0);
+    if (last_use) release(stage);
+    if (last) mma_commit(smem_u32(&c->o_full[st]));
+    return true;
+  }
+  __device__ __forceinline__ void run(Walk w) {
+    QuerySlots qs;
+    Segment g;
+    while (w.next(a, g)) {
+      const int n = g.nb;
+      if (n == 0) continue;
+      const int q0 = qs.slot(g, 0), q1 = qs.slot(g, 1);
+      if (!mbar_wait(smem_u32(&c->q_full[q0]), qs.phase[q0], &c->abort)) return;
+      if (g.pair && !mbar_wait(smem_u32(&c->q_full[q1]), qs.phase[q1], &c->abort)) return;
+      tc_fence_after();
+      int k = take();
+      if (k < 0) return;
+      if (g.pair) {
+        scores(0, q0, k, false);
+        scores(1, q1, k, true);
+        if (n == 1 && lead()) {
+          mma_commit(smem_u32(&c->q_empty[q0]));
+          mma_commit(smem_u32(&c->q_empty[q1]));
+        }
+        for (int j = 0; j < n; ++j) {
+          const int v = take();
+          if (v < 0) return;
+          if (!product(g, 0, v, g.j0 + j, true, j == 0, false, j + 1 == n)) return;
+          if (j + 1 < n) {
+            if ((k = take()) < 0) return;
+            scores(0, q0, k, false);
+          }
+          if (!product(g, 1, v, g.j0 + j, false, j == 0, true, j + 1 == n)) return;
+          if (j + 1 < n) {
+            scores(1, q1, k, true);
+            if (j + 2 == n && lead()) {
+              mma_commit(smem_u32(&c->q_empty[q0]));
+              mma_commit(smem_u32(&c->q_empty[q1]));
+            }
+          }
+        }
+      } else {
+        scores(0, q0, k, true);
+        if (n > 1) {
+          if ((k = take()) < 0) return;
+          scores(1, q0, k, true);
+        }
+        if (n <= 2 && lead()) mma_commit(smem_u32(&c->q_empty[q0]));
+        for (int j = 0; j < n; ++j) {
+          const int st = j & 1, v = take();
+          if (v < 0) return;
+          if (!product(g, st, v, g.j0 + j, true, j < 2, true, j + 2 >= n)) return;
+          if (j + 2 < n) {
+            if ((k = take()) < 0) return;
+            scores(st, q0, k, true);
+            if (j + 3 == n && lead()) mma_commit(smem_u32(&c->q_empty[q0]));
+          }
+        }
+      }
+      qs.step(g);
+    }
+  }
+  // After a wait that ran out: the instructions issued are waited for before tensor memory is freed.
+  __device__ __forceinline__ void drain() {
+    int go_on = 0;
+    if (lead()) mma_commit(smem_u32(&c->drain));
+    __syncwarp();
+    mbar_wait(smem_u32(&c->drain), 0, &go_on);
+  }
+};
+
+// ---- softmax ----
+template <class T>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack16<__nv_bfloat16>(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <>
+__device__ __forceinline__ uint32_t pack16<__half>(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <class T, int DP>
+struct Softmax {
+  const AttendArgs& a;
+  Control* c;
+  uint32_t tmem;  // with the warp's lanes
+  int st;         // stream
+  int row;        // row of the tile = lane of tensor memory
+  uint32_t s_phase = 0, o_phase[2] = {0, 0}, wg_phase = 0, ml_phase = 0;
+  bool joined = false;  // stream 1: its last item was joined by stream 0
+
+  // One block: scores to weights, with the running reference m and sum l.
+  __device__ __forceinline__ void block(int lo, int hi, bool mask, bool fresh, float& m, float& l) {
+    uint32_t r[128];
+    tmem_ld128(r, tmem + col_s(st));
+    if (mask) {
+#pragma unroll
+      for (int i = 0; i < 128; ++i)
+        if (i < lo || i >= hi) r[i] = 0xff800000u;
+    }
+    float mx[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(r[k]);
+#pragma unroll
+    for (int i = 4; i < 124; i += 8)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(r[i + k]), __uint_as_float(r[i + 4 + k]));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(r[124 + k]));
+    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    if (fresh) {
+      m = top;
+    } else {
+      const bool need = top > m && !((top - m) * a.c <= kRescale);
+      if (__any_sync(0xffffffffu, need)) {
+        const float f = need ? exp2_approx((m - top) * a.c) : 1.f;  // m = -inf: 0
+        const uint64_t f2 = pack2(f, f);
+#pragma unroll
+        for (int q = 0; q < DP / 32; ++q) {
+          uint32_t o[32];
+          tmem_ld32(o, tmem + col_o<DP>(st) + q * 32);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float x, y;
+            unpack2(mul2(pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), f2), x, y);
+            o[i] = __float_as_uint(x);
+            o[i + 1] = __float_as_uint(y);
+          }
+          tmem_st32(tmem + col_o<DP>(st) + q * 32, o);
+        }
+        l *= f;
+        if (need) m = top;
+      }
+    }
+    const float ref = m == -INFINITY ? 0.f : -m * a.c;
+    const uint64_t c2 = pack2(a.c, a.c), ref2 = pack2(ref, ref);
+    uint64_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      uint32_t p[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int at = q * 64 + 2 * i;
+        float x, y;
+        unpack2(fma2(pack2(__uint_as_float(r[at]), __uint_as_float(r[at + 1])), c2, ref2), x, y);
+        x = exp2_approx(x);
+        y = exp2_approx(y);
+        sum[i & 3] = add2(sum[i & 3], pack2(x, y));
+        p[i] = pack16<T>(x, y);
+      }
+      tmem_st32(tmem + col_s(st) + q * 32, p);
+    }
+    float x, y;
+    unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), x, y);
+    l += x + y;
+  }
+
+  __device__ __forceinline__ bool wg_sync() {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->wg[st]));
+    const bool ok = mbar_wait(smem_u32(&c->wg[st]), wg_phase, &c->abort);
+    wg_phase ^= 1;
+    return ok;
+  }
+
+  __device__ __forceinline__ T* out_row(const Segment& g, int t0, int r) const {
+    const int t = r / a.group;
+    return static_cast<T*>(a.out.p) + (int64_t)(g.s.begin + g.t0 + t0 + t) * a.out.ts +
+           (int64_t)(g.h * a.group + r - t * a.group) * a.out.hs;
+  }
+  __device__ __forceinline__ void put_lse(const Segment& g, int t0, int r, float m, float l) const {
+    if (!a.lse) return;
+    const int t = r / a.group;
+    a.lse[(int64_t)(g.s.begin + g.t0 + t0 + t) * (a.group * a.hkv) + g.h * a.group + r - t * a.group] =
+        l > 0.f || l != l ? m * a.scale + logf(l) : -INFINITY;
+  }
+  // Eight elements of an output row.
+  __device__ __forceinline__ void put8(T* p, const float (&x)[8]) const {
+    const uint4 v = make_uint4(pack16<T>(x[0], x[1]), pack16<T>(x[2], x[3]), pack16<T>(x[4], x[5]),
+                               pack16<T>(x[6], x[7]));
+    if (a.vec_out) {
+      *reinterpret_cast<uint4*>(p) = v;
+    } else {
+      uint16_t* e = reinterpret_cast<uint16_t*>(p);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    }
+  }
+
+  // Results of a tile, or its partial sums.  join: O, m and l of stream 1 belong to the same rows.
+  __device__ __forceinline__ void finish(const Segment& g, int t0, int rows, bool join, float m, float l) {
+    float w0 = 1.f, w1 = 0.f;
+    if (join) {
+      const float2 o = c->ml[row];
+      const float top = fmaxf(m, o.x);
+      w0 = m == top ? 1.f : exp2_approx((m - top) * a.c);  // equal also when both are -infinity
+      w1 = o.x == top ? 1.f : exp2_approx((o.x - top) * a.c);
+      l = l * w0 + o.y * w1;
+      m = top;
+    }
+    const bool mine = row < rows;
+    const int warp_rows = rows - (row & ~31);
+    const int slot = g.whole ? 0 : (int)((blockIdx.x * 2 + (g.first >= c->per * blockIdx.x)) * 2 + st);
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    T* out = mine ? out_row(g, t0, row) : nullptr;
+    if (warp_rows > 0) {
+#pragma unroll
+      for (int q = 0; q < DP / 32; ++q) {
+        uint32_t o[32], o1[32];
+        __syncwarp();
+        tmem_ld32(o, tmem + col_o<DP>(st) + q * 32);
+        if (join) tmem_ld32(o1, tmem + col_o<DP>(1) + q * 32);
+#pragma unroll
+        for (int e = 0; e < 32 && mine; e += 8) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] = __uint_as_float(o[e + i]);
+            if (join) x[i] = x[i] * w0 + __uint_as_float(o1[e + i]) * w1;
+          }
+          if (g.whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= inv;
+            if (q * 32 + e < a.d) put8(out + q * 32 + e, x);
+          } else {
+            float4* p = a.ws_o + ((int64_t)slot * (DP / 4) + (q * 32 + e) / 4) * kTile + row;
+            p[0] = make_float4(x[0], x[1], x[2], x[3]);
+            p[kTile] = make_float4(x[4], x[5], x[6], x[7]);
+          }
+        }
+      }
+    }
+    if (mine) {
+      if (g.whole) put_lse(g, t0, row, m, l);
+      else a.ws_ml[slot * kTile + row] = make_float2(m, l);
+    }
+  }
+
+  // The item is split between CTAs c0..c1: the last of them to arrive adds the parts.
+  __device__ __forceinline__ bool arrive(const Segment& g, int t0, int rows) {
+    const int64_t per = c->per;
+    const int c0 = (int)(g.first / per), c1 = (int)((g.last - 1) / per);
+    const int wt = threadIdx.x & 127;
+    __threadfence();
+    if (!wg_sync()) return false;
+    if (wt == 0) {
+      const unsigned before = atomicAdd(a.ctr + c0 * 2 + st, 1u);
+      c->last[st] = before == (unsigned)(c1 - c0);
+    }
+    if (!wg_sync()) return false;
+    if (!c->last[st]) return true;
+    __threadfence();
+    if (wt == 0) a.ctr[c0 * 2 + st] = 0;
+    const int n = rows * (a.d / 8);
+    int have = -1;
+    float top = 0.f;
+    for (int i = wt; i < n; i += 128) {
+      const int r = i % rows, g8 = i / rows;
+      if (r != have) {
+        have = r;
+        top = -INFINITY;
+        for (int p = c0; p <= c1; ++p) top = fmaxf(top, __ldcg(a.ws_ml + ((p * 2 + (p == c0)) * 2 + st) * kTile + r).x);
+      }
+      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0.f;
+#pragma unroll 4
+      for (int p = c0; p <= c1; ++p) {
+        const int slot = (p * 2 + (p == c0)) * 2 + st;
+        const float2 ml = __ldcg(a.ws_ml + slot * kTile + r);
+        const float4* o = a.ws_o + ((int64_t)slot * (DP / 4) + g8 * 2) * kTile + r;
+        const float4 u = __ldcg(o), v = __ldcg(o + kTile);
+        const float f = ml.x == top ? 1.f : exp2_approx((ml.x - top) * a.c);
+        sum += ml.y * f;
+        x[0] += u.x * f;
+        x[1] += u.y * f;
+        x[2] += u.z * f;
+        x[3] += u.w * f;
+        x[4] += v.x * f;
+        x[5] += v.y * f;
+        x[6] += v.z * f;
+        x[7] += v.w * f;
+      }
+      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] *= inv;
+      put8(out_row(g, t0, r) + g8 * 8, x);
+      if (g8 == 0) put_lse(g, t0, r, top, sum);
+    }
+    return true;
+  }
+
+  __device__ __forceinline__ void run(Walk w) {
+    Segment g;
+    while (w.next(a, g)) {
+      const int t0 = g.pair ? st * a.tok : 0;
+      const int rows = min(a.tok, g.nt - t0) * a.group;
+      if (g.nb == 0) {  // no row sees a key
+        if ((g.pair || st == 0) && row < rows) {
+          T* out = out_row(g, t0, row);
+          const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          for (int e = 0; e < a.d; e += 8) put8(out + e, zero);
+          put_lse(g, t0, row, 0.f, 0.f);
+        }
+        continue;
+      }
+      const bool active = (row & ~31) < rows;
+      const int p0 = g.s.len - g.s.n + g.t0 + t0;        // position of the tile's first token
+      const int p1 = p0 + min(a.tok, g.nt - t0) - 1;     // and of its last
+      const int pos = row < rows ? p0 + row / a.group : -1;
+      float m = -INFINITY, l = 0.f;
+      const int nb = g.stream_blocks(st);
+      for (int i = 0; i < nb; ++i) {
+        const int k0 = (g.j0 + (g.pair ? i : 2 * i + st)) * kKeys;
+        if (!mbar_wait(smem_u32(&c->s_full[st]), s_phase, &c->abort)) return;
+        s_phase ^= 1;
+        if (active) {
+          tc_fence_after();
+          const bool mask = k0 + kKeys > p0 + 1 || (a.window > 0 && p1 - k0 >= a.window);
+          const int hi = pos + 1 - k0, lo = a.window > 0 && pos - k0 >= a.window ? pos - k0 - a.window + 1 : 0;
+          block(lo, hi, mask, i == 0, m, l);
+          tc_wait_st();
+          tc_fence_before();
+        }
+        // the join of the item before has to have read this stream's O before it is overwritten
+        if (joined) {
+          if (!mbar_wait(smem_u32(&c->ml_free), ml_phase ^ 1, &c->abort)) return;
+          joined = false;
+          tc_fence_after();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->p_full[st]));
+      }
+      const bool join = !g.pair && g.nb > 1;
+      if (nb > 0) {
+        if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase[st], &c->abort)) return;
+        o_phase[st] ^= 1;
+      }
+      if (join && st == 1) {
+        c->ml[row] = make_float2(m, l);
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->ml_full));
+        ml_phase ^= 1;
+        joined = true;
+        continue;
+      }
+      if (st == 1 && !g.pair) continue;
+      if (join) {
+        if (!mbar_wait(smem_u32(&c->o_full[1]), o_phase[1], &c->abort)) return;
+        if (!mbar_wait(smem_u32(&c->ml_full), ml_phase, &c->abort)) return;
+        ml_phase ^= 1;
+      }
+      if (st == 0 && (join || g.pair)) o_phase[1] ^= 1;
+      tc_fence_after();
+      finish(g, t0, rows, join, m, l);
+      tc_fence_before();
+      if (join) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->ml_free));
+      }
+      if (!g.whole && !arrive(g, t0, rows)) return;
+    }
+  }
+};
+
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_attend(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k,
+             const __grid_constant__ CUtensorMap map_v) {
+  using L = Layout<DP>;
+  extern __shared__ char raw[];
+  char* smem = raw + (((smem_u32(raw) + 1023) & ~1023u) - smem_u32(raw));
+  Control* c = reinterpret_cast<Control*>(smem + L::kCtl);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < L::kStages; ++i) {
+      mbar_init(smem_u32(&c->kv_full[i]), 1);
+      mbar_init(smem_u32(&c->kv_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&c->q_full[i]), 2);
+      mbar_init(smem_u32(&c->q_empty[i]), 1);
+      mbar_init(smem_u32(&c->s_full[i]), 1);
+      mbar_init(smem_u32(&c->p_full[i]), 4);
+      mbar_init(smem_u32(&c->o_full[i]), 1);
+      mbar_init(smem_u32(&c->wg[i]), 4);
+    }
+    mbar_init(smem_u32(&c->ml_full), 4);
+    mbar_init(smem_u32(&c->ml_free), 4);
+    mbar_init(smem_u32(&c->drain), 1);
+    c->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_shared();
+  }
+  if (warp == 9) tmem_alloc(smem_u32(&c->tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = c->tmem;
+  chain_wait();
+  Walk w;
+  if (find_run(a, c, w)) {
+    if (warp < 8) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+      Softmax<T, DP> s{a, c, tmem + ((uint32_t)(warp & 3) << 21), warp / 4, (int)(threadIdx.x & 127)};
+      s.run(w);
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
+      if (warp == 8) {
+        Loader<DP> ld{a, &map_k, &map_v, c, smem_u32(smem) + L::kKv};
+        ld.run(w);
+        if (*(volatile int*)&c->abort) ld.drain();
+      } else if (warp == 9) {
+        Issuer<T, DP> is{a, c, smem, smem_u32(smem), tmem};
+        is.run(w);
+        if (*(volatile int*)&c->abort) is.drain();
+      } else {
+        load_queries<T, DP>(a, w, smem, c);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) tmem_free(tmem, 512);
+  if (threadIdx.x == 0 && c->abort) set_error(a.err, MISAT_ERR_INTERNAL);
+}
+
+template <class T, int DP>
+int allow_smem() {
+  return cudaFuncSetAttribute(k_attend<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<DP>()) ==
+                 cudaSuccess
+             ? MISAT_OK
+             : MISAT_ERR_CUDA;
+}
+
+template <class T, int DP>
+void launch(const misat_kv* kv, const AttendArgs& a, cudaStream_t st) {
+  launch_chained(k_attend<T, DP>, kv->num_sms, kThreads, smem_bytes<DP>(), st, a, kv->map_k, kv->map_v);
 }
 
 }  // namespace
 
 namespace misat {
 
+int attend_prepare(misat_kv* kv) {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess)
+    return MISAT_ERR_CUDA;
+  const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
+  // [blocks x kv heads][16][d]; a box is 64 elements of the 16 tokens of one block and head.  Elements past d
+  // are filled with zeros, so a head of any size up to 64 or 128 uses the whole tile.
+  const cuuint64_t dims[3] = {(cuuint64_t)kv->d, kBlockTokens, (cuuint64_t)kv->n_blocks * kv->hkv};
+  const cuuint64_t strides[2] = {(cuuint64_t)kv->d * 2, (cuuint64_t)kv->d * 2 * kBlockTokens};
+  const cuuint32_t box[3] = {64, kBlockTokens, 1}, unit[3] = {1, 1, 1};
+  for (int i = 0; i < 2; ++i) {
+    const CUresult r = encode(i ? &kv->map_v : &kv->map_k,
+                              kv->dtype == MISAT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              3, i ? kv->vb : kv->kb, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return MISAT_ERR_CUDA;
+  }
+  const bool bf = kv->dtype == MISAT_BF16;
+  const int dp = kv->d > 64 ? 128 : 64;
+  const int rc = dp == 128 ? (bf ? allow_smem<__nv_bfloat16, 128>() : allow_smem<__half, 128>())
+                           : (bf ? allow_smem<__nv_bfloat16, 64>() : allow_smem<__half, 64>());
+  if (rc != MISAT_OK) return rc;
+  const size_t slots = (size_t)kv->num_sms * 4;
+  if (cudaMalloc(&kv->ws_o, slots * dp * kTile * sizeof(float)) != cudaSuccess ||
+      cudaMalloc(&kv->ws_ml, slots * kTile * sizeof(float2)) != cudaSuccess ||
+      cudaMalloc(&kv->ctr, kv->num_sms * 2 * sizeof(unsigned)) != cudaSuccess)
+    return MISAT_ERR_OOM;
+  return cudaMemset(kv->ctr, 0, kv->num_sms * 2 * sizeof(unsigned)) == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA;
+}
+
 void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,
                    cudaStream_t st) {
-  AttendArgs a{b, q, out, kv->kb, kv->vb, lse, kv->scale, kv->hq, kv->hq / kv->hkv, kv->hkv, kv->d, kv->n_blocks,
-               window, kv->err};
-  const int64_t warps = (int64_t)b.n_tokens * kv->hq;
-  const int grid = (int)((warps + 3) / 4);
-  if (kv->dtype == MISAT_BF16) launch_chained(k_attend<__nv_bfloat16>, grid, 128, 0, st, a);
-  else launch_chained(k_attend<__half>, grid, 128, 0, st, a);
+  const int group = kv->hq / kv->hkv;
+  AttendArgs a{b, q, out, lse, kv->scale, kv->scale * 1.4426950408889634f, group, kv->hkv, kv->d, kv->n_blocks, window,
+               kTile / group, aligned16(q, 2), aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+  const bool bf = kv->dtype == MISAT_BF16;
+  if (kv->d > 64) bf ? launch<__nv_bfloat16, 128>(kv, a, st) : launch<__half, 128>(kv, a, st);
+  else bf ? launch<__nv_bfloat16, 64>(kv, a, st) : launch<__half, 64>(kv, a, st);
 }
 
 }  // namespace misat

@@ -39,8 +39,10 @@ int misat_kv_create(const misat_kv_config* c, misat_kv** out) {
     rc = MISAT_ERR_CUDA;
   else if (cudaMalloc(&kv->err, sizeof(int32_t)) != cudaSuccess)
     rc = MISAT_ERR_OOM;
-  else if (cudaMemset(kv->err, 0, sizeof(int32_t)) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess)
+  else if (cudaMemset(kv->err, 0, sizeof(int32_t)) != cudaSuccess)
     rc = MISAT_ERR_CUDA;
+  if (rc == MISAT_OK) rc = attend_prepare(kv);
+  if (rc == MISAT_OK && cudaDeviceSynchronize() != cudaSuccess) rc = MISAT_ERR_CUDA;
   if (rc != MISAT_OK) {
     cudaGetLastError();
     misat_kv_destroy(kv);
@@ -53,6 +55,9 @@ int misat_kv_create(const misat_kv_config* c, misat_kv** out) {
 int misat_kv_destroy(misat_kv* kv) {
   if (!kv) return MISAT_ERR_INVALID_ARG;
   cudaFree(kv->err);
+  cudaFree(kv->ws_o);
+  cudaFree(kv->ws_ml);
+  cudaFree(kv->ctr);
   delete kv;
   return MISAT_OK;
 }

@@ -1,6 +1,7 @@
 // Internal definitions of the KV block operators: handles and the launches behind the C ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -25,6 +26,11 @@ struct misat_kv {
   void* kb;
   void* vb;
   int32_t* err;  // device, sticky
+  // of the attention kernel: maps of the blocks, partial sums of split items, their arrivals
+  CUtensorMap map_k, map_v;
+  float4* ws_o;
+  float2* ws_ml;
+  unsigned* ctr;
 };
 
 namespace misat {
@@ -59,6 +65,10 @@ inline KvBatch batch_view(const misat_kv_batch* b) {
   return {b->n, b->n_tokens, b->max_q, b->q_off, b->kv_len, b->block_table, b->table_stride};
 }
 
+inline bool aligned16(const Heads& h, int elem) {
+  return !h.p || ((reinterpret_cast<uintptr_t>(h.p) | (uintptr_t)(h.ts * elem) | (uintptr_t)(h.hs * elem)) & 15) == 0;
+}
+
 // The handle's device is the current one.
 inline bool on_device(int device) {
   int d = -1;
@@ -68,6 +78,8 @@ inline bool on_device(int device) {
 // Return code of the launches just made.
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA; }
 
+// Maps and workspace of the attention kernel; MISAT_OK or an error code.
+int attend_prepare(misat_kv* kv);
 void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,
                    cudaStream_t st);
 

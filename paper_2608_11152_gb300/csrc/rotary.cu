@@ -240,10 +240,6 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ Rot
   }
 }
 
-bool aligned16(const Heads& h, int elem) {
-  return !h.p || ((reinterpret_cast<uintptr_t>(h.p) | (uintptr_t)(h.ts * elem) | (uintptr_t)(h.hs * elem)) & 15) == 0;
-}
-
 template <class T>
 void launch_rotate_t(RotArgs& a, int layout, int num_sms, cudaStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
