@@ -31,11 +31,12 @@ using namespace misat;
 namespace {
 
 constexpr int kKeys = 128;     // keys of a block
+constexpr int kPages = kKeys / kBlockTokens;
 constexpr int kTile = 128;     // rows of a stream's tile
 constexpr int kThreads = 384;
 constexpr int kRing = 160 * 1024;  // bytes of the ring of key and value tiles
 constexpr float kRescale = 8.f;    // log2 of the largest weight before a rescale
-constexpr int kRegsIssue = 88, kRegsSoftmax = 208;  // 128 * 88 + 256 * 208 = 384 * 168 registers
+constexpr int kRegsIssue = 152, kRegsSoftmax = 176;  // 128 * 152 + 256 * 176 = 384 * 168 registers
 
 struct AttendArgs {
   KvBatch b;
@@ -148,6 +149,10 @@ struct Layout {
 };
 
 struct Control {
+  struct {
+    Walk w;
+    Segment g;
+  } part[8];  // of each softmax warp: the scores need the registers
   uint64_t kv_full[10], kv_empty[10];
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
   uint64_t ml_full, ml_free, wg[2], drain;
@@ -160,7 +165,7 @@ struct Control {
   uint32_t tmem;
 };
 template <int DP>
-constexpr int smem_bytes() { return 1024 + Layout<DP>::kCtl + (int)sizeof(Control); }
+constexpr int smem_bytes() { return Layout<DP>::kCtl + (int)sizeof(Control); }
 static_assert(smem_bytes<128>() <= 227 * 1024, "shared memory of a CTA");
 static_assert(Layout<64>::kStages <= 10 && Layout<128>::kStages <= 10, "ring barriers");
 
@@ -252,28 +257,33 @@ struct Loader {
   uint32_t kv;
   Ring ring;
 
-  // The block of this lane's page (lanes 2i, 2i + 1 share page i of 8 where a head has two halves).
+  // Pages [lo, hi) of key block j hold keys that some row of the item sees; a lane has one box of one page.
+  static __device__ __forceinline__ int lo_page(const Segment& g, int j) {
+    return max(g.k.from / kBlockTokens - j * kPages, 0);
+  }
+  static __device__ __forceinline__ int hi_page(const Segment& g, int j) {
+    return min((g.k.to + kBlockTokens - 1) / kBlockTokens - j * kPages, kPages);
+  }
+  // The table's entry for this lane's page; read a block ahead of its use, and checked there.
   __device__ __forceinline__ int page(const Segment& g, int j) const {
     const int i = (threadIdx.x & 31) / (DP / 64);
-    const int p = j * (kKeys / kBlockTokens) + i;
-    if (i >= kKeys / kBlockTokens || p * kBlockTokens >= g.k.to || (p + 1) * kBlockTokens <= g.k.from) return -1;
-    int blk = *(const volatile int32_t*)(a.b.table + (int64_t)g.b * a.b.stride + p);
-    if (blk < 0 || blk >= a.n_blocks) {
-      set_error(a.err, MISAT_ERR_INVALID_ARG);
-      blk = a.n_blocks;  // past the tensor: the box is filled with zeros
-    }
-    return blk;
+    return i >= lo_page(g, j) && i < hi_page(g, j)
+               ? __ldcg(a.b.table + (int64_t)g.b * a.b.stride + j * kPages + i)
+               : 0;
   }
-  __device__ __forceinline__ bool load(const Segment& g, const CUtensorMap* map, int blk) {
-    const int lane = threadIdx.x & 31;
+  __device__ __forceinline__ bool load(const Segment& g, const CUtensorMap* map, int j, int blk) {
+    const int lane = threadIdx.x & 31, lo = lo_page(g, j), hi = hi_page(g, j);
     const uint32_t full = smem_u32(&c->kv_full[ring.at]);
     if (!mbar_wait(smem_u32(&c->kv_empty[ring.at]), ring.phase ^ 1, &c->abort)) return false;
-    const int boxes = __popc(__ballot_sync(0xffffffffu, blk >= 0));
-    if (lane == 0) mbar_expect(full, boxes * kBlockTokens * 128);
+    if (lane == 0) mbar_expect(full, (hi - lo) * (DP / 64) * kBlockTokens * 128);
     __syncwarp();
-    if (blk >= 0) {
-      const int i = lane / (DP / 64), half = lane % (DP / 64);
-      const int row = blk < a.n_blocks ? blk * a.hkv + g.h : a.n_blocks * a.hkv;
+    const int i = lane / (DP / 64), half = lane % (DP / 64);
+    if (i >= lo && i < hi) {
+      int row = blk * a.hkv + g.h;
+      if (blk < 0 || blk >= a.n_blocks) {
+        set_error(a.err, MISAT_ERR_INVALID_ARG);
+        row = a.n_blocks * a.hkv;  // past the tensor: the box is filled with zeros
+      }
       tma_load_3d(kv + ring.at * L::kStage + half * L::kHalf + i * kBlockTokens * 128, map, full, half * 64, 0, row);
     }
     ring.step(L::kStages);
@@ -283,16 +293,16 @@ struct Loader {
     Segment g;
     while (w.next(a, g)) {
       if (g.nb == 0) continue;
-      int cur = page(g, g.j0), ahead = g.nb > 1 ? page(g, g.j0 + 1) : -1;
-      if (!load(g, map_k, cur)) return;
-      if (!g.pair && g.nb > 1 && !load(g, map_k, ahead)) return;
-      for (int j = 0; j < g.nb; ++j) {
-        const int ahead2 = j + 2 < g.nb ? page(g, g.j0 + j + 2) : -1;
-        if (!load(g, map_v, cur)) return;
+      int cur = page(g, g.j0), ahead = g.nb > 1 ? page(g, g.j0 + 1) : 0;
+      if (!load(g, map_k, g.j0, cur)) return;
+      if (!g.pair && g.nb > 1 && !load(g, map_k, g.j0 + 1, ahead)) return;
+      for (int j = g.j0, end = g.j0 + g.nb; j < end; ++j) {
+        const int ahead2 = j + 2 < end ? page(g, j + 2) : 0;
+        if (!load(g, map_v, j, cur)) return;
         if (g.pair) {
-          if (j + 1 < g.nb && !load(g, map_k, ahead)) return;
+          if (j + 1 < end && !load(g, map_k, j + 1, ahead)) return;
         } else {
-          if (j + 2 < g.nb && !load(g, map_k, ahead2)) return;
+          if (j + 2 < end && !load(g, map_k, j + 2, ahead2)) return;
         }
         cur = ahead;
         ahead = ahead2;
@@ -402,16 +412,16 @@ struct Issuer {
     return ok ? at : -1;
   }
   __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
-  __device__ __forceinline__ bool lead() const { return (threadIdx.x & 31) == 0; }
+  static __device__ __forceinline__ bool lead() { return elect_one(); }
 
   __device__ __forceinline__ void scores(int st, int slot, int stage, bool last_use) {
+    const uint32_t q = desc_lo(base + L::kQ + slot * L::kStage, 16), k = desc_lo(base + L::kKv + stage * L::kStage, 16);
+    const uint32_t d = tmem + col_s(st);
     if (!lead()) return;
-    const uint32_t q = base + L::kQ + slot * L::kStage, k = base + L::kKv + stage * L::kStage;
-    const uint32_t id = mma_desc(kBf16, 128, kKeys, false);
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
-      const uint32_t at = (i / 4) * L::kHalf + (i % 4) * 32;
-      mma_ss(tmem + col_s(st), smem_desc(q + at, 16, 1024), smem_desc(k + at, 16, 1024), id, i > 0);
+      const uint32_t at = ((i / 4) * L::kHalf + (i % 4) * 32) / 16;
+      mma_ss(d, q + at, k + at, desc_hi(1024), mma_desc(kBf16, 128, kKeys, false), i > 0);
     }
     mma_commit(smem_u32(&c->s_full[st]));
     if (last_use) release(stage);
@@ -436,13 +446,12 @@ struct Issuer {
     if (!mbar_wait(smem_u32(&c->p_full[st]), p_phase[st], &c->abort)) return false;
     p_phase[st] ^= 1;
     tc_fence_after();
+    const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
+    const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
     if (!lead()) return true;
-    const uint32_t v = base + L::kKv + stage * L::kStage;
-    const uint32_t id = mma_desc(kBf16, 128, DP, true);
 #pragma unroll
     for (int i = 0; i < kKeys / 16; ++i)
-      mma_ts(tmem + col_o<DP>(st), tmem + col_s(st) + i * 8, smem_desc(v + i * 16 * 128, L::kHalf, 1024), id,
-             !fresh || i > 0);
+      mma_ts(d, p + i * 8, v + i * 16 * 128 / 16, desc_hi(1024), mma_desc(kBf16, 128, DP, true), !fresh || i > 0);
     if (last_use) release(stage);
     if (last) mma_commit(smem_u32(&c->o_full[st]));
     return true;
@@ -539,24 +548,33 @@ struct Softmax {
   uint32_t s_phase = 0, o_phase[2] = {0, 0}, wg_phase = 0, ml_phase = 0;
   bool joined = false;  // stream 1: its last item was joined by stream 0
 
-  // One block: scores to weights, with the running reference m and sum l.
-  __device__ __forceinline__ void block(int lo, int hi, bool mask, bool fresh, float& m, float& l) {
-    uint32_t r[128];
-    tmem_ld128(r, tmem + col_s(st));
-    if (mask) {
+  // Scores 32 q .. 32 q + 31 of the row: the hidden ones to -infinity.
+  static __device__ __forceinline__ void hide(uint32_t (&r)[32], int q, int lo, int hi) {
 #pragma unroll
-      for (int i = 0; i < 128; ++i)
-        if (i < lo || i >= hi) r[i] = 0xff800000u;
-    }
-    float mx[4];
+    for (int i = 0; i < 32; ++i)
+      if ((uint32_t)(q * 32 + i - lo) >= (uint32_t)(hi - lo)) r[i] = 0xff800000u;
+  }
+  static __device__ __forceinline__ void top_of(const uint32_t (&r)[32], float (&mx)[4]) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(r[k]);
-#pragma unroll
-    for (int i = 4; i < 124; i += 8)
+    for (int i = 0; i < 32; i += 8)
 #pragma unroll
       for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(r[i + k]), __uint_as_float(r[i + 4 + k]));
+  }
+
+  // One block: scores to weights, with the running reference m and sum l.  The scores are read twice,
+  // once for the maximum and once for the weights: 128 of them held meanwhile do not fit the registers.
+  __device__ __forceinline__ void block(int lo, int hi, bool mask, bool fresh, float& m, float& l) {
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    uint32_t r[2][32];
+    tmem_ld32_issue(r[0], tmem + col_s(st));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(r[124 + k]));
+    for (int q = 0; q < 4; ++q) {
+      tmem_landed();
+      tmem_tie(r[q & 1]);
+      if (q < 3) tmem_ld32_issue(r[(q + 1) & 1], tmem + col_s(st) + (q + 1) * 32);
+      if (mask) hide(r[q & 1], q, lo, hi);
+      top_of(r[q & 1], mx);
+    }
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     if (fresh) {
       m = top;
@@ -566,17 +584,17 @@ struct Softmax {
         const float f = need ? exp2_approx((m - top) * a.c) : 1.f;  // m = -inf: 0
         const uint64_t f2 = pack2(f, f);
 #pragma unroll
-        for (int q = 0; q < DP / 32; ++q) {
-          uint32_t o[32];
-          tmem_ld32(o, tmem + col_o<DP>(st) + q * 32);
+        for (int q = 0; q < DP / 16; ++q) {
+          uint32_t o[16];
+          tmem_ld16(o, tmem + col_o<DP>(st) + q * 16);
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
+          for (int i = 0; i < 16; i += 2) {
             float x, y;
             unpack2(mul2(pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), f2), x, y);
             o[i] = __float_as_uint(x);
             o[i + 1] = __float_as_uint(y);
           }
-          tmem_st32(tmem + col_o<DP>(st) + q * 32, o);
+          tmem_st16(tmem + col_o<DP>(st) + q * 16, o);
         }
         l *= f;
         if (need) m = top;
@@ -585,20 +603,26 @@ struct Softmax {
     const float ref = m == -INFINITY ? 0.f : -m * a.c;
     const uint64_t c2 = pack2(a.c, a.c), ref2 = pack2(ref, ref);
     uint64_t sum[4] = {0, 0, 0, 0};
+    tmem_ld32_issue(r[0], tmem + col_s(st));
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      uint32_t p[32];
+    for (int q = 0; q < 4; ++q) {
+      tmem_landed();
+      tmem_tie(r[q & 1]);
+      if (q < 3) tmem_ld32_issue(r[(q + 1) & 1], tmem + col_s(st) + (q + 1) * 32);
+      if (mask) hide(r[q & 1], q, lo, hi);
+      uint32_t p[16];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int at = q * 64 + 2 * i;
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t(&s)[32] = r[q & 1];
         float x, y;
-        unpack2(fma2(pack2(__uint_as_float(r[at]), __uint_as_float(r[at + 1])), c2, ref2), x, y);
+        unpack2(fma2(pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, ref2), x, y);
         x = exp2_approx(x);
         y = exp2_approx(y);
         sum[i & 3] = add2(sum[i & 3], pack2(x, y));
         p[i] = pack16<T>(x, y);
       }
-      tmem_st32(tmem + col_s(st) + q * 32, p);
+      // Columns 16 q .. 16 q + 15 of the scores, which have been read (32 q and on are still to be).
+      tmem_st16(tmem + col_s(st) + q * 16, p);
     }
     float x, y;
     unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), x, y);
@@ -766,7 +790,7 @@ struct Softmax {
         if (active) {
           tc_fence_after();
           const bool mask = k0 + kKeys > p0 + 1 || (a.window > 0 && p1 - k0 >= a.window);
-          const int hi = pos + 1 - k0, lo = a.window > 0 && pos - k0 >= a.window ? pos - k0 - a.window + 1 : 0;
+          const int hi = max(pos + 1 - k0, 0), lo = a.window > 0 && pos - k0 >= a.window ? pos - k0 - a.window + 1 : 0;
           block(lo, hi, mask, i == 0, m, l);
           tc_wait_st();
           tc_fence_before();
@@ -818,8 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_attend(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k,
              const __grid_constant__ CUtensorMap map_v) {
   using L = Layout<DP>;
-  extern __shared__ char raw[];
-  char* smem = raw + (((smem_u32(raw) + 1023) & ~1023u) - smem_u32(raw));
+  extern __shared__ __align__(1024) char smem[];
   Control* c = reinterpret_cast<Control*>(smem + L::kCtl);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
