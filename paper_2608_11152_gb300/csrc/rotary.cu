@@ -105,21 +105,103 @@ struct alignas(VEC * sizeof(T)) Vec {
   T e[VEC];
 };
 
+// One item of a CTA: a unit of a head of a token.
+struct Item {
+  uint32_t tok, head, unit;  // token of the CTA; head of all heads (queries, keys, values); unit of the head
+};
+__device__ __forceinline__ Item item_of(const RotArgs& a, uint32_t i, int h0) {
+  const uint32_t t = a.per_tok.div(i), r = i - t * a.per_tok.d, h = a.units.div(r);
+  return {t, h0 + h, r - h * a.units.d};
+}
+
 template <class T, int VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ RotArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) k_rotate(const __grid_constant__ RotArgs a) {
   extern __shared__ float2 s_turn[];  // [tok_per_cta][rot / 2]
   __shared__ int32_t s_pos[kMaxTok];
   __shared__ int64_t s_slot[kMaxTok];  // element offset of the token's row of kv head 0, -1: skip
   using V = Vec<T, VEC>;
-  constexpr int W = (HALF || VEC > 1) ? VEC : 2;  // elements of a vector; an interleaved scalar unit is a pair
+  constexpr int W = (HALF || VEC > 1) ? VEC : 2;  // elements of a unit's vector (a scalar interleaved unit: a pair)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t0 = blockIdx.x * a.tok_per_cta;
   const int nt = min(a.tok_per_cta, a.n_tokens - t0);
   const int heads = a.hq + 2 * a.hkv;
   const int h0 = blockIdx.y * a.heads_per_cta + (a.x.p ? 0 : a.hq);
   const int nh = min(a.heads_per_cta, heads - h0);
-  const int half = a.rot / 2;
+  const int half = a.rot / 2, paired = HALF ? half / W : 0;  // paired: units of two vectors
+  const int n_items = nt * nh * (int)a.units.d;
+  // First element of the unit's vector, and of its second one (-1: none).
+  auto element = [&](uint32_t u) { return HALF ? ((int)u < paired ? u * W : (u + paired) * W) : u * W; };
+  auto second = [&](uint32_t u) -> int {
+    if constexpr (HALF) return (int)u < paired ? u * W + half : -1;
+    else if constexpr (VEC > 1) return -1;
+    else return (int)(u * 2 + 1) < a.d ? u * 2 + 1 : -1;
+  };
+  auto fetch = [&](uint32_t i, V& lo, V& hi) {
+    const Item it = item_of(a, i, h0);
+    int h = it.head;
+    const Heads& src = h < a.hq ? a.x : h < a.hq + a.hkv ? a.k : a.v;
+    if (h >= a.hq) h -= h < a.hq + a.hkv ? a.hq : a.hq + a.hkv;
+    const T* s = static_cast<const T*>(src.p) + (int64_t)(t0 + it.tok) * src.ts + (int64_t)h * src.hs;
+    lo = *reinterpret_cast<const V*>(s + element(it.unit));
+    const int e2 = second(it.unit);
+    if (e2 >= 0) hi = *reinterpret_cast<const V*>(s + e2);
+  };
+  auto put = [&](uint32_t i, V& lo, V& hi) {
+    const Item it = item_of(a, i, h0);
+    int h = it.head;
+    const int64_t slot = s_slot[it.tok];
+    if (slot < 0) return;
+    const bool turns = h < a.hq + a.hkv;
+    T* o;
+    if (h < a.hq) {
+      o = static_cast<T*>(a.out.p) + (int64_t)(t0 + it.tok) * a.out.ts + (int64_t)h * a.out.hs;
+    } else {
+      h -= turns ? a.hq : a.hq + a.hkv;
+      o = static_cast<T*>(turns ? a.kb : a.vb) + slot + (int64_t)h * kBlockTokens * a.d;
+    }
+    const int el = element(it.unit), e2 = second(it.unit);
+    const float2* tr = s_turn + it.tok * half;
+    if constexpr (HALF) {
+      if (turns && e2 >= 0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float2 cs = tr[el + e];
+          const float x = to_f(lo.e[e]), y = to_f(hi.e[e]);
+          lo.e[e] = from_f<T>(x * cs.x - y * cs.y);
+          hi.e[e] = from_f<T>(x * cs.y + y * cs.x);
+        }
+      }
+    } else if constexpr (VEC > 1) {
+      if (turns) {
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+          if (el + e < a.rot) {
+            const float2 cs = tr[(el + e) / 2];
+            const float x = to_f(lo.e[e]), y = to_f(lo.e[e + 1]);
+            lo.e[e] = from_f<T>(x * cs.x - y * cs.y);
+            lo.e[e + 1] = from_f<T>(x * cs.y + y * cs.x);
+          }
+        }
+      }
+    } else {
+      if (turns && el < a.rot) {
+        const float2 cs = tr[el / 2];
+        const float x = to_f(lo.e[0]), y = to_f(hi.e[0]);
+        lo.e[0] = from_f<T>(x * cs.x - y * cs.y);
+        hi.e[0] = from_f<T>(x * cs.y + y * cs.x);
+      }
+    }
+    *reinterpret_cast<V*>(o + el) = lo;
+    if (e2 >= 0) *reinterpret_cast<V*>(o + e2) = hi;
+  };
+
   chain_wait();
+  // The first items are on their way before the positions are looked up: a CTA has one round of items
+  // as a rule, and its time is two memory latencies, not three.
+  V lo[kInFlight], hi[kInFlight];
+#pragma unroll
+  for (int j = 0; j < kInFlight; ++j)
+    if (tid + j * kThreads < n_items) fetch(tid + j * kThreads, lo[j], hi[j]);
   if (a.hkv == 0) {
     if (tid < nt) {
       s_pos[tid] = __ldcg(a.positions + t0 + tid);
@@ -144,99 +226,22 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const __grid_constant__ Rot
       s_slot[warp] = slot;
     }
   }
-  // The angles wait for the positions; the first items' loads do not, but sharing the wait
-  // keeps one code path and costs one latency per CTA, which other CTAs cover.
   __syncthreads();
   for (int i = tid; i < nt * half; i += kThreads) {
     const int t = i / half, p = i - t * half;
     s_turn[i] = turn(s_pos[t], __ldg(a.freq + p), a.attn, a.backward);
   }
   __syncthreads();
-
-  const int paired = HALF ? half / W : 0;  // units that hold two vectors
-  const int n_items = nt * nh * (int)a.units.d;
-  for (int base = tid; base < n_items; base += kThreads * kInFlight) {
-    V lo[kInFlight], hi[kInFlight];
-    T* dst[kInFlight];
-    int tok[kInFlight], el[kInFlight];  // token of the CTA, first element; el < 0: nothing to do
-    bool turns[kInFlight];
 #pragma unroll
-    for (int j = 0; j < kInFlight; ++j) {
-      const uint32_t i = base + j * kThreads;
-      el[j] = -1;
-      if (i >= (uint32_t)n_items) continue;
-      const uint32_t t = a.per_tok.div(i), r = i - t * a.per_tok.d;
-      const uint32_t hl = a.units.div(r), u = r - hl * a.units.d;
-      int h = h0 + hl;
-      const int64_t slot = s_slot[t];
-      if (slot < 0) continue;
-      const Heads& src = h < a.hq ? a.x : h < a.hq + a.hkv ? a.k : a.v;
-      if (h < a.hq) {
-        dst[j] = static_cast<T*>(a.out.p) + (int64_t)(t0 + t) * a.out.ts + (int64_t)h * a.out.hs;
-        turns[j] = true;
-      } else {
-        turns[j] = h < a.hq + a.hkv;
-        h -= a.hq + (turns[j] ? 0 : a.hkv);
-        dst[j] = static_cast<T*>(turns[j] ? a.kb : a.vb) + slot + (int64_t)h * kBlockTokens * a.d;
-      }
-      const T* s = static_cast<const T*>(src.p) + (int64_t)(t0 + t) * src.ts + (int64_t)h * src.hs;
-      tok[j] = t;
-      if constexpr (HALF) {
-        const bool two = (int)u < paired;
-        el[j] = two ? u * W : (u + paired) * W;
-        lo[j] = *reinterpret_cast<const V*>(s + el[j]);
-        if (two) hi[j] = *reinterpret_cast<const V*>(s + el[j] + half);
-      } else if constexpr (VEC > 1) {
-        el[j] = u * W;
-        lo[j] = *reinterpret_cast<const V*>(s + el[j]);
-      } else {
-        el[j] = u * W;
-        lo[j] = *reinterpret_cast<const V*>(s + el[j]);
-        if (el[j] + 1 < a.d) hi[j] = *reinterpret_cast<const V*>(s + el[j] + 1);
-      }
-    }
+  for (int j = 0; j < kInFlight; ++j)
+    if (tid + j * kThreads < n_items) put(tid + j * kThreads, lo[j], hi[j]);
+  for (int base = tid + kInFlight * kThreads; base < n_items; base += kThreads * kInFlight) {
 #pragma unroll
-    for (int j = 0; j < kInFlight; ++j) {
-      if (el[j] < 0) continue;
-      const float2* tr = s_turn + tok[j] * half;
-      T* o = dst[j];
-      if constexpr (HALF) {
-        const bool two = el[j] < half;
-        if (two && turns[j]) {
+    for (int j = 0; j < kInFlight; ++j)
+      if (base + j * kThreads < n_items) fetch(base + j * kThreads, lo[j], hi[j]);
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float2 cs = tr[el[j] + e];
-            const float x = to_f(lo[j].e[e]), y = to_f(hi[j].e[e]);
-            lo[j].e[e] = from_f<T>(x * cs.x - y * cs.y);
-            hi[j].e[e] = from_f<T>(x * cs.y + y * cs.x);
-          }
-        }
-        *reinterpret_cast<V*>(o + el[j]) = lo[j];
-        if (two) *reinterpret_cast<V*>(o + el[j] + half) = hi[j];
-      } else if constexpr (VEC > 1) {
-        if (turns[j]) {
-#pragma unroll
-          for (int e = 0; e < VEC; e += 2) {
-            if (el[j] + e < a.rot) {
-              const float2 cs = tr[(el[j] + e) / 2];
-              const float x = to_f(lo[j].e[e]), y = to_f(lo[j].e[e + 1]);
-              lo[j].e[e] = from_f<T>(x * cs.x - y * cs.y);
-              lo[j].e[e + 1] = from_f<T>(x * cs.y + y * cs.x);
-            }
-          }
-        }
-        *reinterpret_cast<V*>(o + el[j]) = lo[j];
-      } else {
-        if (turns[j] && el[j] < a.rot) {
-          const float2 cs = tr[el[j] / 2];
-          const float x = to_f(lo[j].e[0]), y = to_f(hi[j].e[0]);
-          lo[j].e[0] = from_f<T>(x * cs.x - y * cs.y);
-          hi[j].e[0] = from_f<T>(x * cs.y + y * cs.x);
-        }
-        *reinterpret_cast<V*>(o + el[j]) = lo[j];
-        if (el[j] + 1 < a.d) *reinterpret_cast<V*>(o + el[j] + 1) = hi[j];
-      }
-    }
+    for (int j = 0; j < kInFlight; ++j)
+      if (base + j * kThreads < n_items) put(base + j * kThreads, lo[j], hi[j]);
   }
 }
 
