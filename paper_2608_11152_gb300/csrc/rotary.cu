@@ -1,11 +1,12 @@
 // Rotary positions, and the append of new tokens to a paged cache with the rotation on the way.
 //
 // Both are one pass over their data: a CTA takes a few tokens, finds each token's position (and,
-// for the append, its slot), computes the cosines and sines of the tokens' pairs once into shared
-// memory, and then moves heads: an item is one unit of one head of one token, a unit is the piece
-// of a head that a thread holds -- in the half layout two vectors rot/2 apart (or one vector past
-// the rotated part), in the interleaved layout one vector of whole pairs.  All heads of a token
-// share its angles, so the trigonometry is 1/heads of an item.
+// for the append, its slot) and computes the cosines and sines of the tokens' pairs once, into
+// shared memory.  A thread has one unit of a head -- in the half layout two vectors rot/2 apart (or
+// one vector past the rotated part), in the interleaved layout one vector of whole pairs -- of one
+// token, takes the unit's cosines and sines to registers, and goes through heads of the token with
+// them: all heads share the angles, so the trigonometry and the reads of shared memory are a
+// fraction of an item, and the next head is one addition away.
 #include <cmath>
 #include <new>
 
@@ -17,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTok = 8;    // tokens of a CTA, a warp each
-constexpr int kInFlight = 4;  // items a thread loads before it stores the first
+constexpr int kHeads = 4;     // heads of a token that a thread goes through, at least, where there are many tokens
 
 // n / d for n * d < 2^32: m = ceil(2^32 / d) (d = 1 would need 33 bits and is the identity).
 struct FastDiv {
@@ -32,7 +33,8 @@ struct FastDiv {
 struct RotArgs {
   int32_t n_tokens, hq, hkv, d, rot;  // hkv = 0: plain rotation of hq heads
   int32_t tok_per_cta, heads_per_cta, backward;
-  FastDiv units, per_tok;  // units of a head, units of heads_per_cta heads
+  int32_t units;                 // of a head
+  FastDiv unit_threads, groups;  // threads of a head's units, heads of a token side by side
   const uint64_t* freq;
   float attn;
   Heads x, out, k, v;  // x: queries
@@ -105,90 +107,60 @@ struct alignas(VEC * sizeof(T)) Vec {
   T e[VEC];
 };
 
-// One item of a CTA: a unit of a head of a token.
-struct Item {
-  uint32_t tok, head, unit;  // token of the CTA; head of all heads (queries, keys, values); unit of the head
-};
-__device__ __forceinline__ Item item_of(const RotArgs& a, uint32_t i, int h0) {
-  const uint32_t t = a.per_tok.div(i), r = i - t * a.per_tok.d, h = a.units.div(r);
-  return {t, h0 + h, r - h * a.units.d};
-}
-
 template <class T, int VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads, 3) k_rotate(const __grid_constant__ RotArgs a) {
+__global__ void __launch_bounds__(kThreads, HALF ? 5 : 7) k_rotate(const __grid_constant__ RotArgs a) {
   extern __shared__ float2 s_turn[];  // [tok_per_cta][rot / 2]
   __shared__ int32_t s_pos[kMaxTok];
   __shared__ int64_t s_slot[kMaxTok];  // element offset of the token's row of kv head 0, -1: skip
   using V = Vec<T, VEC>;
-  constexpr int W = (HALF || VEC > 1) ? VEC : 2;  // elements of a unit's vector (a scalar interleaved unit: a pair)
+  constexpr bool PAIR = !HALF && VEC == 1;        // a unit is two neighbouring elements, moved one by one
+  constexpr int W = PAIR ? 2 : VEC;               // elements a unit steps over
+  constexpr int N = HALF ? VEC : PAIR ? 1 : VEC / 2;  // pairs of a unit
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t0 = blockIdx.x * a.tok_per_cta;
   const int nt = min(a.tok_per_cta, a.n_tokens - t0);
-  const int heads = a.hq + 2 * a.hkv;
   const int h0 = blockIdx.y * a.heads_per_cta + (a.x.p ? 0 : a.hq);
-  const int nh = min(a.heads_per_cta, heads - h0);
+  const int h1 = min(h0 + a.heads_per_cta, a.hq + 2 * a.hkv);
   const int half = a.rot / 2, paired = HALF ? half / W : 0;  // paired: units of two vectors
-  const int n_items = nt * nh * (int)a.units.d;
-  // First element of the unit's vector, and of its second one (-1: none).
-  auto element = [&](uint32_t u) { return HALF ? ((int)u < paired ? u * W : (u + paired) * W) : u * W; };
-  auto second = [&](uint32_t u) -> int {
-    if constexpr (HALF) return (int)u < paired ? u * W + half : -1;
-    else if constexpr (VEC > 1) return -1;
-    else return (int)(u * 2 + 1) < a.d ? u * 2 + 1 : -1;
+  const int slot = a.unit_threads.div(tid), tok = a.groups.div(slot), group = slot - tok * a.groups.d;
+  const int u0 = tid - slot * a.unit_threads.d;
+  const bool active = tok < nt;
+
+  // First element of a unit, and of its second vector (-1: it has none).
+  auto first = [&](int u) { return HALF && u >= paired ? (u + paired) * W : u * W; };
+  auto second = [&](int u) {
+    return HALF ? (u < paired ? u * W + half : -1) : PAIR && u * 2 + 1 < a.d ? u * 2 + 1 : -1;
   };
-  auto fetch = [&](uint32_t i, V& lo, V& hi) {
-    const Item it = item_of(a, i, h0);
-    int h = it.head;
-    const Heads& src = h < a.hq ? a.x : h < a.hq + a.hkv ? a.k : a.v;
-    if (h >= a.hq) h -= h < a.hq + a.hkv ? a.hq : a.hq + a.hkv;
-    const T* s = static_cast<const T*>(src.p) + (int64_t)(t0 + it.tok) * src.ts + (int64_t)h * src.hs;
-    lo = *reinterpret_cast<const V*>(s + element(it.unit));
-    const int e2 = second(it.unit);
+  auto fetch = [&](int h, int u, V& lo, V& hi) {
+    const bool q = h < a.hq, k = h < a.hq + a.hkv;
+    const Heads& src = q ? a.x : k ? a.k : a.v;
+    const int hh = q ? h : k ? h - a.hq : h - a.hq - a.hkv;
+    const T* s = static_cast<const T*>(src.p) + (int64_t)(t0 + tok) * src.ts + (int64_t)hh * src.hs;
+    lo = *reinterpret_cast<const V*>(s + first(u));
+    const int e2 = second(u);
     if (e2 >= 0) hi = *reinterpret_cast<const V*>(s + e2);
   };
-  auto put = [&](uint32_t i, V& lo, V& hi) {
-    const Item it = item_of(a, i, h0);
-    int h = it.head;
-    const int64_t slot = s_slot[it.tok];
-    if (slot < 0) return;
-    const bool turns = h < a.hq + a.hkv;
-    T* o;
-    if (h < a.hq) {
-      o = static_cast<T*>(a.out.p) + (int64_t)(t0 + it.tok) * a.out.ts + (int64_t)h * a.out.hs;
-    } else {
-      h -= turns ? a.hq : a.hq + a.hkv;
-      o = static_cast<T*>(turns ? a.kb : a.vb) + slot + (int64_t)h * kBlockTokens * a.d;
-    }
-    const int el = element(it.unit), e2 = second(it.unit);
-    const float2* tr = s_turn + it.tok * half;
-    if constexpr (HALF) {
-      if (turns && e2 >= 0) {
+  auto put = [&](int h, int u, const float2 (&cs)[N], V& lo, V& hi) {
+    const bool q = h < a.hq, k = h < a.hq + a.hkv;
+    T* o = q ? static_cast<T*>(a.out.p) + (int64_t)(t0 + tok) * a.out.ts + (int64_t)h * a.out.hs
+             : static_cast<T*>(k ? a.kb : a.vb) + s_slot[tok] +
+                   (int64_t)(h - a.hq - (k ? 0 : a.hkv)) * kBlockTokens * a.d;
+    const int el = first(u), e2 = second(u);
+    if (k && el < a.rot) {
+      if constexpr (HALF || PAIR) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float2 cs = tr[el + e];
+        for (int e = 0; e < N; ++e) {
           const float x = to_f(lo.e[e]), y = to_f(hi.e[e]);
-          lo.e[e] = from_f<T>(x * cs.x - y * cs.y);
-          hi.e[e] = from_f<T>(x * cs.y + y * cs.x);
+          lo.e[e] = from_f<T>(x * cs[e].x - y * cs[e].y);
+          hi.e[e] = from_f<T>(x * cs[e].y + y * cs[e].x);
         }
-      }
-    } else if constexpr (VEC > 1) {
-      if (turns) {
+      } else {
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) {
-          if (el + e < a.rot) {
-            const float2 cs = tr[(el + e) / 2];
-            const float x = to_f(lo.e[e]), y = to_f(lo.e[e + 1]);
-            lo.e[e] = from_f<T>(x * cs.x - y * cs.y);
-            lo.e[e + 1] = from_f<T>(x * cs.y + y * cs.x);
-          }
+        for (int e = 0; e < N; ++e) {  // past the rotated part a pair meets cos 1 and sin 0
+          const float x = to_f(lo.e[2 * e]), y = to_f(lo.e[2 * e + 1]);
+          lo.e[2 * e] = from_f<T>(x * cs[e].x - y * cs[e].y);
+          lo.e[2 * e + 1] = from_f<T>(x * cs[e].y + y * cs[e].x);
         }
-      }
-    } else {
-      if (turns && el < a.rot) {
-        const float2 cs = tr[el / 2];
-        const float x = to_f(lo.e[0]), y = to_f(hi.e[0]);
-        lo.e[0] = from_f<T>(x * cs.x - y * cs.y);
-        hi.e[0] = from_f<T>(x * cs.y + y * cs.x);
       }
     }
     *reinterpret_cast<V*>(o + el) = lo;
@@ -196,12 +168,10 @@ __global__ void __launch_bounds__(kThreads, 3) k_rotate(const __grid_constant__ 
   };
 
   chain_wait();
-  // The first items are on their way before the positions are looked up: a CTA has one round of items
-  // as a rule, and its time is two memory latencies, not three.
-  V lo[kInFlight], hi[kInFlight];
-#pragma unroll
-  for (int j = 0; j < kInFlight; ++j)
-    if (tid + j * kThreads < n_items) fetch(tid + j * kThreads, lo[j], hi[j]);
+  // The first head is on its way before the positions are looked up.
+  V lo, hi;
+  const int begin = h0 + group;
+  if (active && begin < h1) fetch(begin, u0, lo, hi);
   if (a.hkv == 0) {
     if (tid < nt) {
       s_pos[tid] = __ldcg(a.positions + t0 + tid);
@@ -210,20 +180,19 @@ __global__ void __launch_bounds__(kThreads, 3) k_rotate(const __grid_constant__ 
   } else if (warp < nt) {
     const int t = t0 + warp;
     const int b = find_sequence(a.b.q_off, a.b.n, t, lane);
-    const int begin = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
+    const int from = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
     const int64_t pos = (int64_t)len - end + t;
-    const bool ok = begin <= t && t < end && end - begin <= a.b.max_q && len >= end - begin && pos >= 0 &&
+    const bool ok = from <= t && t < end && end - from <= a.b.max_q && len >= end - from && pos >= 0 &&
                     pos < a.b.stride * kBlockTokens;
-    int64_t slot = -1;
+    int64_t at = -1;
     if (ok) {
       const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
-      if (blk >= 0 && blk < a.n_blocks)
-        slot = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
+      if (blk >= 0 && blk < a.n_blocks) at = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
     }
     if (lane == 0) {
-      if (slot < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
+      if (at < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
       s_pos[warp] = (int32_t)pos;
-      s_slot[warp] = slot;
+      s_slot[warp] = at;
     }
   }
   __syncthreads();
@@ -232,16 +201,18 @@ __global__ void __launch_bounds__(kThreads, 3) k_rotate(const __grid_constant__ 
     s_turn[i] = turn(s_pos[t], __ldg(a.freq + p), a.attn, a.backward);
   }
   __syncthreads();
+  if (!active || s_slot[tok] < 0) return;
+  bool loaded = true;
+  for (int u = u0; u < a.units; u += a.unit_threads.d) {
+    float2 cs[N];
+    const int pair = HALF ? first(u) : first(u) / 2;
 #pragma unroll
-  for (int j = 0; j < kInFlight; ++j)
-    if (tid + j * kThreads < n_items) put(tid + j * kThreads, lo[j], hi[j]);
-  for (int base = tid + kInFlight * kThreads; base < n_items; base += kThreads * kInFlight) {
-#pragma unroll
-    for (int j = 0; j < kInFlight; ++j)
-      if (base + j * kThreads < n_items) fetch(base + j * kThreads, lo[j], hi[j]);
-#pragma unroll
-    for (int j = 0; j < kInFlight; ++j)
-      if (base + j * kThreads < n_items) put(base + j * kThreads, lo[j], hi[j]);
+    for (int e = 0; e < N; ++e) cs[e] = pair + e < half ? s_turn[tok * half + pair + e] : make_float2(1.f, 0.f);
+    for (int h = begin; h < h1; h += a.groups.d) {
+      if (!loaded) fetch(h, u, lo, hi);
+      loaded = false;
+      put(h, u, cs, lo, hi);
+    }
   }
 }
 
@@ -259,19 +230,23 @@ void launch_rotate_t(RotArgs& a, int layout, int num_sms, cudaStream_t st) {
   else
     units = half_layout ? a.d - a.rot / 2 : (a.d + 1) / 2;
   const int heads = (a.x.p ? a.hq : 0) + 2 * a.hkv;
-  // A CTA's items: one per thread while all CTAs of that size fit the GPU at once (a step of a few
-  // sequences is latency: more CTAs, each with one round of loads), else kInFlight per thread.
-  const int64_t per_tok = (int64_t)heads * units;
-  const int target = (int64_t)a.n_tokens * per_tok <= (int64_t)num_sms * 8 * kThreads ? kThreads : kThreads * kInFlight;
-  int tok = 1, hpc = heads;
-  if (per_tok >= target)
-    hpc = target / units < 1 ? 1 : target / units;
-  else
-    tok = (int)(target / per_tok) < kMaxTok ? (int)(target / per_tok) : kMaxTok;
+  // The CTA's threads beyond one head's units take other heads of the token (`groups` of them) and other
+  // tokens.  One head per thread while all CTAs of that shape fit the GPU at once: a step of a few
+  // sequences is latency.  Else kHeads heads or more per thread.
+  const int unit_threads = units < kThreads ? units : kThreads, slots = kThreads / unit_threads;
+  const bool few = (int64_t)a.n_tokens * heads * units <= (int64_t)num_sms * 8 * kThreads;
+  int groups = heads;
+  if (!few)
+    for (groups = 1; groups * 2 * kHeads <= heads;) groups *= 2;
+  if (groups > slots) groups = slots;
+  int tok = slots / groups;
+  if (tok > kMaxTok) tok = kMaxTok;
+  const int hpc = few ? groups : heads;
+  a.units = units;
   a.tok_per_cta = tok;
   a.heads_per_cta = hpc;
-  a.units.set(units);
-  a.per_tok.set(units * hpc);
+  a.unit_threads.set(unit_threads);
+  a.groups.set(groups);
   const dim3 grid((a.n_tokens + tok - 1) / tok, (heads + hpc - 1) / hpc);
   const size_t smem = sizeof(float2) * tok * (a.rot / 2);
   cudaLaunchAttribute at{};
