@@ -487,6 +487,11 @@ def test_refused_arguments():
             call()
     with pytest.raises(m.MisatError):
         pool.attend(batch, q, window=-1)
+    other = m.KvPool(*blocks(h=1), n_q_heads=4)  # a batch made for other heads
+    with pytest.raises(ValueError):
+        other.attend(batch, q)
+    with pytest.raises(ValueError):
+        other.append(batch, k, k)
     small = s.pool(4, max_batch=1)
     with pytest.raises(m.MisatError):
         small.attend(s.batch(small), q)
