@@ -100,6 +100,7 @@ struct Segment {
 // The run of blocks of one CTA, item by item.
 struct Walk {
   int b, h, tile, off;
+  int pad;  // what an item counts, where items are not split (0: its blocks)
   int64_t left, at;
   Seq s;
   __device__ __forceinline__ bool next(const AttendArgs& a, Segment& g) {
@@ -111,10 +112,10 @@ struct Walk {
     g.nt = min(2 * a.tok, s.n - g.t0);
     g.pair = g.nt > a.tok;
     g.k = span_of(a, s, g.t0, g.nt);
-    const int cost = max(g.k.blocks, 1);
+    const int cost = pad ? pad : max(g.k.blocks, 1);
     const int take = (int)min(left, (int64_t)(cost - off));
     g.j0 = g.k.jb + off;
-    g.nb = g.k.blocks ? take : 0;
+    g.nb = pad || g.k.blocks == 0 ? g.k.blocks : take;
     g.whole = take == cost;
     g.first = at - off;
     g.last = g.first + cost;
@@ -158,8 +159,9 @@ struct Control {
   uint64_t ml_full, ml_free, wg[2], drain;
   float2 ml[kTile];  // m and l of stream 1 for the join
   int64_t sum[kThreads / 32];
-  int64_t total, per;
-  int b, h, tile, off;
+  int items[kThreads / 32], longest[kThreads / 32];
+  Walk start;
+  int64_t per;  // length of a run
   int last[2];
   int abort;
   uint32_t tmem;
@@ -182,30 +184,79 @@ struct Ring {
 };
 
 // ---- the run of each CTA ----
-// Total of all items' blocks and the place where this CTA's run begins; every thread takes part.
+__device__ __forceinline__ int64_t div_up(int64_t x, uint32_t d) {  // a 64-bit division takes hundreds of cycles
+  return (x >> 31) == 0 ? ((uint32_t)x + d - 1) / d : (x + d - 1) / d;
+}
+__device__ __forceinline__ int64_t div_down(int64_t x, int64_t d) {
+  return (x >> 32) == 0 && (d >> 32) == 0 ? (uint32_t)x / (uint32_t)d : x / d;
+}
+
+// Where this CTA's run begins and how long it is; every thread takes part.
+//
+// With at most one item per CTA, an item is split only where that saves more than kSplit blocks of the
+// longest one: writing, announcing and joining the parts takes about as long as kSplit blocks
+// (4 sequences of 17 to 640 tokens, 8 kv heads: 12.6 us split evenly, 8.9 us whole).  Whole items then count
+// as equally long (`pad`).  A part has two blocks at least: the streams take them at the same time.
+constexpr int kSplit = 8;
 __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Walk& w) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  auto seq_cost = [&](int b) -> int64_t {
-    if (b >= a.b.n) return 0;
-    const Seq s = load_seq(a, b);
-    int64_t sum = 0;
-    for (int t = 0, k = n_items(a, s); t < k; ++t) sum += item_cost(a, s, t);
-    return sum * a.hkv;
+  constexpr int kWarps = kThreads / 32;
+  struct Cost {
+    int64_t blocks;
+    int items, longest;
   };
-  const int64_t first = seq_cost(tid);
-  int64_t sum = first;
-  for (int b = tid + kThreads; b < a.b.n; b += kThreads) sum += seq_cost(b);
+  auto cost_of = [&](const Seq& s) -> Cost {
+    Cost r{0, n_items(a, s), 0};
+    for (int t = 0; t < r.items; ++t) {
+      const int k = item_cost(a, s, t);
+      r.blocks += k;
+      r.longest = max(r.longest, k);
+    }
+    return r;
+  };
+  const Seq mine = tid < a.b.n ? load_seq(a, tid) : Seq{0, 0, 0};
+  const Cost first = cost_of(mine);
+  Cost sum = first;
+  for (int b = tid + kThreads; b < a.b.n; b += kThreads) {
+    const Cost r = cost_of(load_seq(a, b));
+    sum.blocks += r.blocks;
+    sum.items += r.items;
+    sum.longest = max(sum.longest, r.longest);
+  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) c->sum[warp] = sum;
+  for (int o = 16; o > 0; o >>= 1) sum.blocks += __shfl_xor_sync(0xffffffffu, sum.blocks, o);
+  sum.items = __reduce_add_sync(0xffffffffu, sum.items);
+  sum.longest = __reduce_max_sync(0xffffffffu, sum.longest);
+  if (lane == 0) {
+    c->sum[warp] = sum.blocks;
+    c->items[warp] = sum.items;
+    c->longest[warp] = sum.longest;
+  }
   __syncthreads();
-  int64_t total = 0;
-  for (int i = 0; i < kThreads / 32; ++i) total += c->sum[i];
-  const int64_t per = (total + gridDim.x - 1) / gridDim.x, lo = per * blockIdx.x;
+  int64_t total = 0, items = 0;
+  int longest = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    total += c->sum[i];
+    items += c->items[i];
+    longest = max(longest, c->longest[i]);
+  }
+  total *= a.hkv;
+  items *= a.hkv;
+  int64_t per = div_up(total, gridDim.x);
+  const bool whole = items <= gridDim.x && longest <= per + kSplit;
+  if (whole) {
+    per = longest;
+    total = items * longest;
+  } else if (per < 2) {
+    per = 2;
+  }
+  const int64_t lo = per * blockIdx.x;
   if (lo >= total) return false;
   int64_t base = 0;
   for (int b0 = 0; base <= lo; b0 += kThreads) {
-    const int64_t v = b0 == 0 ? first : seq_cost(b0 + tid);
+    const Seq s = b0 == 0 ? mine : b0 + tid < a.b.n ? load_seq(a, b0 + tid) : Seq{0, 0, 0};
+    const int64_t v = (whole ? (int64_t)n_items(a, s) * longest : b0 == 0 ? first.blocks : cost_of(s).blocks) * a.hkv;
     int64_t inc = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -216,33 +267,35 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Walk& 
     if (lane == 31) c->sum[warp] = inc;
     __syncthreads();
     int64_t before = base;
-    for (int i = 0; i < kThreads / 32; ++i) {
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
       if (i < warp) before += c->sum[i];
       base += c->sum[i];
     }
     before += inc - v;
     if (before <= lo && lo < before + v) {
-      const Seq s = load_seq(a, b0 + tid);
-      const int64_t head = v / a.hkv;
-      int64_t rest = lo - before;
-      c->b = b0 + tid;
-      c->h = (int)(rest / head);
-      rest -= c->h * head;
+      const int64_t head = div_down(v, a.hkv), h = div_down(lo - before, head);
+      int64_t rest = lo - before - h * head;
       int t = 0;
-      for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
-      c->tile = t;
-      c->off = (int)rest;
+      if (whole) {
+        t = (int)div_down(rest, longest);
+        rest = 0;
+      } else {
+        for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
+      }
+      c->start.b = b0 + tid;
+      c->start.h = (int)h;
+      c->start.tile = t;
+      c->start.off = (int)rest;
+      c->start.pad = whole ? longest : 0;
+      c->start.left = min(per, total - lo);
+      c->start.at = lo;
+      c->start.s = s;
       c->per = per;
     }
   }
   __syncthreads();
-  w.b = c->b;
-  w.h = c->h;
-  w.tile = c->tile;
-  w.off = c->off;
-  w.at = lo;
-  w.left = min(per, total - lo);
-  w.s = load_seq(a, w.b);
+  w = c->start;
   return true;
 }
 
@@ -583,7 +636,7 @@ struct Softmax {
       if (__any_sync(0xffffffffu, need)) {
         const float f = need ? exp2_approx((m - top) * a.c) : 1.f;  // m = -inf: 0
         const uint64_t f2 = pack2(f, f);
-#pragma unroll
+#pragma unroll 2
         for (int q = 0; q < DP / 16; ++q) {
           uint32_t o[16];
           tmem_ld16(o, tmem + col_o<DP>(st) + q * 16);
@@ -679,7 +732,7 @@ struct Softmax {
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
     T* out = mine ? out_row(g, t0, row) : nullptr;
     if (warp_rows > 0) {
-#pragma unroll
+#pragma unroll 1
       for (int q = 0; q < DP / 32; ++q) {
         uint32_t o[32], o1[32];
         __syncwarp();
@@ -714,7 +767,7 @@ struct Softmax {
   // The item is split between CTAs c0..c1: the last of them to arrive adds the parts.
   __device__ __forceinline__ bool arrive(const Segment& g, int t0, int rows) {
     const int64_t per = c->per;
-    const int c0 = (int)(g.first / per), c1 = (int)((g.last - 1) / per);
+    const int c0 = (int)div_down(g.first, per), c1 = (int)div_down(g.last - 1, per);
     const int wt = threadIdx.x & 127;
     __threadfence();
     if (!wg_sync()) return false;
@@ -866,6 +919,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_async_shared();
   }
   if (warp == 9) tmem_alloc(smem_u32(&c->tmem), 512);
+  if (warp == 8 && elect_one()) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
