@@ -95,6 +95,11 @@ struct Segment {
   bool whole;          // the part is the item
   int64_t first, last; // the item's blocks in the order of all blocks
   __device__ __forceinline__ int stream_blocks(int st) const { return pair ? nb : (nb + 1 - st) / 2; }
+  // The products of a part in the order of issue: step x is stream x & 1's next block.  A stream's
+  // scores are formed two steps ahead of its product with the values, so the loops over the steps
+  // run from -2 to steps() - 1: values of step x, then scores of step x + 2.
+  __device__ __forceinline__ int steps() const { return pair ? 2 * nb : nb; }
+  __device__ __forceinline__ int block(int step) const { return j0 + (pair ? step / 2 : step); }
 };
 
 // The run of blocks of one CTA, item by item.
@@ -374,17 +379,13 @@ struct Loader {
 // Which of the two query tiles a stream of a segment uses: both streams of a pair their own, else
 // the one tile that was not used last, so that the next item's queries load early.
 struct QuerySlots {
-  uint32_t phase[2] = {0, 0};
+  uint32_t phases = 0;  // bit per tile (phases that are chosen at run time are bits: an array would be memory)
   int turn = 0;
   __device__ __forceinline__ int slot(const Segment& g, int st) const { return g.pair ? st : turn; }
+  __device__ __forceinline__ uint32_t phase(int slot) const { return phases >> slot & 1; }
   __device__ __forceinline__ void step(const Segment& g) {
-    if (g.pair) {
-      phase[0] ^= 1;
-      phase[1] ^= 1;
-    } else {
-      phase[turn] ^= 1;
-      turn ^= 1;
-    }
+    phases ^= g.pair ? 3 : 1 << turn;
+    turn ^= !g.pair;
   }
 };
 
@@ -399,7 +400,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, Walk w, char* 
     if (g.nb == 0) continue;
     for (int st = 0; st < (g.pair ? 2 : 1); ++st) {
       const int slot = qs.slot(g, st);
-      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase[slot] ^ 1, &c->abort)) return;
+      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort)) return;
       const int t0 = st * a.tok, rows = min(a.tok, g.nt - t0) * a.group;
       char* dst = smem + L::kQ + slot * L::kStage;
       const T* src = static_cast<const T*>(a.q.p) + (int64_t)(g.s.begin + g.t0 + t0) * a.q.ts +
@@ -455,7 +456,7 @@ struct Issuer {
   char* smem;
   uint32_t base, tmem;
   Ring ring;
-  uint32_t p_phase[2] = {0, 0};
+  uint32_t p_phases = 0;  // bit per stream
 
   // Stage of the next tile, once it has landed (-1: gave up).
   __device__ __forceinline__ int take() {
@@ -467,7 +468,7 @@ struct Issuer {
   __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
   static __device__ __forceinline__ bool lead() { return elect_one(); }
 
-  __device__ __forceinline__ void scores(int st, int slot, int stage, bool last_use) {
+  __device__ __forceinline__ void scores(int st, int slot, int stage) {
     const uint32_t q = desc_lo(base + L::kQ + slot * L::kStage, 16), k = desc_lo(base + L::kKv + stage * L::kStage, 16);
     const uint32_t d = tmem + col_s(st);
     if (!lead()) return;
@@ -477,89 +478,68 @@ struct Issuer {
       mma_ss(d, q + at, k + at, desc_hi(1024), mma_desc(kBf16, 128, kKeys, false), i > 0);
     }
     mma_commit(smem_u32(&c->s_full[st]));
-    if (last_use) release(stage);
   }
-  // O of the stream (+)= weights times the values of block j; rows of V that no row of the item may
-  // see (past the sequence's end they hold anything) are cleared first.
-  __device__ __forceinline__ bool product(const Segment& g, int st, int stage, int j, bool clear, bool fresh,
-                                          bool last_use, bool last) {
-    if (clear) {
-      const int lo = max(g.k.from - j * kKeys, 0), hi = min(g.k.to - j * kKeys, kKeys);
-      if (lo > 0 || hi < kKeys) {
-        char* v = smem + L::kKv + stage * L::kStage;
-        const int lane = threadIdx.x & 31, gone = lo + kKeys - hi;
-        for (int i = lane; i < gone * (DP / 8); i += 32) {
-          const int r = i / (DP / 8), ch = i % (DP / 8), row = r < lo ? r : hi + r - lo;
-          *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
-        }
-        fence_async_shared();
-        __syncwarp();
-      }
+  // Rows of V that no row of the item may see (past the sequence's end they hold anything): zeros.
+  __device__ __forceinline__ void clear(const Segment& g, int stage, int j) {
+    const int lo = max(g.k.from - j * kKeys, 0), hi = min(g.k.to - j * kKeys, kKeys);
+    if (lo == 0 && hi == kKeys) return;
+    char* v = smem + L::kKv + stage * L::kStage;
+    const int lane = threadIdx.x & 31, gone = lo + kKeys - hi;
+    for (int i = lane; i < gone * (DP / 8); i += 32) {
+      const int r = i / (DP / 8), ch = i % (DP / 8), row = r < lo ? r : hi + r - lo;
+      *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
     }
-    if (!mbar_wait(smem_u32(&c->p_full[st]), p_phase[st], &c->abort)) return false;
-    p_phase[st] ^= 1;
-    tc_fence_after();
+    fence_async_shared();
+    __syncwarp();
+  }
+  // O of the stream (+)= weights times values.
+  __device__ __forceinline__ void product(int st, int stage, bool fresh) {
     const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
     const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
-    if (!lead()) return true;
+    if (!lead()) return;
 #pragma unroll
     for (int i = 0; i < kKeys / 16; ++i)
       mma_ts(d, p + i * 8, v + i * 16 * 128 / 16, desc_hi(1024), mma_desc(kBf16, 128, DP, true), !fresh || i > 0);
-    if (last_use) release(stage);
-    if (last) mma_commit(smem_u32(&c->o_full[st]));
-    return true;
   }
   __device__ __forceinline__ void run(Walk w) {
     QuerySlots qs;
     Segment g;
     while (w.next(a, g)) {
-      const int n = g.nb;
+      const int n = g.steps();
       if (n == 0) continue;
-      const int q0 = qs.slot(g, 0), q1 = qs.slot(g, 1);
-      if (!mbar_wait(smem_u32(&c->q_full[q0]), qs.phase[q0], &c->abort)) return;
-      if (g.pair && !mbar_wait(smem_u32(&c->q_full[q1]), qs.phase[q1], &c->abort)) return;
+      for (int st = 0; st < (g.pair ? 2 : 1); ++st) {
+        const int slot = qs.slot(g, st);
+        if (!mbar_wait(smem_u32(&c->q_full[slot]), qs.phase(slot), &c->abort)) return;
+      }
       tc_fence_after();
-      int k = take();
-      if (k < 0) return;
-      if (g.pair) {
-        scores(0, q0, k, false);
-        scores(1, q1, k, true);
-        if (n == 1 && lead()) {
-          mma_commit(smem_u32(&c->q_empty[q0]));
-          mma_commit(smem_u32(&c->q_empty[q1]));
-        }
-        for (int j = 0; j < n; ++j) {
-          const int v = take();
-          if (v < 0) return;
-          if (!product(g, 0, v, g.j0 + j, true, j == 0, false, j + 1 == n)) return;
-          if (j + 1 < n) {
-            if ((k = take()) < 0) return;
-            scores(0, q0, k, false);
+      int k = 0, v = 0;
+#pragma unroll 1
+      for (int x = -2; x < n; ++x) {
+        const int st = x & 1;
+        const bool first_use = !g.pair || st == 0, last_use = !g.pair || st == 1;
+        if (x >= 0) {
+          if (first_use) {
+            if ((v = take()) < 0) return;
+            clear(g, v, g.block(x));
           }
-          if (!product(g, 1, v, g.j0 + j, false, j == 0, true, j + 1 == n)) return;
-          if (j + 1 < n) {
-            scores(1, q1, k, true);
-            if (j + 2 == n && lead()) {
-              mma_commit(smem_u32(&c->q_empty[q0]));
-              mma_commit(smem_u32(&c->q_empty[q1]));
+          if (!mbar_wait(smem_u32(&c->p_full[st]), p_phases >> st & 1, &c->abort)) return;
+          p_phases ^= 1 << st;
+          tc_fence_after();
+          product(st, v, x < 2);
+          if (lead()) {
+            if (last_use) release(v);
+            if (x + 2 >= n) mma_commit(smem_u32(&c->o_full[st]));
+          }
+        }
+        if (x + 2 < n) {
+          if (first_use && (k = take()) < 0) return;
+          scores(st, qs.slot(g, st), k);
+          if (lead()) {
+            if (last_use) release(k);
+            if (x + 3 == n) {  // the last scores: the queries have been read
+              mma_commit(smem_u32(&c->q_empty[qs.slot(g, 0)]));
+              if (g.pair) mma_commit(smem_u32(&c->q_empty[1]));
             }
-          }
-        }
-      } else {
-        scores(0, q0, k, true);
-        if (n > 1) {
-          if ((k = take()) < 0) return;
-          scores(1, q0, k, true);
-        }
-        if (n <= 2 && lead()) mma_commit(smem_u32(&c->q_empty[q0]));
-        for (int j = 0; j < n; ++j) {
-          const int st = j & 1, v = take();
-          if (v < 0) return;
-          if (!product(g, st, v, g.j0 + j, true, j < 2, true, j + 2 >= n)) return;
-          if (j + 2 < n) {
-            if ((k = take()) < 0) return;
-            scores(st, q0, k, true);
-            if (j + 3 == n && lead()) mma_commit(smem_u32(&c->q_empty[q0]));
           }
         }
       }
@@ -598,14 +578,23 @@ struct Softmax {
   uint32_t tmem;  // with the warp's lanes
   int st;         // stream
   int row;        // row of the tile = lane of tensor memory
-  uint32_t s_phase = 0, o_phase[2] = {0, 0}, wg_phase = 0, ml_phase = 0;
+  uint32_t s_phase = 0, o_phase = 0, o1_phase = 0, wg_phase = 0, ml_phase = 0;  // o1: of stream 1, kept by stream 0
   bool joined = false;  // stream 1: its last item was joined by stream 0
 
-  // Scores 32 q .. 32 q + 31 of the row: the hidden ones to -infinity.
-  static __device__ __forceinline__ void hide(uint32_t (&r)[32], int q, int lo, int hi) {
+  // The scores outside [lo, hi) become -infinity, in tensor memory: few blocks need it, and the loops over
+  // the scores stay small (the kernel's code does not fit the instruction cache otherwise).
+  __device__ __forceinline__ void hide(int lo, int hi) {
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+      uint32_t r[32];
+      __syncwarp();
+      tmem_ld32(r, tmem + col_s(st) + q * 32);
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if ((uint32_t)(q * 32 + i - lo) >= (uint32_t)(hi - lo)) r[i] = 0xff800000u;
+      for (int i = 0; i < 32; ++i)
+        if ((uint32_t)(q * 32 + i - lo) >= (uint32_t)(hi - lo)) r[i] = 0xff800000u;
+      tmem_st32(tmem + col_s(st) + q * 32, r);
+    }
+    tc_wait_st();
   }
   static __device__ __forceinline__ void top_of(const uint32_t (&r)[32], float (&mx)[4]) {
 #pragma unroll
@@ -617,6 +606,7 @@ struct Softmax {
   // One block: scores to weights, with the running reference m and sum l.  The scores are read twice,
   // once for the maximum and once for the weights: 128 of them held meanwhile do not fit the registers.
   __device__ __forceinline__ void block(int lo, int hi, bool mask, bool fresh, float& m, float& l) {
+    if (mask) hide(lo, hi);
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     uint32_t r[2][32];
     tmem_ld32_issue(r[0], tmem + col_s(st));
@@ -625,7 +615,6 @@ struct Softmax {
       tmem_landed();
       tmem_tie(r[q & 1]);
       if (q < 3) tmem_ld32_issue(r[(q + 1) & 1], tmem + col_s(st) + (q + 1) * 32);
-      if (mask) hide(r[q & 1], q, lo, hi);
       top_of(r[q & 1], mx);
     }
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
@@ -636,9 +625,10 @@ struct Softmax {
       if (__any_sync(0xffffffffu, need)) {
         const float f = need ? exp2_approx((m - top) * a.c) : 1.f;  // m = -inf: 0
         const uint64_t f2 = pack2(f, f);
-#pragma unroll 2
+#pragma unroll 1
         for (int q = 0; q < DP / 16; ++q) {
           uint32_t o[16];
+          __syncwarp();
           tmem_ld16(o, tmem + col_o<DP>(st) + q * 16);
 #pragma unroll
           for (int i = 0; i < 16; i += 2) {
@@ -662,7 +652,6 @@ struct Softmax {
       tmem_landed();
       tmem_tie(r[q & 1]);
       if (q < 3) tmem_ld32_issue(r[(q + 1) & 1], tmem + col_s(st) + (q + 1) * 32);
-      if (mask) hide(r[q & 1], q, lo, hi);
       uint32_t p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -729,32 +718,36 @@ struct Softmax {
     const bool mine = row < rows;
     const int warp_rows = rows - (row & ~31);
     const int slot = g.whole ? 0 : (int)((blockIdx.x * 2 + (g.first >= c->per * blockIdx.x)) * 2 + st);
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    if (g.whole) {
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      w0 *= inv;
+      w1 *= inv;
+    }
     T* out = mine ? out_row(g, t0, row) : nullptr;
     if (warp_rows > 0) {
 #pragma unroll 1
-      for (int q = 0; q < DP / 32; ++q) {
-        uint32_t o[32], o1[32];
+      for (int q = 0; q < DP; q += 16) {
+        uint32_t o[16], o1[16];
         __syncwarp();
-        tmem_ld32(o, tmem + col_o<DP>(st) + q * 32);
-        if (join) tmem_ld32(o1, tmem + col_o<DP>(1) + q * 32);
+        tmem_ld16(o, tmem + col_o<DP>(st) + q);
+        if (join) tmem_ld16(o1, tmem + col_o<DP>(1) + q);
+        float x[2][8];
 #pragma unroll
-        for (int e = 0; e < 32 && mine; e += 8) {
-          float x[8];
+        for (int i = 0; i < 16; ++i) {
+          x[i / 8][i % 8] = __uint_as_float(o[i]) * w0;
+          if (join) x[i / 8][i % 8] += __uint_as_float(o1[i]) * w1;
+        }
+        if (!mine) continue;
+        if (g.whole) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[i] = __uint_as_float(o[e + i]);
-            if (join) x[i] = x[i] * w0 + __uint_as_float(o1[e + i]) * w1;
-          }
-          if (g.whole) {
+          for (int e = 0; e < 2; ++e)
+            if (q + e * 8 < a.d) put8(out + q + e * 8, x[e]);
+        } else {
+          float4* p = a.ws_o + ((int64_t)slot * (DP / 4) + q / 4) * kTile + row;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= inv;
-            if (q * 32 + e < a.d) put8(out + q * 32 + e, x);
-          } else {
-            float4* p = a.ws_o + ((int64_t)slot * (DP / 4) + (q * 32 + e) / 4) * kTile + row;
-            p[0] = make_float4(x[0], x[1], x[2], x[3]);
-            p[kTile] = make_float4(x[4], x[5], x[6], x[7]);
-          }
+          for (int e = 0; e < 4; ++e)
+            p[e * kTile] = make_float4(x[e / 2][e % 2 * 4], x[e / 2][e % 2 * 4 + 1], x[e / 2][e % 2 * 4 + 2],
+                                       x[e / 2][e % 2 * 4 + 3]);
         }
       }
     }
@@ -860,8 +853,8 @@ struct Softmax {
       }
       const bool join = !g.pair && g.nb > 1;
       if (nb > 0) {
-        if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase[st], &c->abort)) return;
-        o_phase[st] ^= 1;
+        if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase, &c->abort)) return;
+        o_phase ^= 1;
       }
       if (join && st == 1) {
         c->ml[row] = make_float2(m, l);
@@ -873,11 +866,11 @@ struct Softmax {
       }
       if (st == 1 && !g.pair) continue;
       if (join) {
-        if (!mbar_wait(smem_u32(&c->o_full[1]), o_phase[1], &c->abort)) return;
+        if (!mbar_wait(smem_u32(&c->o_full[1]), o1_phase, &c->abort)) return;
         if (!mbar_wait(smem_u32(&c->ml_full), ml_phase, &c->abort)) return;
         ml_phase ^= 1;
       }
-      if (st == 0 && (join || g.pair)) o_phase[1] ^= 1;
+      if (st == 0 && (join || g.pair)) o1_phase ^= 1;
       tc_fence_after();
       finish(g, t0, rows, join, m, l);
       tc_fence_before();
