@@ -300,6 +300,18 @@ def test_attend_many_ragged_sequences():
     check_attend(seqs, 4, 2, 64, BF16, poison=False)
 
 
+@pytest.mark.parametrize("hq,hkv,d,window", [(16, 8, 64, 0), (8, 8, 128, 200), (28, 4, 128, 0)])
+def test_attend_more_items_than_processors(hq, hkv, d, window):
+    """Batches whose items a processor takes several of, in an order that is not theirs."""
+    g = torch.Generator().manual_seed(hq)
+    seqs = []
+    for i in range(60):
+        n = [1, 0, 77, 300, 129][i % 5] + int(torch.randint(0, 30, (1,), generator=g)) * (i % 2)
+        seqs.append((n, n + int(torch.randint(0, 1500, (1,), generator=g)) * (i % 3)))
+    check_attend(seqs, hq, hkv, d, BF16, window)
+    check_attend(seqs * 5, hq, hkv, d, F16, window, poison=False)  # 300 sequences
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "spikes"])
 def test_attend_maxima_that_move(order):
     """Scores whose running maximum moves a little, a lot, or far below what came before."""
