@@ -561,48 +561,47 @@ struct Issuer {
   Ring ring;
   uint32_t p_phases = 0;  // bit per stream
 
-  // Stage of the next tile, once it has landed (-1: gave up).
-  __device__ __forceinline__ int take() {
-    const int at = ring.at;
-    const bool ok = mbar_wait(smem_u32(&c->kv_full[at]), ring.phase, &c->abort);
-    ring.step(L::kStages);
-    return ok ? at : -1;
-  }
-  __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
   static __device__ __forceinline__ bool lead() { return elect_one(); }
+  __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
 
   __device__ __forceinline__ void scores(int st, int slot, int stage) {
     const uint32_t q = desc_lo(base + L::kQ + slot * L::kStage, 16), k = desc_lo(base + L::kKv + stage * L::kStage, 16);
     const uint32_t d = tmem + col_s(st);
-    if (!lead()) return;
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
       const uint32_t at = ((i / 4) * L::kHalf + (i % 4) * 32) / 16;
       mma_ss(d, q + at, k + at, desc_hi(1024), mma_desc(kBf16, 128, kKeys, false), i > 0);
     }
-    mma_commit(smem_u32(&c->s_full[st]));
   }
-  // Rows of V that no row of the item may see (past the sequence's end they hold anything): zeros.
-  __device__ __forceinline__ void clear(const Segment& g, int stage, int j) {
-    const int lo = max(g.k.from - j * kKeys, 0), hi = min(g.k.to - j * kKeys, kKeys);
-    if (lo == 0 && hi == kKeys) return;
-    char* v = smem + L::kKv + stage * L::kStage;
-    const int lane = threadIdx.x & 31, gone = lo + kKeys - hi;
-    for (int i = lane; i < gone * (DP / 8); i += 32) {
-      const int r = i / (DP / 8), ch = i % (DP / 8), row = r < lo ? r : hi + r - lo;
-      *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
-    }
-    fence_async_shared();
-    __syncwarp();
-  }
-  // O of the stream (+)= weights times values.
-  __device__ __forceinline__ void product(int st, int stage, bool fresh) {
+  // O of the stream (+)= weights times values, over pages [lo, hi) of the block.
+  __device__ __forceinline__ void product(int st, int stage, int lo, int hi, bool fresh) {
     const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
     const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
-    if (!lead()) return;
 #pragma unroll
-    for (int i = 0; i < kKeys / 16; ++i)
-      mma_ts(d, p + i * 8, v + i * 16 * 128 / 16, desc_hi(1024), mma_desc(kBf16, 128, DP, true), !fresh || i > 0);
+    for (int i = 0; i < kPages; ++i)
+      if (i >= lo && i < hi)
+        mma_ts(d, p + i * 8, v + i * kBlockTokens * 128 / 16, desc_hi(1024), mma_desc(kBf16, 128, DP, true),
+               !fresh || i > lo);
+  }
+  // Keys of block j that no row of the item sees but that share a page with one that is seen: their
+  // values may be anything (a sequence's last page is filled to its length only), and are cleared.
+  __device__ __forceinline__ bool ragged(const Segment& g, int j) const {
+    return ((g.k.from > j * kKeys && g.k.from % kBlockTokens) ||
+            (g.k.to < (j + 1) * kKeys && g.k.to % kBlockTokens));
+  }
+  __device__ __forceinline__ void clear(const Segment& g, int stage, int j) {
+    const int lane = threadIdx.x & 31, from = g.k.from - j * kKeys, to = g.k.to - j * kKeys;
+    char* v = smem + L::kKv + stage * L::kStage;
+    auto zero = [&](int r0, int r1) {
+      for (int i = r0 * (DP / 8) + lane; i < r1 * (DP / 8); i += 32) {
+        const int row = i / (DP / 8), ch = i % (DP / 8);
+        *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+    };
+    if (from > 0) zero(from / kBlockTokens * kBlockTokens, from);
+    if (to < kKeys) zero(to, (to + kBlockTokens - 1) / kBlockTokens * kBlockTokens);
+    fence_async_shared();
+    __syncwarp();
   }
   __device__ __forceinline__ void run() {
     QuerySlots qs;
@@ -616,36 +615,52 @@ struct Issuer {
         if (!mbar_wait(smem_u32(&c->q_full[slot]), qs.phase(slot), &c->abort)) return;
       }
       tc_fence_after();
-      int k = 0, v = 0;
+      // The next tile of the ring is the values of step x, then the keys of step x + 2; in a pair the
+      // second stream uses the first one's.
+      Ring k, v;
 #pragma unroll 1
       for (int x = -2; x < n; ++x) {
-        const int st = x & 1;
+        const int st = x & 1, j = g.block(x);
         const bool first_use = !g.pair || st == 0, last_use = !g.pair || st == 1;
-        if (x >= 0) {
-          if (first_use) {
-            if ((v = take()) < 0) return;
-            clear(g, v, g.block(x));
-          }
-          if (!mbar_wait(smem_u32(&c->p_full[st]), p_phases >> st & 1, &c->abort)) return;
-          p_phases ^= 1 << st;
-          tc_fence_after();
-          product(st, v, x < 2);
-          if (lead()) {
-            if (last_use) release(v);
-            if (x + 2 >= n) mma_commit(smem_u32(&c->o_full[st]));
+        const bool has_v = x >= 0, has_k = x + 2 < n;
+        if (has_v && first_use) {
+          v = ring;
+          ring.step(L::kStages);
+          if (ragged(g, j)) {
+            if (!mbar_wait(smem_u32(&c->kv_full[v.at]), v.phase, &c->abort)) return;
+            clear(g, v.at, j);
           }
         }
-        if (x + 2 < n) {
-          if (first_use && (k = take()) < 0) return;
-          scores(st, qs.slot(g, st), k);
-          if (lead()) {
-            if (last_use) release(k);
+        if (has_k && first_use) {
+          k = ring;
+          ring.step(L::kStages);
+        }
+        // One thread waits and issues: votes and elections between the instructions left the tensor cores idle.
+        bool ok = true;
+        if (lead()) {
+          if (has_v) ok = mbar_wait_one(smem_u32(&c->kv_full[v.at]), v.phase, &c->abort);
+          if (has_k && ok) ok = mbar_wait_one(smem_u32(&c->kv_full[k.at]), k.phase, &c->abort);
+          if (has_v && ok) {
+            ok = mbar_wait_one(smem_u32(&c->p_full[st]), p_phases >> st & 1, &c->abort);
+            tc_fence_after();
+            if (ok) {
+              product(st, v.at, Loader<DP>::lo_page(g, j), Loader<DP>::hi_page(g, j), x < 2);
+              if (last_use) release(v.at);
+              if (!has_k) mma_commit(smem_u32(&c->o_full[st]));
+            }
+          }
+          if (has_k && ok) {
+            scores(st, qs.slot(g, st), k.at);
+            mma_commit(smem_u32(&c->s_full[st]));
+            if (last_use) release(k.at);
             if (x + 3 == n) {  // the last scores: the queries have been read
               mma_commit(smem_u32(&c->q_empty[qs.slot(g, 0)]));
               if (g.pair) mma_commit(smem_u32(&c->q_empty[1]));
             }
           }
         }
+        if (has_v) p_phases ^= 1 << st;
+        if (!__all_sync(0xffffffffu, ok)) return;
       }
       qs.step(g);
     }

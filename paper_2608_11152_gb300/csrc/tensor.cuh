@@ -30,22 +30,23 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 
 // Waits for the phase of the given parity, for at most kWaitCycles (about a second): returns false
-// then, or when another warp of the CTA has given up (*abort), for the whole warp alike.  The
-// caller leaves its role; the kernel ends in order with an error recorded.
+// then, or when another warp of the CTA has given up (*abort).  The caller leaves its role; the
+// kernel ends in order with an error recorded.  mbar_wait: a whole warp, with one result.
 constexpr long long kWaitCycles = 2000000000ll;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
-  bool ok = mbar_try(bar, parity);
-  if (!ok) {
-    const long long t0 = clock64();
-    while (!(ok = mbar_try(bar, parity))) {
-      if (*abort) break;
-      if (clock64() - t0 > kWaitCycles) {
-        *abort = 1;
-        break;
-      }
+__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile int* abort) {
+  if (mbar_try(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try(bar, parity)) {
+    if (*abort) return false;
+    if (clock64() - t0 > kWaitCycles) {
+      *abort = 1;
+      return false;
     }
   }
-  return __all_sync(0xffffffffu, ok);
+  return true;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait_one(bar, parity, abort));
 }
 
 // Writes of this thread to shared memory become visible to bulk copies and matrix instructions.
