@@ -21,6 +21,7 @@
 //
 // Warps: 0-3 and 4-7 softmax of stream 0 and 1; 8 loads keys and values (a page of 16 tokens is one
 // or two boxes, 2 KB each); 9 issues the matrix instructions; 10 loads queries; 11 works out the parts.
+#include <cstddef>
 #include <type_traits>
 
 #include "kv.h"
@@ -557,31 +558,41 @@ struct Issuer {
   const AttendArgs& a;
   Control* c;
   char* smem;
-  uint32_t base, tmem;
+  uint32_t base, ctl, tmem;
   Ring ring;
+  int k_stage = 0, v_stage = 0;
   uint32_t p_phases = 0;  // bit per stream
 
-  static __device__ __forceinline__ bool lead() { return elect_one(); }
-  __device__ __forceinline__ void release(int stage) { mma_commit(smem_u32(&c->kv_empty[stage])); }
+  // Address of a barrier of the control block.
+  __device__ __forceinline__ uint32_t bar(size_t offset, int i = 0) const { return ctl + (uint32_t)offset + i * 8; }
+#define MISAT_BAR(name, ...) bar(offsetof(Control, name), ##__VA_ARGS__)
 
-  __device__ __forceinline__ void scores(int st, int slot, int stage) {
+  template <int ST>
+  __device__ __forceinline__ void scores(int slot, int stage) const {
     const uint32_t q = desc_lo(base + L::kQ + slot * L::kStage, 16), k = desc_lo(base + L::kKv + stage * L::kStage, 16);
-    const uint32_t d = tmem + col_s(st);
+    const uint32_t d = tmem + col_s(ST);
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
       const uint32_t at = ((i / 4) * L::kHalf + (i % 4) * 32) / 16;
       mma_ss(d, q + at, k + at, desc_hi(1024), mma_desc(kBf16, 128, kKeys, false), i > 0);
     }
   }
-  // O of the stream (+)= weights times values, over pages [lo, hi) of the block.
-  __device__ __forceinline__ void product(int st, int stage, int lo, int hi, bool fresh) {
+  // O of the stream (+)= weights times values, over the pages of the block that hold visible keys.
+  template <int ST>
+  __device__ __forceinline__ void product(const Segment& g, int stage, int j, bool fresh) const {
     const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
-    const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
+    const uint32_t d = tmem + col_o<DP>(ST), p = tmem + col_s(ST);
+    constexpr uint32_t id = mma_desc(kBf16, 128, DP, true);
+    if (j * kKeys >= g.k.from && (j + 1) * kKeys <= g.k.to) {
 #pragma unroll
-    for (int i = 0; i < kPages; ++i)
-      if (i >= lo && i < hi)
-        mma_ts(d, p + i * 8, v + i * kBlockTokens * 128 / 16, desc_hi(1024), mma_desc(kBf16, 128, DP, true),
-               !fresh || i > lo);
+      for (int i = 0; i < kPages; ++i)
+        mma_ts(d, p + i * 8, v + i * kBlockTokens * 128 / 16, desc_hi(1024), id, !fresh || i > 0);
+    } else {
+      const int lo = Loader<DP>::lo_page(g, j), hi = Loader<DP>::hi_page(g, j);
+#pragma unroll 1
+      for (int i = lo; i < hi; ++i)
+        mma_ts(d, p + i * 8, v + i * kBlockTokens * 128 / 16, desc_hi(1024), id, !fresh || i > lo);
+    }
   }
   // Keys of block j that no row of the item sees but that share a page with one that is seen: their
   // values may be anything (a sequence's last page is filled to its length only), and are cleared.
@@ -603,6 +614,41 @@ struct Issuer {
     fence_async_shared();
     __syncwarp();
   }
+  // Step x, by one thread.  The ring's next tile is the values of step x, then the keys of step x + 2;
+  // in a pair the second stream uses the first one's.
+  template <int ST>
+  __device__ __forceinline__ bool step(const Segment& g, int x, int n, int slot0, int slot) {
+    const bool has_v = x >= 0, has_k = x + 2 < n;
+    const bool first_use = !g.pair || ST == 0, last_use = !g.pair || ST == 1;
+    if (has_v) {
+      if (first_use) {
+        v_stage = ring.at;
+        if (!mbar_wait_one(MISAT_BAR(kv_full, v_stage), ring.phase, &c->abort)) return false;
+        ring.step(L::kStages);
+      }
+      if (!mbar_wait_one(MISAT_BAR(p_full, ST), p_phases >> ST & 1, &c->abort)) return false;
+      p_phases ^= 1 << ST;
+      tc_fence_after();
+      product<ST>(g, v_stage, g.block(x), x < 2);
+      if (last_use) mma_commit(MISAT_BAR(kv_empty, v_stage));
+      if (!has_k) mma_commit(MISAT_BAR(o_full, ST));
+    }
+    if (has_k) {
+      if (first_use) {
+        k_stage = ring.at;
+        if (!mbar_wait_one(MISAT_BAR(kv_full, k_stage), ring.phase, &c->abort)) return false;
+        ring.step(L::kStages);
+      }
+      scores<ST>(slot, k_stage);
+      mma_commit(MISAT_BAR(s_full, ST));
+      if (last_use) mma_commit(MISAT_BAR(kv_empty, k_stage));
+      if (x + 3 == n) {  // the last scores: the queries have been read
+        mma_commit(MISAT_BAR(q_empty, slot0));
+        if (g.pair) mma_commit(MISAT_BAR(q_empty, 1));
+      }
+    }
+    return true;
+  }
   __device__ __forceinline__ void run() {
     QuerySlots qs;
     Feed feed{c};
@@ -615,60 +661,42 @@ struct Issuer {
         if (!mbar_wait(smem_u32(&c->q_full[slot]), qs.phase(slot), &c->abort)) return;
       }
       tc_fence_after();
-      // The next tile of the ring is the values of step x, then the keys of step x + 2; in a pair the
-      // second stream uses the first one's.
-      Ring k, v;
+      // Steps in runs: one thread waits and issues without a vote or an election in between, which left the
+      // tensor cores idle; the warp meets where values have to be cleared, at the ends of the item's keys.
+      const int slot0 = qs.slot(g, 0), slot1 = qs.slot(g, 1), by = g.pair ? 2 : 1;
+      const int tail = ragged(g, g.j0 + g.nb - 1) ? n - by : n;
 #pragma unroll 1
-      for (int x = -2; x < n; ++x) {
-        const int st = x & 1, j = g.block(x);
-        const bool first_use = !g.pair || st == 0, last_use = !g.pair || st == 1;
-        const bool has_v = x >= 0, has_k = x + 2 < n;
-        if (has_v && first_use) {
-          v = ring;
-          ring.step(L::kStages);
-          if (ragged(g, j)) {
-            if (!mbar_wait(smem_u32(&c->kv_full[v.at]), v.phase, &c->abort)) return;
-            clear(g, v.at, j);
-          }
+      for (int x = -2; x < n;) {
+        int end = x < 0 ? 0 : x < tail ? tail : n;
+        if (x >= 0 && ragged(g, g.block(x))) {
+          end = x + by;
+          if (!mbar_wait(MISAT_BAR(kv_full, ring.at), ring.phase, &c->abort)) return;
+          clear(g, ring.at, g.block(x));
         }
-        if (has_k && first_use) {
-          k = ring;
-          ring.step(L::kStages);
+        int state = 0;
+        uint32_t lead;
+        if (elect_one(lead)) {
+          bool ok = true;
+#pragma unroll 1
+          for (int y = x; y < min(end, n) && ok; ++y)
+            ok = y & 1 ? step<1>(g, y, n, slot0, slot1) : step<0>(g, y, n, slot0, slot0);
+          state = ring.at | (int)ring.phase << 8 | (int)p_phases << 9 | (int)ok << 11;
         }
-        // One thread waits and issues: votes and elections between the instructions left the tensor cores idle.
-        bool ok = true;
-        if (lead()) {
-          if (has_v) ok = mbar_wait_one(smem_u32(&c->kv_full[v.at]), v.phase, &c->abort);
-          if (has_k && ok) ok = mbar_wait_one(smem_u32(&c->kv_full[k.at]), k.phase, &c->abort);
-          if (has_v && ok) {
-            ok = mbar_wait_one(smem_u32(&c->p_full[st]), p_phases >> st & 1, &c->abort);
-            tc_fence_after();
-            if (ok) {
-              product(st, v.at, Loader<DP>::lo_page(g, j), Loader<DP>::hi_page(g, j), x < 2);
-              if (last_use) release(v.at);
-              if (!has_k) mma_commit(smem_u32(&c->o_full[st]));
-            }
-          }
-          if (has_k && ok) {
-            scores(st, qs.slot(g, st), k.at);
-            mma_commit(smem_u32(&c->s_full[st]));
-            if (last_use) release(k.at);
-            if (x + 3 == n) {  // the last scores: the queries have been read
-              mma_commit(smem_u32(&c->q_empty[qs.slot(g, 0)]));
-              if (g.pair) mma_commit(smem_u32(&c->q_empty[1]));
-            }
-          }
-        }
-        if (has_v) p_phases ^= 1 << st;
-        if (!__all_sync(0xffffffffu, ok)) return;
+        state = __shfl_sync(0xffffffffu, state, lead);
+        ring.at = state & 0xff;
+        ring.phase = state >> 8 & 1;
+        p_phases = state >> 9 & 3;
+        if (!(state >> 11 & 1)) return;
+        x = end;
       }
       qs.step(g);
     }
   }
-  // After a wait that ran out: the instructions issued are waited for before tensor memory is freed.
+  // The instructions issued and their arrivals are waited for (for a bounded time) before tensor memory is
+  // freed and the CTA's shared memory with it.
   __device__ __forceinline__ void drain() {
     int go_on = 0;
-    if (lead()) mma_commit(smem_u32(&c->drain));
+    if (elect_one()) mma_commit(smem_u32(&c->drain));
     __syncwarp();
     mbar_wait(smem_u32(&c->drain), 0, &go_on);
   }
@@ -987,8 +1015,9 @@ struct Softmax {
       }
       if (st == 1 && !g.pair) continue;
       if (join) {
-        if (!mbar_wait(smem_u32(&c->o_full[1]), o1_phase, &c->abort)) return;
+        // In this order: o_full[1] may be a phase behind until stream 1 says that its item is done.
         if (!mbar_wait(smem_u32(&c->ml_full), ml_phase, &c->abort)) return;
+        if (!mbar_wait(smem_u32(&c->o_full[1]), o1_phase, &c->abort)) return;
         ml_phase ^= 1;
       }
       if (st == 0 && (join || g.pair)) o1_phase ^= 1;
@@ -1059,9 +1088,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         ld.run();
         if (*(volatile int*)&c->abort) ld.drain();
       } else if (warp == 9) {
-        Issuer<T, DP> is{a, c, smem, smem_u32(smem), tmem};
+        Issuer<T, DP> is{a, c, smem, smem_u32(smem), smem_u32(smem) + L::kCtl, tmem};
         is.run();
-        if (*(volatile int*)&c->abort) is.drain();
+        is.drain();
       } else if (warp == 10) {
         load_queries<T, DP>(a, smem, c);
       } else {

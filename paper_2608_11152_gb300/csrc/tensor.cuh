@@ -180,13 +180,18 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, ui
       "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)add)
       : "memory");
 }
-// One lane of a converged warp, always the same.
-__device__ __forceinline__ bool elect_one() {
+// One lane of a converged warp, always the same; `lane` gets its number.  (Behind this test the compiler knows
+// that one thread is left, and an instruction for one thread costs half of what it does behind lane == 0.)
+__device__ __forceinline__ bool elect_one(uint32_t& lane) {
   uint32_t p;
   asm volatile(
-      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(p));
+      "{\n\t.reg .pred p;\n\telect.sync %1|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p), "=r"(lane));
   return p != 0;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t lane;
+  return elect_one(lane);
 }
 // bar gets one arrival when every matrix instruction that this thread issued before is complete.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
