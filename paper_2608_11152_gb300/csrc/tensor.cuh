@@ -32,13 +32,13 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 // Waits for the phase of the given parity, for at most kWaitCycles (about a second): returns false
 // then, or when another warp of the CTA has given up (*abort).  The caller leaves its role; the
 // kernel ends in order with an error recorded.  mbar_wait: a whole warp, with one result.
-constexpr long long kWaitCycles = 2000000000ll;
+constexpr uint32_t kWaitCycles = 2000000000u;
 __device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile int* abort) {
   if (mbar_try(bar, parity)) return true;
-  const long long t0 = clock64();
+  const uint32_t t0 = (uint32_t)clock();
   while (!mbar_try(bar, parity)) {
     if (*abort) return false;
-    if (clock64() - t0 > kWaitCycles) {
+    if ((uint32_t)clock() - t0 > kWaitCycles) {
       *abort = 1;
       return false;
     }
