@@ -45,7 +45,7 @@ struct AttendArgs {
   float* lse;
   float scale, c;  // c = scale * log2(e)
   int32_t group, hkv, d, n_blocks, window, tok;  // tok: tokens of a stream's tile
-  bool vec_q, vec_out;  // rows at 16-byte boundaries
+  bool map_q, vec_out;  // queries through a tensor map; output rows at 16-byte boundaries
   float4* ws_o;  // [slots][DP / 4][128 rows]
   float2* ws_ml; // [slots][128 rows]: m, l
   unsigned* ctr; // [2 x CTAs] arrivals of split items, zero between calls
@@ -500,44 +500,40 @@ struct QuerySlots {
 };
 
 template <class T, int DP>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, char* smem, Control* c) {
+__device__ __forceinline__ void load_queries(const AttendArgs& a, const CUtensorMap* map, char* smem, Control* c) {
   using L = Layout<DP>;
-  constexpr int kChunks = DP / 8;  // 16-byte pieces of a row
-  const int lane = threadIdx.x & 31, ch = lane % kChunks;
+  const int lane = threadIdx.x & 31;
   QuerySlots qs;
   Feed feed{c};
   for (; const Segment* g = feed.next(); feed.done()) {
     if (g->nb == 0) continue;
     for (int st = 0; st < (g->pair ? 2 : 1); ++st) {
       const int slot = qs.slot(*g, st);
+      const uint32_t full = smem_u32(&c->q_full[slot]);
       if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort)) return;
-      const int t0 = st * a.tok, rows = min(a.tok, g->nt - t0) * a.group;
-      char* dst = smem + L::kQ + slot * L::kStage + (ch / 8) * L::kHalf;
-      const T* src = static_cast<const T*>(a.q.p) + (int64_t)(g->s.begin + g->t0 + t0) * a.q.ts +
-                     (int64_t)g->h * a.group * a.q.hs + ch * 8;
-      // Row r is token r / group and head r % group; elements past d are zeros.
-      int r = lane / kChunks, t = r / a.group, h = r - t * a.group;
-#pragma unroll 4
-      for (; r < rows; r += 32 / kChunks) {
-        char* to = dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-        const T* from = src + (int64_t)t * a.q.ts + (int64_t)h * a.q.hs;
-        if (a.vec_q) {
-          copy16(smem_u32(to), ch * 8 < a.d ? from : a.q.p, ch * 8 < a.d ? 16 : 0);
-        } else {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (ch * 8 < a.d) {
-            const uint16_t* e = reinterpret_cast<const uint16_t*>(from);
-            v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16,
-                           e[6] | (uint32_t)e[7] << 16);
-          }
-          *reinterpret_cast<uint4*>(to) = v;
+      const int token = g->s.begin + g->t0 + st * a.tok, head = g->h * a.group;
+      char* dst = smem + L::kQ + slot * L::kStage;
+      // Row r of a tile is token r / group and head r % group: the order of a box of heads and tokens.
+      if (a.map_q) {
+        if (elect_one()) {
+          mbar_expect(full, DP * 2 * a.group * a.tok);
+          for (int x = 0; x < DP; x += 64)
+            tma_load_3d(smem_u32(dst) + x / 64 * L::kHalf, map, full, x, head, token);
         }
-        for (h += 32 / kChunks; h >= a.group; h -= a.group) ++t;
+        continue;
       }
-      copy16_wait();
+      // Rows that no map can describe: an element at a time; elements past d are zeros.
+      const int rows = min(a.tok, g->nt - st * a.tok) * a.group;
+      for (int i = lane; i < rows * DP; i += 32) {
+        const int r = i / DP, e = i % DP, t = r / a.group;
+        const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (int64_t)(token + t) * a.q.ts +
+                            (int64_t)(head + r - t * a.group) * a.q.hs;
+        *reinterpret_cast<uint16_t*>(dst + e / 64 * L::kHalf + r * 128 + ((e / 8 & 7) ^ (r & 7)) * 16 + e % 8 * 2) =
+            e < a.d ? q[e] : 0;
+      }
       fence_async_shared();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&c->q_full[slot]));
+      if (lane == 0) mbar_arrive(full);
     }
     qs.step(*g);
   }
@@ -1036,7 +1032,7 @@ struct Softmax {
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
     k_attend(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k,
-             const __grid_constant__ CUtensorMap map_v) {
+             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_q) {
   using L = Layout<DP>;
   extern __shared__ __align__(1024) char smem[];
   Control* c = reinterpret_cast<Control*>(smem + L::kCtl);
@@ -1069,6 +1065,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 8 && elect_one()) {
     prefetch_map(&map_k);
     prefetch_map(&map_v);
+    if (a.map_q) prefetch_map(&map_q);
   }
   tc_fence_before();
   __syncthreads();
@@ -1092,7 +1089,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         is.run();
         is.drain();
       } else if (warp == 10) {
-        load_queries<T, DP>(a, smem, c);
+        load_queries<T, DP>(a, &map_q, smem, c);
       } else {
         feed(a, c, w);
       }
@@ -1114,8 +1111,18 @@ int allow_smem() {
 }
 
 template <class T, int DP>
-void launch(const misat_kv* kv, const AttendArgs& a, cudaStream_t st) {
-  launch_chained(k_attend<T, DP>, kv->num_sms, kThreads, smem_bytes<DP>(), st, a, kv->map_k, kv->map_v);
+void launch(const misat_kv* kv, const AttendArgs& a, const CUtensorMap& map_q, cudaStream_t st) {
+  launch_chained(k_attend<T, DP>, kv->num_sms, kThreads, smem_bytes<DP>(), st, a, kv->map_k, kv->map_v, map_q);
+}
+
+// Map of [n2][n1][d] 16-bit elements, strides in bytes, for boxes of 64 elements x b1 x b2.
+bool encode_map(const misat_kv* kv, CUtensorMap* map, void* p, cuuint64_t n1, cuuint64_t stride1, cuuint64_t n2,
+                cuuint64_t stride2, cuuint32_t b1, cuuint32_t b2) {
+  const cuuint64_t dims[3] = {(cuuint64_t)kv->d, n1, n2}, strides[2] = {stride1, stride2};
+  const cuuint32_t box[3] = {64, b1, b2}, unit[3] = {1, 1, 1};
+  return kv->encode(map, kv->dtype == MISAT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                    3, p, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -1128,20 +1135,13 @@ int attend_prepare(misat_kv* kv) {
   if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
       found != cudaDriverEntryPointSuccess)
     return MISAT_ERR_CUDA;
-  const auto encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
+  kv->encode = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn);
   // [blocks x kv heads][16][d]; a box is 64 elements of the 16 tokens of one block and head.  Elements past d
   // are filled with zeros, so a head of any size up to 64 or 128 uses the whole tile.
-  const cuuint64_t dims[3] = {(cuuint64_t)kv->d, kBlockTokens, (cuuint64_t)kv->n_blocks * kv->hkv};
-  const cuuint64_t strides[2] = {(cuuint64_t)kv->d * 2, (cuuint64_t)kv->d * 2 * kBlockTokens};
-  const cuuint32_t box[3] = {64, kBlockTokens, 1}, unit[3] = {1, 1, 1};
-  for (int i = 0; i < 2; ++i) {
-    const CUresult r = encode(i ? &kv->map_v : &kv->map_k,
-                              kv->dtype == MISAT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                              3, i ? kv->vb : kv->kb, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return MISAT_ERR_CUDA;
-  }
+  const cuuint64_t rows = (cuuint64_t)kv->n_blocks * kv->hkv, row = (cuuint64_t)kv->d * 2;
+  if (!encode_map(kv, &kv->map_k, kv->kb, kBlockTokens, row, rows, row * kBlockTokens, kBlockTokens, 1) ||
+      !encode_map(kv, &kv->map_v, kv->vb, kBlockTokens, row, rows, row * kBlockTokens, kBlockTokens, 1))
+    return MISAT_ERR_CUDA;
   const bool bf = kv->dtype == MISAT_BF16;
   const int dp = kv->d > 64 ? 128 : 64;
   const int rc = dp == 128 ? (bf ? allow_smem<__nv_bfloat16, 128>() : allow_smem<__half, 128>())
@@ -1159,10 +1159,16 @@ void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& 
                    cudaStream_t st) {
   const int group = kv->hq / kv->hkv;
   AttendArgs a{b, q, out, lse, kv->scale, kv->scale * 1.4426950408889634f, group, kv->hkv, kv->d, kv->n_blocks, window,
-               kTile / group, aligned16(q, 2), aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+               kTile / group, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+  // Queries come through a map where rows start at 16-byte boundaries (a head or token that is read as
+  // several has a stride of zero, which a map cannot have); the strides of single heads and tokens are free.
+  CUtensorMap map_q{};
+  const int64_t hs = kv->hq > 1 ? q.hs : kv->d, ts = b.n_tokens > 1 ? q.ts : (int64_t)kv->hq * kv->d;
+  if (aligned16({q.p, ts, hs}, 2) && hs > 0 && ts > 0)
+    a.map_q = encode_map(kv, &map_q, q.p, kv->hq, hs * 2, b.n_tokens, ts * 2, group, a.tok);
   const bool bf = kv->dtype == MISAT_BF16;
-  if (kv->d > 64) bf ? launch<__nv_bfloat16, 128>(kv, a, st) : launch<__half, 128>(kv, a, st);
-  else bf ? launch<__nv_bfloat16, 64>(kv, a, st) : launch<__half, 64>(kv, a, st);
+  if (kv->d > 64) bf ? launch<__nv_bfloat16, 128>(kv, a, map_q, st) : launch<__half, 128>(kv, a, map_q, st);
+  else bf ? launch<__nv_bfloat16, 64>(kv, a, map_q, st) : launch<__half, 64>(kv, a, map_q, st);
 }
 
 }  // namespace misat

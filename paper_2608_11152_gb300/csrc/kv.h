@@ -27,6 +27,7 @@ struct misat_kv {
   void* vb;
   int32_t* err;  // device, sticky
   // of the attention kernel: maps of the blocks, partial sums of split items, their arrivals
+  decltype(&cuTensorMapEncodeTiled) encode;
   CUtensorMap map_k, map_v;
   float4* ws_o;
   float2* ws_ml;
