@@ -82,7 +82,7 @@ __device__ __forceinline__ int item_cost(const AttendArgs& a, const Seq& s, int 
   return max(span_of(a, s, t0, min(2 * a.tok, s.n - t0)).blocks, 1);
 }
 __device__ __forceinline__ int n_items(const AttendArgs& a, const Seq& s) {
-  return (s.n + 2 * a.tok - 1) / (2 * a.tok);
+  return (uint32_t)(s.n + 2 * a.tok - 1) / (uint32_t)(2 * a.tok);
 }
 
 // A CTA's part of one item.
@@ -124,6 +124,7 @@ struct Walk {
   // In columns: the sequence, head and tile of the item, from the number of items before each sequence.
   __device__ __forceinline__ void locate(const AttendArgs& a, const int* before) {
     int lo = 0, hi = a.b.n;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
       if (before[mid] <= item) lo = mid;
@@ -252,11 +253,20 @@ __device__ __forceinline__ void feed(const AttendArgs& a, Control* c, Walk w) {
 }
 
 // ---- the run of each CTA ----
-__device__ __forceinline__ int64_t div_up(int64_t x, uint32_t d) {  // a 64-bit division takes hundreds of cycles
-  return (x >> 31) == 0 ? ((uint32_t)x + d - 1) / d : (x + d - 1) / d;
-}
+// x / d.  Counts of blocks fit 31 bits but for the wildest batches; those take 63 steps instead of the
+// hundreds of instructions that a 64-bit division is at every place of use.
 __device__ __forceinline__ int64_t div_down(int64_t x, int64_t d) {
-  return (x >> 32) == 0 && (d >> 32) == 0 ? (uint32_t)x / (uint32_t)d : x / d;
+  if ((x >> 31) == 0 && (d >> 31) == 0) return (uint32_t)x / (uint32_t)d;
+  uint64_t q = 0, r = 0;
+#pragma unroll 1
+  for (int i = 62; i >= 0; --i) {
+    r = r << 1 | ((uint64_t)x >> i & 1);
+    if (r >= (uint64_t)d) {
+      r -= (uint64_t)d;
+      q |= (uint64_t)1 << i;
+    }
+  }
+  return (int64_t)q;
 }
 
 // Where this CTA's run begins and how long it is; every thread takes part.
@@ -275,6 +285,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   };
   auto cost_of = [&](const Seq& s) -> Cost {
     Cost r{0, n_items(a, s), 0};
+#pragma unroll 1
     for (int t = 0; t < r.items; ++t) {
       const int k = item_cost(a, s, t);
       r.blocks += k;
@@ -285,6 +296,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   const Seq mine = tid < a.b.n ? load_seq(a, tid) : Seq{0, 0, 0};
   const Cost first = cost_of(mine);
   Cost sum = first;
+#pragma unroll 1
   for (int b = tid + kThreads; b < a.b.n; b += kThreads) {
     const Cost r = cost_of(load_seq(a, b));
     sum.blocks += r.blocks;
@@ -311,7 +323,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   }
   total *= a.hkv;
   items *= a.hkv;
-  int64_t per = div_up(total, gridDim.x);
+  int64_t per = div_down(total + gridDim.x - 1, gridDim.x);
   const bool whole = items <= gridDim.x && longest <= per + kSplit;
   if (whole) {
     per = longest;
@@ -321,7 +333,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   }
   const int64_t lo = per * blockIdx.x;
   if (lo >= total) return false;
-  const int rows = (int)((items + gridDim.x - 1) / gridDim.x);
+  const int rows = (int)div_down(items + gridDim.x - 1, gridDim.x);
   if (rows > 1 && a.b.n <= kMaxSeqs && items <= kMaxItems) {
     // Items before each sequence, the cost of each column, and the place in the column.
     auto scan = [&](int64_t v) {  // sum over the threads before this one
@@ -349,6 +361,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
     const int cols = ((int)items + rows - 1) / rows;
     auto cost_at = [&](int item) {
       int x = 0, y = a.b.n;
+#pragma unroll 1
       while (y - x > 1) {
         const int mid = (x + y) / 2;
         if (c->before[mid] <= item) x = mid;
@@ -359,11 +372,13 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
     };
     int64_t v = 0;
     if (tid < cols)
+#pragma unroll 1
       for (int i = tid; i < (int)items; i += cols) v += cost_at(i);
     const int64_t before = scan(v);
     if (before <= lo && lo < before + v) {
       int64_t rest = lo - before;
       int i = tid;
+#pragma unroll 1
       for (int cost; rest >= (cost = cost_at(i)); i += cols) rest -= cost;
       c->start = Walk{0, 0, 0, (int)rest, 0, cols, i, (int)items, min(per, total - lo), lo, {0, 0, 0}};
       c->per = per;
@@ -375,6 +390,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
     return true;
   }
   int64_t base = 0;
+#pragma unroll 1
   for (int b0 = 0; base <= lo; b0 += kThreads) {
     const Seq s = b0 == 0 ? mine : b0 + tid < a.b.n ? load_seq(a, b0 + tid) : Seq{0, 0, 0};
     const int64_t v = (whole ? (int64_t)n_items(a, s) * longest : b0 == 0 ? first.blocks : cost_of(s).blocks) * a.hkv;
@@ -402,6 +418,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
         t = (int)div_down(rest, longest);
         rest = 0;
       } else {
+#pragma unroll 1
         for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
       }
       c->start = Walk{b0 + tid, (int)h, t, (int)rest, whole ? longest : 0, 0, 0, 0, min(per, total - lo), lo, s};
