@@ -45,6 +45,7 @@ struct AttendArgs {
   float* lse;
   float scale, c;  // c = scale * log2(e)
   int32_t group, hkv, d, n_blocks, window, tok;  // tok: tokens of a stream's tile
+  bool small;           // find_run_small's conditions hold
   bool map_q, vec_out;  // queries through a tensor map; output rows at 16-byte boundaries
   float4* ws_o;  // [slots][DP / 4][128 rows]
   float2* ws_ml; // [slots][128 rows]: m, l
@@ -172,6 +173,17 @@ struct Walk {
   }
 };
 
+// Blocks, items and longest item of a sequence and one kv head, or of several.
+struct Cost {
+  int64_t blocks;
+  int items, longest;
+  __device__ __forceinline__ void add(const Cost& r) {
+    blocks += r.blocks;
+    items += r.items;
+    longest = max(longest, r.longest);
+  }
+};
+
 // ---- shared memory ----
 
 constexpr int kSegs = 4;
@@ -194,8 +206,7 @@ struct Control {
   uint64_t ml_full, ml_free, wg[2], drain;
   float2 ml[kTile];  // m and l of stream 1 for the join
   int before[kMaxSeqs];  // items before each sequence, where they are taken in columns
-  int64_t sum[kThreads / 32];
-  int items[kThreads / 32], longest[kThreads / 32];
+  Cost sum[kThreads / 32];
   Walk start;
   int64_t per;  // length of a run
   int last[2];
@@ -269,96 +280,136 @@ __device__ __forceinline__ int64_t div_down(int64_t x, int64_t d) {
   return (int64_t)q;
 }
 
-// Where this CTA's run begins and how long it is; every thread takes part.
+__device__ __forceinline__ Cost cost_of(const AttendArgs& a, const Seq& s) {
+  Cost r{0, n_items(a, s), 0};
+#pragma unroll 1
+  for (int t = 0; t < r.items; ++t) {
+    const int k = item_cost(a, s, t);
+    r.blocks += k;
+    r.longest = max(r.longest, k);
+  }
+  return r;
+}
+__device__ __forceinline__ void warp_sum(Cost& r) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) r.blocks += __shfl_xor_sync(0xffffffffu, r.blocks, o);
+  r.items = __reduce_add_sync(0xffffffffu, r.items);
+  r.longest = __reduce_max_sync(0xffffffffu, r.longest);
+}
+__device__ __forceinline__ int64_t warp_scan(int64_t v) {  // sum over this lane and those before it
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t t = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += t;
+  }
+  return v;
+}
+
+// How the blocks are dealt out, from their sum over the batch.
 //
 // With at most one item per CTA, an item is split only where that saves more than kSplit blocks of the
 // longest one: writing, announcing and joining the parts takes about as long as kSplit blocks
-// (4 sequences of 17 to 640 tokens, 8 kv heads: 12.6 us split evenly, 8.9 us whole).  Whole items then count
-// as equally long (`pad`).  A part has two blocks at least: the streams take them at the same time.
+// (4 sequences of 17 to 640 tokens, 8 kv heads: 14.8 us split evenly, 14.1 us whole).  Whole items then count
+// as equally long.  A part has two blocks at least: the streams take them at the same time.
 constexpr int kSplit = 8;
+struct Deal {
+  int64_t total, items, per;
+  int longest;
+  bool whole;
+  __device__ __forceinline__ Deal(const AttendArgs& a, const Cost& sum)
+      : total(sum.blocks * a.hkv), items((int64_t)sum.items * a.hkv), longest(sum.longest) {
+    per = div_down(total + gridDim.x - 1, gridDim.x);
+    whole = items <= gridDim.x && longest <= per + kSplit;
+    if (whole) {
+      per = longest;
+      total = items * longest;
+    } else if (per < 2) {
+      per = 2;
+    }
+  }
+  __device__ __forceinline__ int64_t lo() const { return per * blockIdx.x; }
+};
+
+// The place of block `lo` in sequence b, whose blocks are [before, before + v).
+__device__ __forceinline__ Walk place(const AttendArgs& a, const Deal& d, int b, const Seq& s, int64_t before,
+                                      int64_t v) {
+  const int64_t head = div_down(v, a.hkv), h = div_down(d.lo() - before, head);
+  int64_t rest = d.lo() - before - h * head;
+  int t = 0;
+  if (d.whole) {
+    t = (int)div_down(rest, d.longest);
+    rest = 0;
+  } else {
+#pragma unroll 1
+    for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
+  }
+  return {b, (int)h, t, (int)rest, d.whole ? d.longest : 0, 0, 0, 0, min(d.per, d.total - d.lo()), d.lo(), s};
+}
+
+// Where this CTA's run begins and how long it is, for at most 32 sequences with at most one item per CTA:
+// by one warp, a lane per sequence, while the others set out.
+__device__ __forceinline__ bool find_run_small(const AttendArgs& a, Control* c, Walk& w) {
+  const int lane = threadIdx.x & 31;
+  const Seq s = lane < a.b.n ? load_seq(a, lane) : Seq{0, 0, 0};
+  const Cost mine = cost_of(a, s);
+  Cost sum = mine;
+  warp_sum(sum);
+  const Deal d(a, sum);
+  if (d.lo() >= d.total) return false;
+  const int64_t v = (d.whole ? (int64_t)mine.items * d.longest : mine.blocks) * a.hkv;
+  const int64_t before = warp_scan(v) - v;
+  if (before <= d.lo() && d.lo() < before + v) {
+    c->start = place(a, d, lane, s, before, v);
+    c->per = d.per;
+  }
+  __syncwarp();
+  w = c->start;
+  return true;
+}
+
+// The same by all threads, for any batch.
 __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* seqs, Walk& w) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kWarps = kThreads / 32;
-  struct Cost {
-    int64_t blocks;
-    int items, longest;
-  };
-  auto cost_of = [&](const Seq& s) -> Cost {
-    Cost r{0, n_items(a, s), 0};
-#pragma unroll 1
-    for (int t = 0; t < r.items; ++t) {
-      const int k = item_cost(a, s, t);
-      r.blocks += k;
-      r.longest = max(r.longest, k);
-    }
-    return r;
-  };
   const Seq mine = tid < a.b.n ? load_seq(a, tid) : Seq{0, 0, 0};
-  const Cost first = cost_of(mine);
+  const Cost first = cost_of(a, mine);
   Cost sum = first;
 #pragma unroll 1
-  for (int b = tid + kThreads; b < a.b.n; b += kThreads) {
-    const Cost r = cost_of(load_seq(a, b));
-    sum.blocks += r.blocks;
-    sum.items += r.items;
-    sum.longest = max(sum.longest, r.longest);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum.blocks += __shfl_xor_sync(0xffffffffu, sum.blocks, o);
-  sum.items = __reduce_add_sync(0xffffffffu, sum.items);
-  sum.longest = __reduce_max_sync(0xffffffffu, sum.longest);
-  if (lane == 0) {
-    c->sum[warp] = sum.blocks;
-    c->items[warp] = sum.items;
-    c->longest[warp] = sum.longest;
-  }
+  for (int b = tid + kThreads; b < a.b.n; b += kThreads) sum.add(cost_of(a, load_seq(a, b)));
+  warp_sum(sum);
+  if (lane == 0) c->sum[warp] = sum;
   __syncthreads();
-  int64_t total = 0, items = 0;
-  int longest = 0;
+  sum = Cost{0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    total += c->sum[i];
-    items += c->items[i];
-    longest = max(longest, c->longest[i]);
-  }
-  total *= a.hkv;
-  items *= a.hkv;
-  int64_t per = div_down(total + gridDim.x - 1, gridDim.x);
-  const bool whole = items <= gridDim.x && longest <= per + kSplit;
-  if (whole) {
-    per = longest;
-    total = items * longest;
-  } else if (per < 2) {
-    per = 2;
-  }
-  const int64_t lo = per * blockIdx.x;
-  if (lo >= total) return false;
-  const int rows = (int)div_down(items + gridDim.x - 1, gridDim.x);
-  if (rows > 1 && a.b.n <= kMaxSeqs && items <= kMaxItems) {
+  for (int i = 0; i < kWarps; ++i) sum.add(c->sum[i]);
+  const Deal d(a, sum);
+  const int64_t lo = d.lo();
+  if (lo >= d.total) return false;
+  auto scan = [&](int64_t v, int64_t& all) {  // sum over the threads before this one, and over all
+    const int64_t inc = warp_scan(v);
+    __syncthreads();
+    if (lane == 31) c->sum[warp].blocks = inc;
+    __syncthreads();
+    int64_t before = inc - v;
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) before += c->sum[i].blocks;
+      all += c->sum[i].blocks;
+    }
+    return before;
+  };
+  int64_t all;
+  const int rows = (int)div_down(d.items + gridDim.x - 1, gridDim.x);
+  if (rows > 1 && a.b.n <= kMaxSeqs && d.items <= kMaxItems) {
     // Items before each sequence, the cost of each column, and the place in the column.
-    auto scan = [&](int64_t v) {  // sum over the threads before this one
-      int64_t inc = v;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      __syncthreads();
-      if (lane == 31) c->sum[warp] = inc;
-      __syncthreads();
-      int64_t before = inc - v;
-#pragma unroll
-      for (int i = 0; i < kWarps; ++i)
-        if (i < warp) before += c->sum[i];
-      return before;
-    };
-    const int64_t mine_before = scan((int64_t)first.items * a.hkv);
+    const int64_t mine_before = scan((int64_t)first.items * a.hkv, all);
     if (tid < a.b.n) {
       c->before[tid] = (int)mine_before;
       seqs[tid] = mine;
     }
     __syncthreads();
-    const int cols = ((int)items + rows - 1) / rows;
+    const int items = (int)d.items, cols = (items + rows - 1) / rows;
     auto cost_at = [&](int item) {
       int x = 0, y = a.b.n;
 #pragma unroll 1
@@ -373,15 +424,15 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
     int64_t v = 0;
     if (tid < cols)
 #pragma unroll 1
-      for (int i = tid; i < (int)items; i += cols) v += cost_at(i);
-    const int64_t before = scan(v);
+      for (int i = tid; i < items; i += cols) v += cost_at(i);
+    const int64_t before = scan(v, all);
     if (before <= lo && lo < before + v) {
       int64_t rest = lo - before;
       int i = tid;
 #pragma unroll 1
       for (int cost; rest >= (cost = cost_at(i)); i += cols) rest -= cost;
-      c->start = Walk{0, 0, 0, (int)rest, 0, cols, i, (int)items, min(per, total - lo), lo, {0, 0, 0}};
-      c->per = per;
+      c->start = Walk{0, 0, 0, (int)rest, 0, cols, i, items, min(d.per, d.total - lo), lo, {0, 0, 0}};
+      c->per = d.per;
     }
     fence_async_shared();  // `seqs` lies where keys are going to land
     __syncthreads();
@@ -393,36 +444,13 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
 #pragma unroll 1
   for (int b0 = 0; base <= lo; b0 += kThreads) {
     const Seq s = b0 == 0 ? mine : b0 + tid < a.b.n ? load_seq(a, b0 + tid) : Seq{0, 0, 0};
-    const int64_t v = (whole ? (int64_t)n_items(a, s) * longest : b0 == 0 ? first.blocks : cost_of(s).blocks) * a.hkv;
-    int64_t inc = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += t;
-    }
-    __syncthreads();
-    if (lane == 31) c->sum[warp] = inc;
-    __syncthreads();
-    int64_t before = base;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      if (i < warp) before += c->sum[i];
-      base += c->sum[i];
-    }
-    before += inc - v;
+    const int64_t v =
+        (d.whole ? (int64_t)n_items(a, s) * d.longest : b0 == 0 ? first.blocks : cost_of(a, s).blocks) * a.hkv;
+    const int64_t before = base + scan(v, all);
+    base += all;
     if (before <= lo && lo < before + v) {
-      const int64_t head = div_down(v, a.hkv), h = div_down(lo - before, head);
-      int64_t rest = lo - before - h * head;
-      int t = 0;
-      if (whole) {
-        t = (int)div_down(rest, longest);
-        rest = 0;
-      } else {
-#pragma unroll 1
-        for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
-      }
-      c->start = Walk{b0 + tid, (int)h, t, (int)rest, whole ? longest : 0, 0, 0, 0, min(per, total - lo), lo, s};
-      c->per = per;
+      c->start = place(a, d, b0 + tid, s, before, v);
+      c->per = d.per;
     }
   }
   __syncthreads();
@@ -1090,7 +1118,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = c->tmem;
   chain_wait();
   Walk w;
-  if (find_run(a, c, reinterpret_cast<Seq*>(smem + L::kKv), w)) {
+  if (a.small || find_run(a, c, reinterpret_cast<Seq*>(smem + L::kKv), w)) {
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
       Softmax<T, DP> s{a, c, tmem + ((uint32_t)(warp & 3) << 21), warp / 4, (int)(threadIdx.x & 127)};
@@ -1108,6 +1136,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else if (warp == 10) {
         load_queries<T, DP>(a, &map_q, smem, c);
       } else {
+        if (a.small && !find_run_small(a, c, w)) w.left = 0;
         feed(a, c, w);
       }
     }
@@ -1176,7 +1205,8 @@ void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& 
                    cudaStream_t st) {
   const int group = kv->hq / kv->hkv;
   AttendArgs a{b, q, out, lse, kv->scale, kv->scale * 1.4426950408889634f, group, kv->hkv, kv->d, kv->n_blocks, window,
-               kTile / group, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+               kTile / group, false, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+  a.small = b.n <= 32 && (b.n_tokens / (2 * a.tok) + (int64_t)b.n) * kv->hkv <= kv->num_sms;
   // Queries come through a map where rows start at 16-byte boundaries (a head or token that is read as
   // several has a stride of zero, which a map cannot have); the strides of single heads and tokens are free.
   CUtensorMap map_q{};
