@@ -506,19 +506,17 @@ struct Loader {
     for (; const Segment* p = feed.next(); feed.done()) {
       const Segment g = *p;
       if (g.nb == 0) continue;
-      int cur = page(g, g.j0), ahead = g.nb > 1 ? page(g, g.j0 + 1) : 0;
-      if (!load(g, map_k, g.j0, cur)) return;
-      if (!g.pair && g.nb > 1 && !load(g, map_k, g.j0 + 1, ahead)) return;
-      for (int j = g.j0, end = g.j0 + g.nb; j < end; ++j) {
-        const int ahead2 = j + 2 < end ? page(g, j + 2) : 0;
-        if (!load(g, map_v, j, cur)) return;
-        if (g.pair) {
-          if (j + 1 < end && !load(g, map_k, j + 1, ahead)) return;
-        } else {
-          if (j + 2 < end && !load(g, map_k, j + 2, ahead2)) return;
-        }
-        cur = ahead;
-        ahead = ahead2;
+      // Table entries of the blocks of steps x, x + 1 and x + 2 (in a pair: of block x / 2 and the next one).
+      const int n = g.nb, lead = g.pair ? 1 : 2;
+      int now = 0, next = 0, ahead = page(g, g.j0);
+#pragma unroll 1
+      for (int j = -lead; j < n; ++j) {
+        const int fetched = j + lead + 1 < n ? page(g, g.j0 + j + lead + 1) : 0;
+        if (j >= 0 && !load(g, map_v, g.j0 + j, now)) return;
+        if (j + lead < n && !load(g, map_k, g.j0 + j + lead, ahead)) return;
+        now = g.pair ? ahead : next;
+        next = ahead;
+        ahead = fetched;
       }
     }
   }
@@ -608,10 +606,9 @@ struct Issuer {
   __device__ __forceinline__ uint32_t bar(size_t offset, int i = 0) const { return ctl + (uint32_t)offset + i * 8; }
 #define MISAT_BAR(name, ...) bar(offsetof(Control, name), ##__VA_ARGS__)
 
-  template <int ST>
-  __device__ __forceinline__ void scores(int slot, int stage) const {
+  __device__ __forceinline__ void scores(int st, int slot, int stage) const {
     const uint32_t q = desc_lo(base + L::kQ + slot * L::kStage, 16), k = desc_lo(base + L::kKv + stage * L::kStage, 16);
-    const uint32_t d = tmem + col_s(ST);
+    const uint32_t d = tmem + col_s(st);
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
       const uint32_t at = ((i / 4) * L::kHalf + (i % 4) * 32) / 16;
@@ -619,10 +616,9 @@ struct Issuer {
     }
   }
   // O of the stream (+)= weights times values, over the pages of the block that hold visible keys.
-  template <int ST>
-  __device__ __forceinline__ void product(const Segment& g, int stage, int j, bool fresh) const {
+  __device__ __forceinline__ void product(const Segment& g, int st, int stage, int j, bool fresh) const {
     const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
-    const uint32_t d = tmem + col_o<DP>(ST), p = tmem + col_s(ST);
+    const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
     constexpr uint32_t id = mma_desc(kBf16, 128, DP, true);
     if (j * kKeys >= g.k.from && (j + 1) * kKeys <= g.k.to) {
 #pragma unroll
@@ -657,22 +653,22 @@ struct Issuer {
   }
   // Step x, by one thread.  The ring's next tile is the values of step x, then the keys of step x + 2;
   // in a pair the second stream uses the first one's.
-  template <int ST>
-  __device__ __forceinline__ bool step(const Segment& g, int x, int n, int slot0, int slot) {
+  __device__ __forceinline__ bool step(const Segment& g, int x, int n, int slot0, int slot1) {
+    const int st = x & 1, slot = st ? slot1 : slot0;
     const bool has_v = x >= 0, has_k = x + 2 < n;
-    const bool first_use = !g.pair || ST == 0, last_use = !g.pair || ST == 1;
+    const bool first_use = !g.pair || st == 0, last_use = !g.pair || st == 1;
     if (has_v) {
       if (first_use) {
         v_stage = ring.at;
         if (!mbar_wait_one(MISAT_BAR(kv_full, v_stage), ring.phase, &c->abort)) return false;
         ring.step(L::kStages);
       }
-      if (!mbar_wait_one(MISAT_BAR(p_full, ST), p_phases >> ST & 1, &c->abort)) return false;
-      p_phases ^= 1 << ST;
+      if (!mbar_wait_one(MISAT_BAR(p_full, st), p_phases >> st & 1, &c->abort)) return false;
+      p_phases ^= 1 << st;
       tc_fence_after();
-      product<ST>(g, v_stage, g.block(x), x < 2);
+      product(g, st, v_stage, g.block(x), x < 2);
       if (last_use) mma_commit(MISAT_BAR(kv_empty, v_stage));
-      if (!has_k) mma_commit(MISAT_BAR(o_full, ST));
+      if (!has_k) mma_commit(MISAT_BAR(o_full, st));
     }
     if (has_k) {
       if (first_use) {
@@ -680,8 +676,8 @@ struct Issuer {
         if (!mbar_wait_one(MISAT_BAR(kv_full, k_stage), ring.phase, &c->abort)) return false;
         ring.step(L::kStages);
       }
-      scores<ST>(slot, k_stage);
-      mma_commit(MISAT_BAR(s_full, ST));
+      scores(st, slot, k_stage);
+      mma_commit(MISAT_BAR(s_full, st));
       if (last_use) mma_commit(MISAT_BAR(kv_empty, k_stage));
       if (x + 3 == n) {  // the last scores: the queries have been read
         mma_commit(MISAT_BAR(q_empty, slot0));
@@ -720,7 +716,7 @@ struct Issuer {
           bool ok = true;
 #pragma unroll 1
           for (int y = x; y < min(end, n) && ok; ++y)
-            ok = y & 1 ? step<1>(g, y, n, slot0, slot1) : step<0>(g, y, n, slot0, slot0);
+            ok = step(g, y, n, slot0, slot1);
           state = ring.at | (int)ring.phase << 8 | (int)p_phases << 9 | (int)ok << 11;
         }
         state = __shfl_sync(0xffffffffu, state, lead);
@@ -961,33 +957,51 @@ struct Softmax {
     if (!c->last[st]) return true;
     __threadfence();
     if (wt == 0) a.ctr[c0 * 2 + st] = 0;
+    // A thread has eight columns of a row, and goes through the parts with a running maximum, kAhead of
+    // them loaded at a time: each round of loads is a trip to the L2 cache.
+    constexpr int kAhead = 8;
     const int n = rows * (a.d / 8);
-    int have = -1;
-    float top = 0.f;
+#pragma unroll 1
     for (int i = wt; i < n; i += 128) {
       const int r = i % rows, g8 = i / rows;
-      if (r != have) {
-        have = r;
-        top = -INFINITY;
-        for (int p = c0; p <= c1; ++p) top = fmaxf(top, __ldcg(a.ws_ml + ((p * 2 + (p == c0)) * 2 + st) * kTile + r).x);
-      }
-      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0.f;
-#pragma unroll 4
-      for (int p = c0; p <= c1; ++p) {
-        const int slot = (p * 2 + (p == c0)) * 2 + st;
-        const float2 ml = __ldcg(a.ws_ml + slot * kTile + r);
-        const float4* o = a.ws_o + ((int64_t)slot * (DP / 4) + g8 * 2) * kTile + r;
-        const float4 u = __ldcg(o), v = __ldcg(o + kTile);
-        const float f = ml.x == top ? 1.f : exp2_approx((ml.x - top) * a.c);
-        sum += ml.y * f;
-        x[0] += u.x * f;
-        x[1] += u.y * f;
-        x[2] += u.z * f;
-        x[3] += u.w * f;
-        x[4] += v.x * f;
-        x[5] += v.y * f;
-        x[6] += v.z * f;
-        x[7] += v.w * f;
+      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0.f, top = -INFINITY;
+#pragma unroll 1
+      for (int p0 = c0; p0 <= c1; p0 += kAhead) {
+        float2 ml[kAhead];
+        float4 u[kAhead], v[kAhead];
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int p = p0 + k, slot = (p * 2 + (p == c0)) * 2 + st;
+          ml[k] = make_float2(-INFINITY, 0.f);
+          u[k] = v[k] = make_float4(0, 0, 0, 0);
+          if (p <= c1) {
+            ml[k] = __ldcg(a.ws_ml + slot * kTile + r);
+            const float4* o = a.ws_o + ((int64_t)slot * (DP / 4) + g8 * 2) * kTile + r;
+            u[k] = __ldcg(o);
+            v[k] = __ldcg(o + kTile);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) next = fmaxf(next, ml[k].x);
+        const float old = top == next ? 1.f : exp2_approx((top - next) * a.c);
+        sum *= old;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= old;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float f = ml[k].x == next ? 1.f : exp2_approx((ml[k].x - next) * a.c);
+          sum += ml[k].y * f;
+          x[0] += u[k].x * f;
+          x[1] += u[k].y * f;
+          x[2] += u[k].z * f;
+          x[3] += u[k].w * f;
+          x[4] += v[k].x * f;
+          x[5] += v[k].y * f;
+          x[6] += v[k].z * f;
+          x[7] += v[k].w * f;
+        }
+        top = next;
       }
       const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
 #pragma unroll
