@@ -471,7 +471,8 @@ int misat_recheck_delays(int32_t n, const uint64_t* group, const uint8_t* held, 
  *     anything of a call for the next, so all of them can be captured into a CUDA graph).
  *     A pool's calls share its workspace: calls on two streams must be ordered by the caller.
  *   - A tensor of heads is [n_tokens][heads][head_dim] with the elements of a head next to
- *     each other and any non-negative strides between tokens and heads, given in elements.
+ *     each other and any non-negative strides between tokens and heads, given in elements (in
+ *     a tensor that is written, positive ones).
  *     Rows at 16-byte boundaries are moved 16 bytes at a time, others an element at a time.
  *   - Whole numbers found malformed on the device (offsets out of order, a length beyond its
  *     block table, a block outside the pool) are sticky errors of the pool, returned by
@@ -547,7 +548,7 @@ typedef struct misat_kv_batch {
   int32_t n_tokens;           /* q_off[n] */
   int32_t max_q;              /* at least the new tokens of any sequence */
   const int32_t* q_off;       /* [n+1], q_off[0] = 0, non-decreasing */
-  const int32_t* kv_len;      /* [n] tokens of the sequence, the new ones included */
+  const int32_t* kv_len;      /* [n] tokens of the sequence, the new ones included; at most 2^30 */
   const int32_t* block_table; /* [n][table_stride] */
   int64_t table_stride;       /* blocks per row, kv_len <= 16 table_stride */
 } misat_kv_batch;

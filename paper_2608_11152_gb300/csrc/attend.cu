@@ -62,7 +62,7 @@ struct Seq {
 __device__ __forceinline__ Seq load_seq(const AttendArgs& a, int b) {
   const int begin = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
   const bool ok = begin >= 0 && end >= begin && end <= a.b.n_tokens && end - begin <= a.b.max_q && len >= 0 &&
-                  len <= a.b.stride * kBlockTokens;
+                  len <= kMaxLen && len <= a.b.stride * kBlockTokens;
   if (!ok) set_error(a.err, MISAT_ERR_INVALID_ARG);
   return {begin, ok ? end - begin : 0, len};
 }
@@ -231,6 +231,7 @@ struct Ring {
 };
 
 // ---- the parts of a run, from the warp that works them out to the others ----
+constexpr int kItemLimit = 64;  // limit of waits that last as long as an item: 2^30 keys take some 15 seconds
 constexpr int kReaders = 11;  // 8 softmax warps, keys and values, matrix instructions, queries
 struct Feed {
   Control* c;
@@ -254,7 +255,7 @@ __device__ __forceinline__ void feed(const AttendArgs& a, Control* c, Walk w) {
     Segment g;
     more = w.next(a, c->before, g);
     if (!more) g.nb = -1;
-    if (!mbar_wait(smem_u32(&c->seg_empty[ring.at]), ring.phase ^ 1, &c->abort)) return;
+    if (!mbar_wait(smem_u32(&c->seg_empty[ring.at]), ring.phase ^ 1, &c->abort, kItemLimit)) return;
     if (lead) {
       c->seg[ring.at] = g;
       mbar_arrive(smem_u32(&c->seg_full[ring.at]));
@@ -553,7 +554,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const CUtensor
     for (int st = 0; st < (g->pair ? 2 : 1); ++st) {
       const int slot = qs.slot(*g, st);
       const uint32_t full = smem_u32(&c->q_full[slot]);
-      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort)) return;
+      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort, kItemLimit)) return;
       const int token = g->s.begin + g->t0 + st * a.tok, head = g->h * a.group;
       char* dst = smem + L::kQ + slot * L::kStage;
       // Row r of a tile is token r / group and head r % group: the order of a box of heads and tokens.

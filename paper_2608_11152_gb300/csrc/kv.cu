@@ -66,7 +66,7 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
                     int64_t o_ts, int64_t o_hs, float* lse, int32_t window, void* cuda_stream) {
   if (!batch_ok(kv, batch) || window < 0) return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
-  if (!heads_ok(q, q_ts, q_hs, 2) || !heads_ok(out, o_ts, o_hs, 2) || (reinterpret_cast<uintptr_t>(lse) & 3) ||
+  if (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) || (reinterpret_cast<uintptr_t>(lse) & 3) ||
       !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
   launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, window,

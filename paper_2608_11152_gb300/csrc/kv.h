@@ -51,16 +51,22 @@ struct KvBatch {
   int64_t stride;
 };
 
+constexpr int kMaxLen = 1 << 30;  // tokens of a sequence
+
 // Checks of the arguments that both pool calls share.  A tensor's pointer has to be aligned to its
 // elements; strides may be anything non-negative.
 inline bool heads_ok(const void* p, int64_t ts, int64_t hs, int elem) {
   return p && ts >= 0 && hs >= 0 && (reinterpret_cast<uintptr_t>(p) % elem) == 0;
 }
+// A tensor that is written: no two tokens or heads in one place.
+inline bool result_ok(const void* p, int64_t ts, int64_t hs, int elem, int n_tokens, int n_heads) {
+  return heads_ok(p, ts, hs, elem) && (n_tokens <= 1 || ts > 0) && (n_heads <= 1 || hs > 0);
+}
 inline bool batch_ok(const misat_kv* kv, const misat_kv_batch* b) {
   if (!kv || !b || b->n < 0 || b->n > kv->max_batch || b->n_tokens < 0 || b->max_q < 0 || b->table_stride < 0)
     return false;
   if (b->n_tokens > 0 && b->n == 0) return false;
-  return b->n_tokens == 0 || (b->q_off && b->kv_len && b->block_table);
+  return b->n_tokens == 0 || (b->q_off && b->kv_len && (b->block_table || b->table_stride == 0));
 }
 inline KvBatch batch_view(const misat_kv_batch* b) {
   return {b->n, b->n_tokens, b->max_q, b->q_off, b->kv_len, b->block_table, b->table_stride};

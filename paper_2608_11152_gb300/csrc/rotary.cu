@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, HALF ? 5 : 7) k_rotate(const __grid_
     const int from = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
     const int64_t pos = (int64_t)len - end + t;
     const bool ok = from <= t && t < end && end - from <= a.b.max_q && len >= end - from && pos >= 0 &&
-                    pos < a.b.stride * kBlockTokens;
+                    len <= kMaxLen && pos < a.b.stride * kBlockTokens;
     int64_t at = -1;
     if (ok) {
       const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
@@ -344,7 +344,8 @@ int misat_rotary(const misat_rope* r, int32_t dtype, int32_t n_tokens, int32_t n
     return MISAT_ERR_INVALID_ARG;
   if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
   const int elem = dtype == MISAT_F32 ? 4 : 2;
-  if (!heads_ok(x, x_ts, x_hs, elem) || !heads_ok(out, o_ts, o_hs, elem) || !positions) return MISAT_ERR_INVALID_ARG;
+  if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions)
+    return MISAT_ERR_INVALID_ARG;
   if (x == out && (x_ts != o_ts || x_hs != o_hs)) return MISAT_ERR_INVALID_ARG;
   if (!on_device(r->device)) return MISAT_ERR_INVALID_ARG;
   RotArgs a{};
@@ -368,7 +369,7 @@ int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, in
   if (!batch_ok(kv, batch)) return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!heads_ok(k, k_ts, k_hs, 2) || !heads_ok(v, v_ts, v_hs, 2)) return MISAT_ERR_INVALID_ARG;
-  if (q && (!heads_ok(q, q_ts, q_hs, 2) || !heads_ok(q_out, qo_ts, qo_hs, 2) ||
+  if (q && (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(q_out, qo_ts, qo_hs, 2, batch->n_tokens, kv->hq) ||
             (q == q_out && (q_ts != qo_ts || q_hs != qo_hs))))
     return MISAT_ERR_INVALID_ARG;
   if (!on_device(kv->device)) return MISAT_ERR_INVALID_ARG;

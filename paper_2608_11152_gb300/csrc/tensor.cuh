@@ -29,24 +29,27 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Waits for the phase of the given parity, for at most kWaitCycles (about a second): returns false
+// Waits for the phase of the given parity, for at most `limit` times kWaitCycles (about a second): returns false
 // then, or when another warp of the CTA has given up (*abort).  The caller leaves its role; the
 // kernel ends in order with an error recorded.  mbar_wait: a whole warp, with one result.
 constexpr uint32_t kWaitCycles = 2000000000u;
-__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile int* abort) {
+__device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile int* abort, int limit = 1) {
   if (mbar_try(bar, parity)) return true;
-  const uint32_t t0 = (uint32_t)clock();
+  uint32_t t0 = (uint32_t)clock();
   while (!mbar_try(bar, parity)) {
     if (*abort) return false;
     if ((uint32_t)clock() - t0 > kWaitCycles) {
-      *abort = 1;
-      return false;
+      if (--limit == 0) {
+        *abort = 1;
+        return false;
+      }
+      t0 = (uint32_t)clock();
     }
   }
   return true;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
-  return __all_sync(0xffffffffu, mbar_wait_one(bar, parity, abort));
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort, int limit = 1) {
+  return __all_sync(0xffffffffu, mbar_wait_one(bar, parity, abort, limit));
 }
 
 // Writes of this thread to shared memory become visible to bulk copies and matrix instructions.

@@ -149,6 +149,15 @@ def test_rotary_gradient_against_differences():
         assert abs(grad.view(-1)[i] - want) < 2 * 4 * 8 * 6 * 2.0 ** -23
 
 
+def test_rotary_positions_far_out_and_negative():
+    m = misat()
+    x = rand((6, 2, 64), F32, 1)
+    pos = torch.tensor([2 ** 31 - 1, -(2 ** 31), -1, 123456789, 1 << 24, (1 << 24) + 1], device="cuda", dtype=torch.int32)
+    y, tol = ref.rotate(x, pos, ref.frequencies(64), True)
+    # the 64-bit angle of the definition itself is only good to 2^31 * 2^-53 radians
+    ref.assert_within("rotate", m.Rope(64).rotate(x, pos), y, tol + 2.0 ** -21 * x.double().abs().cpu().amax())
+
+
 def test_rotary_empty():
     m = misat()
     rope = m.Rope(16)
@@ -528,4 +537,10 @@ def test_null_and_misaligned_pointers_are_refused_by_the_library():
     assert a(pool._h, b._ref, p, 64, 32, None, 64, 32, None, 0, 0, None, 0, 0, st) == m.ERR_INVALID_ARG
     assert a(pool._h, b._ref, p, 64, 32, p, 64, 32, p, 64, 32, None, 0, 0, st) == m.ERR_INVALID_ARG
     assert m._lib.misat_rotary(None, 0, 1, 1, 16, p, 16, 16, p, p, 16, 16, 0, st) == m.ERR_INVALID_ARG
+    # results whose heads or tokens would share a place
+    assert f(pool._h, b._ref, p, 64, 32, p, 64, 0, None, 0, st) == m.ERR_INVALID_ARG
+    rope = m.Rope(16)
+    for ts, hs in ((0, 16), (32, 0)):
+        assert m._lib.misat_rotary(rope._h, 0, 2, 2, 16, p, 32, 16, s.kv_len.data_ptr(), p, ts, hs, 0, st) == \
+            m.ERR_INVALID_ARG
     assert m._lib.misat_kv_create(None, ctypes.byref(ctypes.c_void_p())) == m.ERR_INVALID_ARG
