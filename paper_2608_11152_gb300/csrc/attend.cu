@@ -21,6 +21,7 @@
 //
 // Warps: 0-3 and 4-7 softmax of stream 0 and 1; 8 loads keys and values (a page of 16 tokens is one
 // or two boxes, 2 KB each); 9 issues the matrix instructions; 10 loads queries; 11 works out the parts.
+#include <algorithm>
 #include <cstddef>
 #include <type_traits>
 
@@ -44,7 +45,7 @@ struct AttendArgs {
   Heads q, out;
   float* lse;
   float scale, c;  // c = scale * log2(e)
-  int32_t group, hkv, d, n_blocks, window, tok;  // tok: tokens of a stream's tile
+  int32_t group, hkv, d, n_blocks, window, tok, rows;  // tok: tokens of a stream's tile; rows: of the fullest tile
   bool small;           // find_run_small's conditions hold
   bool map_q, vec_out;  // queries through a tensor map; output rows at 16-byte boundaries
   float4* ws_o;  // [slots][DP / 4][128 rows]
@@ -311,8 +312,15 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v) {  // sum over this lane
 // With at most one item per CTA, an item is split only where that saves more than kSplit blocks of the
 // longest one: writing, announcing and joining the parts takes about as long as kSplit blocks
 // (4 sequences of 17 to 640 tokens, 8 kv heads: 14.8 us split evenly, 14.1 us whole).  Whole items then count
-// as equally long.  A part has two blocks at least: the streams take them at the same time.
+// as equally long.
+//
+// A part has two blocks at least, which the streams take at the same time, and no fewer than make the
+// parts' time and the time to join them even: n blocks in p parts take n / p block times, and the join
+// p / kJoin block times for up to 8 rows, in proportion more for more of them (2 sequences of 6,400 tokens
+// with 280 new ones, 2 heads of 128: 63 us with kJoin = 112, 51 with 28, 46 with 14 and 7, 59 with 1.75;
+// one of 30,000 tokens with 64 new ones, 8 heads: 101, 73, 68, 73 and 98).
 constexpr int kSplit = 8;
+constexpr float kJoin = 14.f;
 struct Deal {
   int64_t total, items, per;
   int longest;
@@ -324,8 +332,8 @@ struct Deal {
     if (whole) {
       per = longest;
       total = items * longest;
-    } else if (per < 2) {
-      per = 2;
+    } else {
+      per = max(per, (int64_t)max(2.f, sqrtf((float)longest * (float)max(a.rows, 8) / (8.f * kJoin))));
     }
   }
   __device__ __forceinline__ int64_t lo() const { return per * blockIdx.x; }
@@ -1220,7 +1228,7 @@ void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& 
                    cudaStream_t st) {
   const int group = kv->hq / kv->hkv;
   AttendArgs a{b, q, out, lse, kv->scale, kv->scale * 1.4426950408889634f, group, kv->hkv, kv->d, kv->n_blocks, window,
-               kTile / group, false, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+               kTile / group, (int)std::min<int64_t>((int64_t)b.max_q * group, kTile / group * group), false, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
   a.small = b.n <= 32 && (b.n_tokens / (2 * a.tok) + (int64_t)b.n) * kv->hkv <= kv->num_sms;
   // Queries come through a map where rows start at 16-byte boundaries (a head or token that is read as
   // several has a stride of zero, which a map cannot have); the strides of single heads and tokens are free.
