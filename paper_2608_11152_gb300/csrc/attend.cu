@@ -47,7 +47,7 @@ struct AttendArgs {
   float scale, c;  // c = scale * log2(e)
   int32_t group, hkv, d, n_blocks, window, tok, rows;  // tok: tokens of a stream's tile; rows: of the fullest tile
   bool small;           // find_run_small's conditions hold
-  bool map_q, vec_out;  // queries through a tensor map; output rows at 16-byte boundaries
+  bool map_q, vec_out, vec32;  // queries through a tensor map; output rows at 16- and 32-byte boundaries
   float4* ws_o;  // [slots][DP / 4][128 rows]
   float2* ws_ml; // [slots][128 rows]: m, l
   unsigned* ctr; // [2 x CTAs] arrivals of split items, zero between calls
@@ -811,12 +811,12 @@ struct Softmax {
       top_of(r[q], mx);
     }
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-    if (fresh) {
-      m = top;
-    } else {
+    // While a row has seen no key (a window that begins inside the block), its O and l are zeros of any scale.
+    if (fresh || m == -INFINITY) m = top;
+    if (!fresh) {
       const bool need = top > m && !((top - m) * a.c <= kRescale);
       if (__any_sync(0xffffffffu, need)) {
-        const float f = need ? exp2_approx((m - top) * a.c) : 1.f;  // m = -inf: 0
+        const float f = need ? exp2_approx((m - top) * a.c) : 1.f;
         const uint64_t f2 = pack2(f, f);
 #pragma unroll 1
         for (int q = 0; q < DP / 16; ++q) {
@@ -933,9 +933,15 @@ struct Softmax {
         }
         if (!mine) continue;
         if (g.whole) {
+          if (a.vec32 && q + 16 <= a.d) {
+            store32(out + q, pack16<T>(x[0][0], x[0][1]), pack16<T>(x[0][2], x[0][3]), pack16<T>(x[0][4], x[0][5]),
+                    pack16<T>(x[0][6], x[0][7]), pack16<T>(x[1][0], x[1][1]), pack16<T>(x[1][2], x[1][3]),
+                    pack16<T>(x[1][4], x[1][5]), pack16<T>(x[1][6], x[1][7]));
+          } else {
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (q + e * 8 < a.d) put8(out + q + e * 8, x[e]);
+            for (int e = 0; e < 2; ++e)
+              if (q + e * 8 < a.d) put8(out + q + e * 8, x[e]);
+          }
         } else {
           float4* p = a.ws_o + ((int64_t)slot * (DP / 4) + q / 4) * kTile + row;
 #pragma unroll
@@ -1228,7 +1234,8 @@ void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& 
                    cudaStream_t st) {
   const int group = kv->hq / kv->hkv;
   AttendArgs a{b, q, out, lse, kv->scale, kv->scale * 1.4426950408889634f, group, kv->hkv, kv->d, kv->n_blocks, window,
-               kTile / group, (int)std::min<int64_t>((int64_t)b.max_q * group, kTile / group * group), false, false, aligned16(out, 2), kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
+               kTile / group, (int)std::min<int64_t>((int64_t)b.max_q * group, kTile / group * group), false, false, aligned16(out, 2),
+               ((reinterpret_cast<uintptr_t>(out.p) | (uintptr_t)(out.ts * 2) | (uintptr_t)(out.hs * 2)) & 31) == 0, kv->ws_o, kv->ws_ml, kv->ctr, kv->err};
   a.small = b.n <= 32 && (b.n_tokens / (2 * a.tok) + (int64_t)b.n) * kv->hkv <= kv->num_sms;
   // Queries come through a map where rows start at 16-byte boundaries (a head or token that is read as
   // several has a stride of zero, which a map cannot have); the strides of single heads and tokens are free.
