@@ -12,7 +12,8 @@
 // Two streams of such tiles share a CTA, so that one's matrix products run under the other's
 // exponentials.  An item of more than 128 rows gives each stream half of its rows, and both read the same
 // keys; a smaller item (a step of single tokens) gives each stream every other block of 128 keys, and
-// the first stream joins the two at the end.
+// the first stream joins the two at the end; and two such items of neighbouring heads are taken together,
+// a stream each.
 //
 // One CTA per SM.  The blocks of all items, in order, are dealt out in equal contiguous runs, so
 // long and short sequences, and the triangle of a chunk, load every SM alike.  An item that
@@ -94,15 +95,18 @@ struct Segment {
   int b, h;
   int t0, nt;          // tokens of the item
   int j0, nb;          // first block (of the sequence) and blocks of this part
-  bool pair;           // both streams have rows of their own
+  bool pair;           // both streams have rows of their own, and read the same keys
+  bool twin;           // both streams have an item of their own: the same rows of kv heads h and h + 1
   bool whole;          // the part is the item
   int64_t first, last; // the item's blocks in the order of all blocks
-  __device__ __forceinline__ int stream_blocks(int st) const { return pair ? nb : (nb + 1 - st) / 2; }
+  __device__ __forceinline__ bool both() const { return pair || twin; }  // each stream takes all blocks
+  __device__ __forceinline__ int head(int st) const { return h + (twin ? st : 0); }
+  __device__ __forceinline__ int stream_blocks(int st) const { return both() ? nb : (nb + 1 - st) / 2; }
   // The products of a part in the order of issue: step x is stream x & 1's next block.  A stream's
   // scores are formed two steps ahead of its product with the values, so the loops over the steps
   // run from -2 to steps() - 1: values of step x, then scores of step x + 2.
-  __device__ __forceinline__ int steps() const { return pair ? 2 * nb : nb; }
-  __device__ __forceinline__ int block(int step) const { return j0 + (pair ? step / 2 : step); }
+  __device__ __forceinline__ int steps() const { return both() ? 2 * nb : nb; }
+  __device__ __forceinline__ int block(int step) const { return j0 + (both() ? step / 2 : step); }
 };
 
 // The items in the order in which their blocks are dealt out.  Natural: by sequence, kv head, tile.
@@ -157,6 +161,15 @@ struct Walk {
     at += take;
     left -= take;
     off = 0;
+    // Two heads of an item at a time, where the run has both whole: they have equally many blocks, and
+    // neither waits for the other (single tokens of 256 sequences, 8 kv heads of 128, 10 to 100 cached tokens: 73.5
+    // us one by one, 38.6 in twos; 63 to 511 tokens: 108 and 77; 512 to 16,000 tokens: 1,285 and 1,275).
+    g.twin = !g.pair && g.whole && pad == 0 && cols == 0 && g.nt == s.n && h + 1 < a.hkv && left >= cost;
+    if (g.twin) {
+      at += cost;
+      left -= cost;
+      ++h;
+    }
     if (left <= 0) return true;
     if (cols > 0) {
       item = item + cols < items ? item + cols : item % cols + 1;
@@ -410,7 +423,7 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   };
   int64_t all;
   const int rows = (int)div_down(d.items + gridDim.x - 1, gridDim.x);
-  if (rows > 1 && a.b.n <= kMaxSeqs && d.items <= kMaxItems) {
+  if (rows > 1 && a.b.max_q > 2 * a.tok && a.b.n <= kMaxSeqs && d.items <= kMaxItems) {
     // Items before each sequence, the cost of each column, and the place in the column.
     const int64_t mine_before = scan((int64_t)first.items * a.hkv, all);
     if (tid < a.b.n) {
@@ -492,7 +505,7 @@ struct Loader {
                ? __ldcg(a.b.table + (int64_t)g.b * a.b.stride + j * kPages + i)
                : 0;
   }
-  __device__ __forceinline__ bool load(const Segment& g, const CUtensorMap* map, int j, int blk) {
+  __device__ __forceinline__ bool load(const Segment& g, const CUtensorMap* map, int head, int j, int blk) {
     const int lane = threadIdx.x & 31, lo = lo_page(g, j), hi = hi_page(g, j);
     const uint32_t full = smem_u32(&c->kv_full[ring.at]);
     if (!mbar_wait(smem_u32(&c->kv_empty[ring.at]), ring.phase ^ 1, &c->abort)) return false;
@@ -500,7 +513,7 @@ struct Loader {
     __syncwarp();
     const int i = lane / (DP / 64), half = lane % (DP / 64);
     if (i >= lo && i < hi) {
-      int row = blk * a.hkv + g.h;
+      int row = blk * a.hkv + head;
       if (blk < 0 || blk >= a.n_blocks) {
         set_error(a.err, MISAT_ERR_INVALID_ARG);
         row = a.n_blocks * a.hkv;  // past the tensor: the box is filled with zeros
@@ -515,14 +528,17 @@ struct Loader {
     for (; const Segment* p = feed.next(); feed.done()) {
       const Segment g = *p;
       if (g.nb == 0) continue;
-      // Table entries of the blocks of steps x, x + 1 and x + 2 (in a pair: of block x / 2 and the next one).
-      const int n = g.nb, lead = g.pair ? 1 : 2;
+      // Keys are loaded two steps ahead of values; a pair's two steps use one tile.  Table entries of the steps
+      // between, and of one more.
+      const int n = g.pair ? g.nb : g.steps(), lead = g.pair ? 1 : 2;
+      auto block = [&](int x) { return g.j0 + (g.twin ? x / 2 : x); };
       int now = 0, next = 0, ahead = page(g, g.j0);
 #pragma unroll 1
-      for (int j = -lead; j < n; ++j) {
-        const int fetched = j + lead + 1 < n ? page(g, g.j0 + j + lead + 1) : 0;
-        if (j >= 0 && !load(g, map_v, g.j0 + j, now)) return;
-        if (j + lead < n && !load(g, map_k, g.j0 + j + lead, ahead)) return;
+      for (int x = -lead; x < n; ++x) {
+        const int y = x + lead, head = g.head(x & 1);  // x and x + 2: the same stream
+        const int fetched = y + 1 < n ? page(g, block(y + 1)) : 0;
+        if (x >= 0 && !load(g, map_v, head, block(x), now)) return;
+        if (y < n && !load(g, map_k, head, block(y), ahead)) return;
         now = g.pair ? ahead : next;
         next = ahead;
         ahead = fetched;
@@ -543,11 +559,11 @@ struct Loader {
 struct QuerySlots {
   uint32_t phases = 0;  // bit per tile (phases that are chosen at run time are bits: an array would be memory)
   int turn = 0;
-  __device__ __forceinline__ int slot(const Segment& g, int st) const { return g.pair ? st : turn; }
+  __device__ __forceinline__ int slot(const Segment& g, int st) const { return g.both() ? st : turn; }
   __device__ __forceinline__ uint32_t phase(int slot) const { return phases >> slot & 1; }
   __device__ __forceinline__ void step(const Segment& g) {
-    phases ^= g.pair ? 3 : 1 << turn;
-    turn ^= !g.pair;
+    phases ^= g.both() ? 3 : 1 << turn;
+    turn ^= !g.both();
   }
 };
 
@@ -559,11 +575,12 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const CUtensor
   Feed feed{c};
   for (; const Segment* g = feed.next(); feed.done()) {
     if (g->nb == 0) continue;
-    for (int st = 0; st < (g->pair ? 2 : 1); ++st) {
+    for (int st = 0; st < (g->both() ? 2 : 1); ++st) {
       const int slot = qs.slot(*g, st);
       const uint32_t full = smem_u32(&c->q_full[slot]);
       if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort, kItemLimit)) return;
-      const int token = g->s.begin + g->t0 + st * a.tok, head = g->h * a.group;
+      const int first = g->pair ? st * a.tok : 0;  // token of the item
+      const int token = g->s.begin + g->t0 + first, head = g->head(st) * a.group;
       char* dst = smem + L::kQ + slot * L::kStage;
       // Row r of a tile is token r / group and head r % group: the order of a box of heads and tokens.
       if (a.map_q) {
@@ -575,7 +592,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const CUtensor
         continue;
       }
       // Rows that no map can describe: an element at a time; elements past d are zeros.
-      const int rows = min(a.tok, g->nt - st * a.tok) * a.group;
+      const int rows = min(a.tok, g->nt - first) * a.group;
       for (int i = lane; i < rows * DP; i += 32) {
         const int r = i / DP, e = i % DP, t = r / a.group;
         const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (int64_t)(token + t) * a.q.ts +
@@ -690,7 +707,7 @@ struct Issuer {
       if (last_use) mma_commit(MISAT_BAR(kv_empty, k_stage));
       if (x + 3 == n) {  // the last scores: the queries have been read
         mma_commit(MISAT_BAR(q_empty, slot0));
-        if (g.pair) mma_commit(MISAT_BAR(q_empty, 1));
+        if (g.both()) mma_commit(MISAT_BAR(q_empty, 1));
       }
     }
     return true;
@@ -702,7 +719,7 @@ struct Issuer {
       const Segment g = *p;
       const int n = g.steps();
       if (n == 0) continue;
-      for (int st = 0; st < (g.pair ? 2 : 1); ++st) {
+      for (int st = 0; st < (g.both() ? 2 : 1); ++st) {
         const int slot = qs.slot(g, st);
         if (!mbar_wait(smem_u32(&c->q_full[slot]), qs.phase(slot), &c->abort)) return;
       }
@@ -710,7 +727,7 @@ struct Issuer {
       // Steps in runs: one thread waits and issues without a vote or an election in between, which left the
       // tensor cores idle; the warp meets where values have to be cleared, at the ends of the item's keys.
       const int slot0 = qs.slot(g, 0), slot1 = qs.slot(g, 1), by = g.pair ? 2 : 1;
-      const int tail = ragged(g, g.j0 + g.nb - 1) ? n - by : n;
+      const int tail = ragged(g, g.j0 + g.nb - 1) ? n - (g.both() ? 2 : 1) : n;
 #pragma unroll 1
       for (int x = -2; x < n;) {
         int end = x < 0 ? 0 : x < tail ? tail : n;
@@ -876,12 +893,12 @@ struct Softmax {
   __device__ __forceinline__ T* out_row(const Segment& g, int t0, int r) const {
     const int t = r / a.group;
     return static_cast<T*>(a.out.p) + (int64_t)(g.s.begin + g.t0 + t0 + t) * a.out.ts +
-           (int64_t)(g.h * a.group + r - t * a.group) * a.out.hs;
+           (int64_t)(g.head(st) * a.group + r - t * a.group) * a.out.hs;
   }
   __device__ __forceinline__ void put_lse(const Segment& g, int t0, int r, float m, float l) const {
     if (!a.lse) return;
     const int t = r / a.group;
-    a.lse[(int64_t)(g.s.begin + g.t0 + t0 + t) * (a.group * a.hkv) + g.h * a.group + r - t * a.group] =
+    a.lse[(int64_t)(g.s.begin + g.t0 + t0 + t) * (a.group * a.hkv) + g.head(st) * a.group + r - t * a.group] =
         l > 0.f || l != l ? m * a.scale + logf(l) : -INFINITY;
   }
   // Eight elements of an output row.
@@ -1034,7 +1051,7 @@ struct Softmax {
       const int t0 = g.pair ? st * a.tok : 0;
       const int rows = min(a.tok, g.nt - t0) * a.group;
       if (g.nb == 0) {  // no row sees a key
-        if ((g.pair || st == 0) && row < rows) {
+        if ((g.both() || st == 0) && row < rows) {
           T* out = out_row(g, t0, row);
           const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
           for (int e = 0; e < a.d; e += 8) put8(out + e, zero);
@@ -1049,7 +1066,7 @@ struct Softmax {
       float m = -INFINITY, l = 0.f;
       const int nb = g.stream_blocks(st);
       for (int i = 0; i < nb; ++i) {
-        const int k0 = (g.j0 + (g.pair ? i : 2 * i + st)) * kKeys;
+        const int k0 = (g.j0 + (g.both() ? i : 2 * i + st)) * kKeys;
         if (!mbar_wait(smem_u32(&c->s_full[st]), s_phase, &c->abort)) return;
         s_phase ^= 1;
         if (active) {
@@ -1070,7 +1087,7 @@ struct Softmax {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->p_full[st]));
       }
-      const bool join = !g.pair && g.nb > 1;
+      const bool join = !g.both() && g.nb > 1;
       if (nb > 0) {
         if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase, &c->abort)) return;
         o_phase ^= 1;
@@ -1083,14 +1100,14 @@ struct Softmax {
         joined = true;
         continue;
       }
-      if (st == 1 && !g.pair) continue;
+      if (st == 1 && !g.both()) continue;
       if (join) {
         // In this order: o_full[1] may be a phase behind until stream 1 says that its item is done.
         if (!mbar_wait(smem_u32(&c->ml_full), ml_phase, &c->abort)) return;
         if (!mbar_wait(smem_u32(&c->o_full[1]), o1_phase, &c->abort)) return;
         ml_phase ^= 1;
       }
-      if (st == 0 && (join || g.pair)) o1_phase ^= 1;
+      if (st == 0 && (join || g.both())) o1_phase ^= 1;
       tc_fence_after();
       finish(g, t0, rows, join, m, l);
       tc_fence_before();

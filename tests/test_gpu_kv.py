@@ -309,6 +309,16 @@ def test_attend_many_ragged_sequences():
     check_attend(seqs, 4, 2, 64, BF16, poison=False)
 
 
+@pytest.mark.parametrize("window", [0, 37])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 64), (12, 3, 128), (10, 5, 72), (4, 1, 64)])
+def test_attend_many_single_tokens(hq, hkv, d, window):
+    """Several whole items a processor, two heads at a time; odd numbers of heads, and of blocks."""
+    g = torch.Generator().manual_seed(d)
+    seqs = [(1, int(torch.randint(1, 600 if i % 7 == 0 else 140, (1,), generator=g))) for i in range(333)]
+    check_attend(seqs, hq, hkv, d, BF16, window)
+    check_attend([(n + i % 3, L + i % 3) for i, (n, L) in enumerate(seqs)][:200], hq, hkv, d, F16, window)
+
+
 @pytest.mark.parametrize("hq,hkv,d,window", [(16, 8, 64, 0), (8, 8, 128, 200), (28, 4, 128, 0)])
 def test_attend_more_items_than_processors(hq, hkv, d, window):
     """Batches whose items a processor takes several of, in an order that is not theirs."""
