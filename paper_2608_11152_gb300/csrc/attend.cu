@@ -799,9 +799,11 @@ struct Softmax {
       uint32_t r[32];
       __syncwarp();
       tmem_ld32(r, tmem + col_s(st) + q * 32);
+      const int from = lo - q * 32, to = hi - q * 32;
+      const uint32_t seen = (from >= 32 ? 0u : ~0u << max(from, 0)) & (to >= 32 ? ~0u : (1u << max(to, 0)) - 1);
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if ((uint32_t)(q * 32 + i - lo) >= (uint32_t)(hi - lo)) r[i] = 0xff800000u;
+        if (!(seen & 1u << i)) r[i] = 0xff800000u;
       tmem_st32(tmem + col_s(st) + q * 32, r);
     }
     tc_wait_st();
