@@ -545,40 +545,21 @@ def recheck_delays(group, held, base_delay_us: int, min_delay_us: int) -> np.nda
 # ---- KV blocks of an inference instance: rotary positions, append, attention ----
 
 
-def _dtype_codes():
-    import torch
-
-    return {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+_calls = None
 
 
-def _raw_stream():
-    """A function from a device index to the current stream's cudaStream_t: the calls below are made
-    once a layer and token, and building a torch.cuda.Stream for each takes longer than the launch."""
-    import torch
+def _torch_calls():
+    """The calls on torch tensors (csrc/torch_calls.cpp); imported with the first Rope or KvPool, behind torch,
+    whose libraries it uses."""
+    global _calls
+    if _calls is None:
+        import torch  # noqa: F401
 
-    return getattr(torch._C, "_cuda_getCurrentRawStream",
-                   lambda index: torch.cuda.current_stream(index).cuda_stream)
+        from . import _calls as module
 
-
-def _heads(t, name, dtype, device, shape):
-    """Checks a [tokens, heads, head_dim] tensor whose heads are contiguous; returns its strides."""
-    if t.shape != shape or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: {dtype} {list(shape)} on {device} expected, got {t.dtype} {list(t.shape)} on "
-                         f"{t.device}")
-    s = t.stride()
-    if s[2] != 1 and shape[2] > 1:
-        raise ValueError(f"{name}: the elements of a head must be contiguous")
-    return s
-
-
-def _ints(t, name, shape, device):
-    """Checks a contiguous int32 tensor."""
-    import torch
-
-    if t.dtype != torch.int32 or t.device != device or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous int32 {list(shape)} on {device} expected, got {t.dtype} "
-                         f"{list(t.shape)} on {t.device}")
-    return t
+        module.init(MisatError)
+        _calls = module
+    return _calls
 
 
 class Rope:
@@ -592,14 +573,17 @@ class Rope:
         self.rot_dim = int(rot_dim)
         cfg = misat_rope_config(self.rot_dim, layout, scaling, base, factor, orig_len, beta_slow, beta_fast,
                                 attn_factor)
+        calls = _torch_calls()
         h = _p()
         _ck(_lib.misat_rope_create(C.byref(cfg), C.byref(h)), "misat_rope_create")
         self._h = h
-        self._empty, self._int32, self._codes, self._raw = torch.empty, torch.int32, _dtype_codes(), _raw_stream()
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._state = calls.rope_state(h.value, self.device.index)
+        self._rotary = calls.rotary
 
     def close(self):
         if getattr(self, "_h", None):
+            self._state = None
             _lib.misat_rope_destroy(self._h)
             self._h = None
 
@@ -609,62 +593,27 @@ class Rope:
         except Exception:
             pass
 
-    def _apply(self, x, positions, out, backward):
-        dev, dt, shape = self.device, x.dtype, x.shape
-        code = self._codes.get(dt)
-        if code is None or len(shape) != 3:
-            raise ValueError(f"x: [tokens, heads, head_dim] of bfloat16, float16 or float32 expected, got {dt} "
-                             f"{list(shape)}")
-        xs = _heads(x, "x", dt, dev, shape)
-        n, heads, d = shape
-        if positions.shape != (n,) or positions.dtype != self._int32 or positions.device != dev or \
-                not positions.is_contiguous():
-            _ints(positions, "positions", (n,), dev)
-        if out is None:
-            out = self._empty(shape, dtype=dt, device=dev)
-            os_ = (heads * d, d)
-        else:
-            os_ = _heads(out, "out", dt, dev, shape)
-        _ck(_lib.misat_rotary(self._h, code, n, heads, d, x.data_ptr(), xs[0], xs[1], positions.data_ptr(),
-                              out.data_ptr(), os_[0], os_[1], backward, self._raw(dev.index)), "misat_rotary")
-        return out
-
     def rotate(self, x, positions, out=None):
         """x [tokens, heads, head_dim] turned to `positions` (int32 [tokens]); out may be x."""
-        return self._apply(x, positions, out, 0)
+        return self._rotary(self._state, x, positions, out, False)
 
     def backward(self, grad, positions, out=None):
         """Gradient of rotate()'s x, given the gradient of its result."""
-        return self._apply(grad, positions, out, 1)
+        return self._rotary(self._state, grad, positions, out, True)
 
 
 class KvBatch:
-    """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer."""
+    """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer.  It serves
+    every pool of the same heads."""
 
     def __init__(self, pool, q_off, kv_len, block_table, n_tokens, max_q):
-        import torch
-
-        n, dev = kv_len.shape[0], pool.device
-        _ints(q_off, "q_off", (n + 1,), dev)
-        _ints(kv_len, "kv_len", (n,), dev)
-        if block_table.dim() != 2 or block_table.shape[0] != n or block_table.dtype != torch.int32 or \
-                block_table.device != dev:
-            raise ValueError(f"block_table: int32 [{n}, blocks] on {dev} expected, got {block_table.dtype} "
-                             f"{list(block_table.shape)} on {block_table.device}")
-        blocks = block_table.shape[1]
-        if blocks > 1 and block_table.stride(1) != 1:
-            raise ValueError("block_table: the blocks of a sequence must be contiguous")
-        stride = block_table.stride(0) if n > 1 else blocks
-        if stride < blocks:
-            raise ValueError("block_table: rows must not overlap")
-        self.n, self.n_tokens = n, int(n_tokens)
+        self._state = _torch_calls().batch_state(pool._state, q_off, kv_len, block_table, int(n_tokens), int(max_q))
         self._keep = (q_off, kv_len, block_table)
-        self._c = misat_kv_batch(n, self.n_tokens, int(max_q), q_off.data_ptr(), kv_len.data_ptr(),
+        self.n, self.n_tokens = kv_len.shape[0], int(n_tokens)
+        stride = block_table.stride(0) if self.n > 1 else block_table.shape[1]
+        self._c = misat_kv_batch(self.n, self.n_tokens, int(max_q), q_off.data_ptr(), kv_len.data_ptr(),
                                  block_table.data_ptr(), stride)
-        self._ref = C.addressof(self._c)
-        self._heads = pool._heads  # a batch serves every pool of the same heads
-        self._q = (self.n_tokens, pool.n_q_heads, pool.head_dim)
-        self._kv = (self.n_tokens, pool.n_kv_heads, pool.head_dim)
+        self._ref = C.addressof(self._c)  # for calls of the C functions
 
 
 class KvPool:
@@ -678,21 +627,20 @@ class KvPool:
     def __init__(self, k_blocks, v_blocks, *, n_q_heads, rope=None, scale=0.0, max_batch=1 << 20):
         import torch
 
-        self._torch = torch
         self._h = None
         if k_blocks.dim() != 4 or k_blocks.shape[2] != BLOCK_TOKENS or v_blocks.shape != k_blocks.shape:
             raise ValueError(f"k_blocks, v_blocks: one shape [blocks, kv heads, {BLOCK_TOKENS}, head_dim] expected")
         if not (k_blocks.is_contiguous() and v_blocks.is_contiguous()):
             raise ValueError("k_blocks, v_blocks: contiguous tensors expected")
         self.device = torch.device("cuda", torch.cuda.current_device())
-        code = _dtype_codes().get(k_blocks.dtype)
+        code = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}.get(k_blocks.dtype)
         if code is None or k_blocks.device != self.device or v_blocks.device != self.device or \
                 v_blocks.dtype != k_blocks.dtype:
             raise ValueError(f"k_blocks, v_blocks: one floating-point dtype on {self.device} expected")
+        calls = _torch_calls()
         self.dtype = k_blocks.dtype
         self.n_blocks, self.n_kv_heads, _, self.head_dim = k_blocks.shape
         self.n_q_heads = int(n_q_heads)
-        self._heads = (self.n_q_heads, self.n_kv_heads, self.head_dim)
         self.k_blocks, self.v_blocks, self.rope = k_blocks, v_blocks, rope
         cfg = misat_kv_config(self.n_blocks, self.n_kv_heads, self.n_q_heads, self.head_dim, code,
                               int(max_batch), float(scale), rope._h if rope is not None else None,
@@ -700,11 +648,12 @@ class KvPool:
         h = _p()
         _ck(_lib.misat_kv_create(C.byref(cfg), C.byref(h)), "misat_kv_create")
         self._h = h
-        self._empty, self._float32, self._raw = torch.empty, torch.float32, _raw_stream()
-        self._last, self._last_raw = None, None  # stream of the last call
+        self._state = calls.pool_state(h.value, self.device.index, k_blocks, self.n_q_heads)
+        self._append, self._attend, self._sync = calls.append, calls.attend, calls.sync
 
     def close(self):
         if getattr(self, "_h", None):
+            self._state = None
             _lib.misat_kv_destroy(self._h)
             self._h = None
 
@@ -719,59 +668,16 @@ class KvPool:
         tokens), kv_len [n] (tokens after the append), block_table [n, blocks]."""
         return KvBatch(self, q_off, kv_len, block_table, n_tokens, max_q)
 
-    def _stream(self):
-        raw = self._raw(self.device.index)
-        if raw != self._last_raw:
-            if self._torch.cuda.is_current_stream_capturing():
-                return raw  # whoever replays the graph orders it with the pool's other calls
-            st = self._torch.cuda.current_stream(self.device)
-            if self._last is not None:
-                st.wait_stream(self._last)
-            self._last, self._last_raw = st, raw
-        return raw
-
-    def _check(self, batch):
-        if batch._heads != self._heads:
-            raise ValueError(f"batch: made for (q heads, kv heads, head_dim) {batch._heads}, not {self._heads}")
-
     def append(self, batch, k, v, q=None, q_out=None):
         """Put the new tokens' k (rotated) and v, [n_tokens, kv heads, head_dim], into their
         blocks; returns the rotated q [n_tokens, q heads, head_dim] (None without q).  q_out may be q."""
-        self._check(batch)
-        dt, dev = self.dtype, self.device
-        ks, vs = _heads(k, "k", dt, dev, batch._kv), _heads(v, "v", dt, dev, batch._kv)
-        if q is None:
-            qp, qs, op, os_ = None, (0, 0), None, (0, 0)
-            q_out = None
-        else:
-            shape = batch._q
-            qs = _heads(q, "q", dt, dev, shape)
-            if q_out is None:
-                q_out = self._empty(shape, dtype=dt, device=dev)
-                os_ = (shape[1] * shape[2], shape[2])
-            else:
-                os_ = _heads(q_out, "q_out", dt, dev, shape)
-            qp, op = q.data_ptr(), q_out.data_ptr()
-        _ck(_lib.misat_kv_append(self._h, batch._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], qp,
-                                 qs[0], qs[1], op, os_[0], os_[1], self._stream()), "misat_kv_append")
-        return q_out
+        return self._append(self._state, batch._state, k, v, q, q_out)
 
     def attend(self, batch, q, out=None, window=0, return_lse=False):
         """Attention of the new tokens' q [n_tokens, q heads, head_dim] over the cached tokens up to
         and including each; window > 0: over the last `window` of them.  Returns out, or (out, lse)."""
-        self._check(batch)
-        dt, dev, shape = self.dtype, self.device, batch._q
-        qs = _heads(q, "q", dt, dev, shape)
-        if out is None:
-            out = self._empty(shape, dtype=dt, device=dev)
-            os_ = (shape[1] * shape[2], shape[2])
-        else:
-            os_ = _heads(out, "out", dt, dev, shape)
-        lse = self._empty(shape[:2], dtype=self._float32, device=dev) if return_lse else None
-        _ck(_lib.misat_kv_attend(self._h, batch._ref, q.data_ptr(), qs[0], qs[1], out.data_ptr(), os_[0], os_[1],
-                                 lse.data_ptr() if return_lse else None, window, self._stream()), "misat_kv_attend")
-        return (out, lse) if return_lse else out
+        return self._attend(self._state, batch._state, q, out, window, return_lse)
 
     def sync(self):
         """Wait for the current stream and raise the pool's sticky device error, if there is one."""
-        _ck(_lib.misat_kv_sync(self._h, self._stream()), "misat_kv_sync")
+        self._sync(self._state)
