@@ -336,6 +336,9 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v) {  // sum over this lane
 // one of 30,000 tokens with 64 new ones, 8 heads: 101, 73, 68, 73 and 98).
 constexpr int kSplit = 8;
 constexpr float kJoin = 14.f;
+__device__ __forceinline__ int least_part(const AttendArgs& a, int longest) {
+  return (int)max(2.f, sqrtf((float)longest * (float)max(a.rows, 8) / (8.f * kJoin)));
+}
 struct Deal {
   int64_t total, items, per;
   int longest;
@@ -348,7 +351,7 @@ struct Deal {
       per = longest;
       total = items * longest;
     } else {
-      per = max(per, (int64_t)max(2.f, sqrtf((float)longest * (float)max(a.rows, 8) / (8.f * kJoin))));
+      per = max(per, (int64_t)least_part(a, longest));
     }
   }
   __device__ __forceinline__ int64_t lo() const { return per * blockIdx.x; }
@@ -371,20 +374,42 @@ __device__ __forceinline__ Walk place(const AttendArgs& a, const Deal& d, int b,
 }
 
 // Where this CTA's run begins and how long it is, for at most 32 sequences with at most one item per CTA:
-// by one warp, a lane per sequence, while the others set out.
+// by one warp, a lane per sequence, while the others set out.  The deal is Deal's, in 32 bits: fewer items
+// than CTAs, of at most 2^23 blocks.
 __device__ __forceinline__ bool find_run_small(const AttendArgs& a, Control* c, Walk& w) {
   const int lane = threadIdx.x & 31;
   const Seq s = lane < a.b.n ? load_seq(a, lane) : Seq{0, 0, 0};
   const Cost mine = cost_of(a, s);
-  Cost sum = mine;
-  warp_sum(sum);
-  const Deal d(a, sum);
-  if (d.lo() >= d.total) return false;
-  const int64_t v = (d.whole ? (int64_t)mine.items * d.longest : mine.blocks) * a.hkv;
-  const int64_t before = warp_scan(v) - v;
-  if (before <= d.lo() && d.lo() < before + v) {
-    c->start = place(a, d, lane, s, before, v);
-    c->per = d.per;
+  const int own = (int)mine.blocks;
+  const int total = __reduce_add_sync(0xffffffffu, own) * a.hkv, items = __reduce_add_sync(0xffffffffu, mine.items) * a.hkv;
+  const int longest = __reduce_max_sync(0xffffffffu, mine.longest), grid = (int)gridDim.x;
+  int per = (uint32_t)(total + grid - 1) / (uint32_t)grid;
+  const bool whole = longest <= per + kSplit;
+  if (!whole) per = max(per, least_part(a, longest));
+  // Counted in items where they stay whole, else in blocks.
+  const int head = whole ? mine.items : own, v = head * a.hkv;
+  const int lo = whole ? (int)blockIdx.x : per * (int)blockIdx.x;
+  if (lo >= (whole ? items : total)) return false;
+  int before = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += t;
+  }
+  before -= v;
+  if (before <= lo && lo < before + v) {
+    const int h = (uint32_t)(lo - before) / (uint32_t)head;
+    int rest = lo - before - h * head, t = 0;
+    if (whole) {
+      t = rest;
+      rest = 0;
+    } else {
+#pragma unroll 1
+      for (int cost; rest >= (cost = item_cost(a, s, t)); ++t) rest -= cost;
+    }
+    c->start = Walk{lane, h, t, rest, whole ? longest : 0, 0, 0, 0, whole ? longest : min(per, total - lo),
+                    whole ? (int64_t)longest * lo : lo, s};
+    c->per = whole ? longest : per;
   }
   __syncwarp();
   w = c->start;
