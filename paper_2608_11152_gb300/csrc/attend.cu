@@ -944,7 +944,9 @@ struct Softmax {
   }
 
   // Results of a tile, or its partial sums.  join: O, m and l of stream 1 belong to the same rows.
-  __device__ __forceinline__ void finish(const Segment& g, int t0, int rows, bool join, float m, float l) {
+  // out: the row's first element.
+  __device__ __forceinline__ void finish(const Segment& g, int t0, int rows, bool join, float m, float l, T* out) {
+    const bool whole = g.whole;
     float w0 = 1.f, w1 = 0.f;
     if (join) {
       const float2 o = c->ml[row];
@@ -956,13 +958,15 @@ struct Softmax {
     }
     const bool mine = row < rows;
     const int warp_rows = rows - (row & ~31);
-    const int slot = g.whole ? 0 : (int)((blockIdx.x * 2 + (g.first >= c->per * blockIdx.x)) * 2 + st);
-    if (g.whole) {
+    int slot = 0;
+    if (!whole) slot = (blockIdx.x * 2 + (g.first >= c->per * blockIdx.x)) * 2 + st;
+    if (whole) {
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
       w0 *= inv;
       w1 *= inv;
     }
-    T* out = mine ? out_row(g, t0, row) : nullptr;
+    const int d = a.d;
+    const bool vec32 = a.vec32;
     if (warp_rows > 0) {
 #pragma unroll 1
       for (int q = 0; q < DP; q += 16) {
@@ -977,15 +981,15 @@ struct Softmax {
           if (join) x[i / 8][i % 8] += __uint_as_float(o1[i]) * w1;
         }
         if (!mine) continue;
-        if (g.whole) {
-          if (a.vec32 && q + 16 <= a.d) {
+        if (whole) {
+          if (vec32 && q + 16 <= d) {
             store32(out + q, pack16<T>(x[0][0], x[0][1]), pack16<T>(x[0][2], x[0][3]), pack16<T>(x[0][4], x[0][5]),
                     pack16<T>(x[0][6], x[0][7]), pack16<T>(x[1][0], x[1][1]), pack16<T>(x[1][2], x[1][3]),
                     pack16<T>(x[1][4], x[1][5]), pack16<T>(x[1][6], x[1][7]));
           } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-              if (q + e * 8 < a.d) put8(out + q + e * 8, x[e]);
+              if (q + e * 8 < d) put8(out + q + e * 8, x[e]);
           }
         } else {
           float4* p = a.ws_o + ((int64_t)slot * (DP / 4) + q / 4) * kTile + row;
@@ -997,7 +1001,7 @@ struct Softmax {
       }
     }
     if (mine) {
-      if (g.whole) put_lse(g, t0, row, m, l);
+      if (whole) put_lse(g, t0, row, m, l);
       else a.ws_ml[slot * kTile + row] = make_float2(m, l);
     }
   }
@@ -1116,6 +1120,7 @@ struct Softmax {
         if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->p_full[st]));
       }
       const bool join = !g.both() && g.nb > 1;
+      T* out = row < rows ? out_row(g, t0, row) : nullptr;  // (while the last product runs)
       if (nb > 0) {
         if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase, &c->abort)) return;
         o_phase ^= 1;
@@ -1137,7 +1142,7 @@ struct Softmax {
       }
       if (st == 0 && (join || g.both())) o1_phase ^= 1;
       tc_fence_after();
-      finish(g, t0, rows, join, m, l);
+      finish(g, t0, rows, join, m, l, out);
       tc_fence_before();
       if (join) {
         __syncwarp();
