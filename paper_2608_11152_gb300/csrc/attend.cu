@@ -1096,15 +1096,16 @@ struct Softmax {
       const int p1 = p0 + min(a.tok, g.nt - t0) - 1;     // and of its last
       const int pos = row < rows ? p0 + row / a.group : -1;
       float m = -INFINITY, l = 0.f;
-      const int nb = g.stream_blocks(st);
-      for (int i = 0; i < nb; ++i) {
-        const int k0 = (g.j0 + (g.both() ? i : 2 * i + st)) * kKeys;
+      const bool both = g.both(), join = !both && g.nb > 1;
+      const int nb = g.stream_blocks(st), window = a.window;
+      int k0 = (g.j0 + (both ? 0 : st)) * kKeys;  // first key of the stream's next block
+      for (int i = 0; i < nb; ++i, k0 += both ? kKeys : 2 * kKeys) {
         if (!mbar_wait(smem_u32(&c->s_full[st]), s_phase, &c->abort)) return;
         s_phase ^= 1;
         if (active) {
           tc_fence_after();
-          const bool mask = k0 + kKeys > p0 + 1 || (a.window > 0 && p1 - k0 >= a.window);
-          const int hi = max(pos + 1 - k0, 0), lo = a.window > 0 && pos - k0 >= a.window ? pos - k0 - a.window + 1 : 0;
+          const bool mask = k0 + kKeys > p0 + 1 || (window > 0 && p1 - k0 >= window);
+          const int hi = max(pos + 1 - k0, 0), lo = window > 0 && pos - k0 >= window ? pos - k0 - window + 1 : 0;
           block(lo, hi, mask, i == 0, m, l);
           tc_wait_st();
           tc_fence_before();
@@ -1119,7 +1120,6 @@ struct Softmax {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->p_full[st]));
       }
-      const bool join = !g.both() && g.nb > 1;
       T* out = row < rows ? out_row(g, t0, row) : nullptr;  // (while the last product runs)
       if (nb > 0) {
         if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase, &c->abort)) return;
@@ -1133,14 +1133,14 @@ struct Softmax {
         joined = true;
         continue;
       }
-      if (st == 1 && !g.both()) continue;
+      if (st == 1 && !both) continue;
       if (join) {
         // In this order: o_full[1] may be a phase behind until stream 1 says that its item is done.
         if (!mbar_wait(smem_u32(&c->ml_full), ml_phase, &c->abort)) return;
         if (!mbar_wait(smem_u32(&c->o_full[1]), o1_phase, &c->abort)) return;
         ml_phase ^= 1;
       }
-      if (st == 0 && (join || g.both())) o1_phase ^= 1;
+      if (st == 0 && (join || both)) o1_phase ^= 1;
       tc_fence_after();
       finish(g, t0, rows, join, m, l, out);
       tc_fence_before();
