@@ -1272,12 +1272,15 @@ int attend_prepare(misat_kv* kv) {
   const int rc = dp == 128 ? (bf ? allow_smem<__nv_bfloat16, 128>() : allow_smem<__half, 128>())
                            : (bf ? allow_smem<__nv_bfloat16, 64>() : allow_smem<__half, 64>());
   if (rc != MISAT_OK) return rc;
-  const size_t slots = (size_t)kv->num_sms * 4;
-  if (cudaMalloc(&kv->ws_o, slots * dp * kTile * sizeof(float)) != cudaSuccess ||
-      cudaMalloc(&kv->ws_ml, slots * kTile * sizeof(float2)) != cudaSuccess ||
-      cudaMalloc(&kv->ctr, kv->num_sms * 2 * sizeof(unsigned)) != cudaSuccess)
-    return MISAT_ERR_OOM;
-  return cudaMemset(kv->ctr, 0, kv->num_sms * 2 * sizeof(unsigned)) == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA;
+  // Error word and arrivals (zero between calls), statistics and sums of the parts: four slots a CTA.
+  const size_t slots = (size_t)kv->num_sms * 4, head = 256 + (kv->num_sms * 2 * sizeof(unsigned) + 255) / 256 * 256;
+  char* p = nullptr;
+  if (cudaMalloc(&p, head + slots * kTile * (sizeof(float2) + dp * sizeof(float))) != cudaSuccess) return MISAT_ERR_OOM;
+  kv->err = reinterpret_cast<int32_t*>(p);
+  kv->ctr = reinterpret_cast<unsigned*>(p + 256);
+  kv->ws_ml = reinterpret_cast<float2*>(p + head);
+  kv->ws_o = reinterpret_cast<float4*>(p + head + slots * kTile * sizeof(float2));
+  return cudaMemset(p, 0, head) == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA;
 }
 
 void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,

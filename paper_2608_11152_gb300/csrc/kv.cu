@@ -37,10 +37,6 @@ int misat_kv_create(const misat_kv_config* c, misat_kv** out) {
   int rc = MISAT_OK;
   if (cudaDeviceGetAttribute(&kv->num_sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
     rc = MISAT_ERR_CUDA;
-  else if (cudaMalloc(&kv->err, sizeof(int32_t)) != cudaSuccess)
-    rc = MISAT_ERR_OOM;
-  else if (cudaMemset(kv->err, 0, sizeof(int32_t)) != cudaSuccess)
-    rc = MISAT_ERR_CUDA;
   if (rc == MISAT_OK) rc = attend_prepare(kv);
   if (rc == MISAT_OK && cudaDeviceSynchronize() != cudaSuccess) rc = MISAT_ERR_CUDA;
   if (rc != MISAT_OK) {
@@ -54,10 +50,7 @@ int misat_kv_create(const misat_kv_config* c, misat_kv** out) {
 
 int misat_kv_destroy(misat_kv* kv) {
   if (!kv) return MISAT_ERR_INVALID_ARG;
-  cudaFree(kv->err);
-  cudaFree(kv->ws_o);
-  cudaFree(kv->ws_ml);
-  cudaFree(kv->ctr);
+  cudaFree(kv->err);  // with the workspace behind it
   delete kv;
   return MISAT_OK;
 }
@@ -66,8 +59,8 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
                     int64_t o_ts, int64_t o_hs, float* lse, int32_t window, void* cuda_stream) {
   if (!batch_ok(kv, batch) || window < 0) return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
-  if (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) || (reinterpret_cast<uintptr_t>(lse) & 3) ||
-      !on_device(kv->device))
+  if (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3) || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
   launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, window,
                 static_cast<cudaStream_t>(cuda_stream));

@@ -25,13 +25,13 @@ struct misat_kv {
   const misat_rope* rope;
   void* kb;
   void* vb;
-  int32_t* err;  // device, sticky
   // of the attention kernel: maps of the blocks, partial sums of split items, their arrivals
   decltype(&cuTensorMapEncodeTiled) encode;
   CUtensorMap map_k, map_v;
   float4* ws_o;
   float2* ws_ml;
   unsigned* ctr;
+  int32_t* err;  // sticky; in front of the workspace above, which is one allocation with it
 };
 
 namespace misat {
@@ -85,7 +85,7 @@ inline bool on_device(int device) {
 // Return code of the launches just made.
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA; }
 
-// Maps and workspace of the attention kernel; MISAT_OK or an error code.
+// Maps of the attention kernel, and the pool's device memory; MISAT_OK or an error code.
 int attend_prepare(misat_kv* kv);
 void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,
                    cudaStream_t st);
