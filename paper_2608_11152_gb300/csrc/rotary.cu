@@ -6,7 +6,12 @@
 // one vector past the rotated part), in the interleaved layout one vector of whole pairs -- of one
 // token, takes the unit's cosines and sines to registers, and goes through heads of the token with
 // them: all heads share the angles, so the trigonometry and the reads of shared memory are a
-// fraction of an item, and the next head is one addition away.
+// fraction of an item, and the next head is one addition away.  Elements are turned in 32 bits and rounded
+// once.
+//
+// Bound by memory: 65,536 tokens x 32 heads of 128 in bf16 take 175 us for 1.07 GB (6.1 TB/s, 0.90 of a
+// plain copy), the append of 70,000 tokens with 32 + 2 x 8 heads 289 us for 1.75 GB.  One head in flight
+// per thread and five CTAs on an SM: four heads in flight with three CTAs took 255 us for the former.
 #include <cmath>
 #include <new>
 

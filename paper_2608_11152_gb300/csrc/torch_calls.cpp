@@ -241,7 +241,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   at::Tensor q, out;
   if (has_q) {
     q = heads(a[4], "q", p->dtype, p->device, T, p->hq, p->d);
-    out = given ? heads(a[5], "q_out", p->dtype, p->device, T, p->hq, p->d) : fresh({T, p->hq, p->d}, p->dtype, p->device);
+    out = given ? heads(a[5], "q_out", p->dtype, p->device, T, p->hq, p->d)
+                : fresh({T, p->hq, p->d}, p->dtype, p->device);
   }
   const int rc = misat_kv_append(p->h, &b->b, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                                  v.stride(1), has_q ? q.data_ptr() : nullptr, has_q ? q.stride(0) : 0,
@@ -304,7 +305,8 @@ PyObject* sync(PyObject*, PyObject* c) {
   MISAT_END
 }
 
-#define MISAT_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+#define MISAT_FAST(name) \
+  {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"init", init, METH_O, nullptr},
                          MISAT_FAST(rope_state),
                          MISAT_FAST(pool_state),

@@ -152,7 +152,8 @@ def test_rotary_gradient_against_differences():
 def test_rotary_positions_far_out_and_negative():
     m = misat()
     x = rand((6, 2, 64), F32, 1)
-    pos = torch.tensor([2 ** 31 - 1, -(2 ** 31), -1, 123456789, 1 << 24, (1 << 24) + 1], device="cuda", dtype=torch.int32)
+    far = [2 ** 31 - 1, -(2 ** 31), -1, 123456789, 1 << 24, (1 << 24) + 1]
+    pos = torch.tensor(far, device="cuda", dtype=torch.int32)
     y, tol = ref.rotate(x, pos, ref.frequencies(64), True)
     # the 64-bit angle of the definition itself is only good to 2^31 * 2^-53 radians
     ref.assert_within("rotate", m.Rope(64).rotate(x, pos), y, tol + 2.0 ** -21 * x.double().abs().cpu().amax())
