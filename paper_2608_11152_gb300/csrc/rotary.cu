@@ -11,7 +11,8 @@
 //
 // Bound by memory: 65,536 tokens x 32 heads of 128 in bf16 take 175 us for 1.07 GB (6.1 TB/s, 0.90 of a
 // plain copy), the append of 70,000 tokens with 32 + 2 x 8 heads 289 us for 1.75 GB.  One head in flight
-// per thread and five CTAs on an SM: four heads in flight with three CTAs took 255 us for the former.
+// per thread and five CTAs on an SM: four heads in flight with three CTAs took 297 us for the former, two
+// with three 231 us.
 #include <cmath>
 #include <new>
 
