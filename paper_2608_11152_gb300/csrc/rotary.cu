@@ -161,12 +161,19 @@ __global__ void __launch_bounds__(kThreads, HALF ? 5 : 7) k_rotate(const __grid_
           hi.e[e] = from_f<T>(x * cs[e].y + y * cs[e].x);
         }
       } else {
+        auto pairs = [&](bool ends) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {  // past the rotated part a pair meets cos 1 and sin 0
-          const float x = to_f(lo.e[2 * e]), y = to_f(lo.e[2 * e + 1]);
-          lo.e[2 * e] = from_f<T>(x * cs[e].x - y * cs[e].y);
-          lo.e[2 * e + 1] = from_f<T>(x * cs[e].y + y * cs[e].x);
-        }
+          for (int e = 0; e < N; ++e) {
+            if (ends && el + 2 * e >= a.rot) continue;
+            const float x = to_f(lo.e[2 * e]), y = to_f(lo.e[2 * e + 1]);
+            lo.e[2 * e] = from_f<T>(x * cs[e].x - y * cs[e].y);
+            lo.e[2 * e + 1] = from_f<T>(x * cs[e].y + y * cs[e].x);
+          }
+        };
+        // A vector in which the rotated part ends keeps the rest as it is: x * 1 - y * 0 is NaN where y is
+        // infinite.  The test in every vector took 315 us instead of 308 (append of 28 + 8 heads of 64).
+        if (el + W <= a.rot) pairs(false);
+        else pairs(true);
       }
     }
     *reinterpret_cast<V*>(o + el) = lo;

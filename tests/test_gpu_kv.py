@@ -159,6 +159,23 @@ def test_rotary_positions_far_out_and_negative():
     ref.assert_within("rotate", m.Rope(64).rotate(x, pos), y, tol + 2.0 ** -21 * x.double().abs().cpu().amax())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("d,rot,half", [(24, 10, False), (24, 10, True), (72, 34, False), (96, 48, False),
+                                        (16, 2, False)])
+def test_rotary_copies_the_rest_bit_for_bit(d, rot, half, dtype):
+    m = misat()
+    rope = m.Rope(rot, layout=m.ROPE_HALF if half else m.ROPE_INTERLEAVED, attn_factor=1.25)
+    pos = torch.arange(9, device="cuda", dtype=torch.int32) * 1001
+    x = rand((9, 3, d), dtype, 3)
+    odd = torch.tensor([float("inf"), -0.0, float("nan"), 1.5, -float("inf"), -1.0, 0.0], dtype=dtype, device="cuda")
+    n = 9 * 3 * (d - rot)
+    x[..., rot:] = odd[torch.arange(n, device="cuda") % 7].view(9, 3, d - rot)
+    bits = torch.int32 if dtype == F32 else torch.int16
+    for y in (rope.rotate(x, pos), rope.backward(x, pos)):
+        assert torch.equal(y[..., rot:].contiguous().view(bits), x[..., rot:].contiguous().view(bits))
+        assert y[..., :rot].isfinite().all()
+
+
 def test_rotary_empty():
     m = misat()
     rope = m.Rope(16)
