@@ -547,7 +547,7 @@ typedef struct misat_kv_batch {
   int32_t n;                  /* sequences, 0..max_batch */
   int32_t n_tokens;           /* q_off[n] */
   int32_t max_q;              /* at least the new tokens of any sequence */
-  const int32_t* q_off;       /* [n+1], q_off[0] = 0, non-decreasing */
+  const int32_t* q_off;       /* [n+1], from 0 to n_tokens, non-decreasing */
   const int32_t* kv_len;      /* [n] tokens of the sequence, the new ones included; at most 2^30 */
   const int32_t* block_table; /* [n][table_stride] */
   int64_t table_stride;       /* blocks per row, kv_len <= 16 table_stride */

@@ -1204,6 +1204,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = c->tmem;
   chain_wait();
+  // Tokens before the first sequence and behind the last are in none: their rows are not written.
+  if (blockIdx.x == 0 && threadIdx.x == 256 && (__ldcg(a.b.q_off) != 0 || __ldcg(a.b.q_off + a.b.n) != a.b.n_tokens))
+    set_error(a.err, MISAT_ERR_INVALID_ARG);
   Walk w;
   if (a.small || find_run(a, c, reinterpret_cast<Seq*>(smem + L::kKv), w)) {
     if (warp < 8) {

@@ -447,6 +447,28 @@ def test_attend_malformed_is_a_sticky_error():
         pool.sync()
 
 
+@pytest.mark.parametrize("n", [3, 40])
+@pytest.mark.parametrize("skip", ["front", "back", "all"])
+def test_attend_tokens_of_no_sequence_are_a_sticky_error(skip, n):
+    m = misat()
+    s = Step([(1, 20)] * n, 2, 64, BF16)
+    pool = s.pool(4)
+    q = rand((n, 4, 64), BF16, 1)
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    if skip == "front":
+        off[0] = 1
+    elif skip == "back":
+        off[n] = n - 1
+    else:
+        off.zero_()
+    lens = torch.full((n,), 21, dtype=torch.int32, device="cuda")
+    pool.attend(pool.batch(off, lens, s.table.cuda(), n_tokens=n, max_q=1), q)
+    with pytest.raises(m.MisatError) as e:
+        pool.sync()
+    assert e.value.code == m.ERR_INVALID_ARG
+    pool.sync()
+
+
 def test_calls_on_other_streams_and_in_a_graph():
     m = misat()
     s = Step([(1, 3000), (40, 200)], 2, 64, BF16)
