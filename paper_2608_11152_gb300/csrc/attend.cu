@@ -188,8 +188,12 @@ struct Walk {
       if (++h == a.hkv) {
         h = 0;
         do {
+          if (b + 1 >= a.b.n) {  // fewer blocks than were counted: the lengths changed under the call
+            left = 0;
+            break;
+          }
           s = load_seq(a, ++b);
-        } while (s.n == 0 && b + 1 < a.b.n);
+        } while (s.n == 0);
       }
     }
     return true;
@@ -259,9 +263,9 @@ constexpr int kReaders = 11;  // 8 softmax warps, keys and values, matrix instru
 struct Feed {
   Control* c;
   Ring ring;
-  // The next part, or nullptr: the end, or gave up.
+  // The next part, or nullptr: the end, or gave up.  (It may wait for a reader that is an item behind.)
   __device__ __forceinline__ const Segment* next() {
-    if (!mbar_wait(smem_u32(&c->seg_full[ring.at]), ring.phase, &c->abort)) return nullptr;
+    if (!mbar_wait(smem_u32(&c->seg_full[ring.at]), ring.phase, &c->abort, kItemLimit)) return nullptr;
     const Segment* g = &c->seg[ring.at];
     return g->nb < 0 ? nullptr : g;
   }
@@ -497,9 +501,10 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
     w.locate(a, c->before);
     return true;
   }
+  if (tid == 0) c->start.left = 0;
   int64_t base = 0;
 #pragma unroll 1
-  for (int b0 = 0; base <= lo; b0 += kThreads) {
+  for (int b0 = 0; base <= lo && b0 < a.b.n; b0 += kThreads) {
     const Seq s = b0 == 0 ? mine : b0 + tid < a.b.n ? load_seq(a, b0 + tid) : Seq{0, 0, 0};
     const int64_t v =
         (d.whole ? (int64_t)n_items(a, s) * d.longest : b0 == 0 ? first.blocks : cost_of(a, s).blocks) * a.hkv;
@@ -1290,6 +1295,7 @@ int attend_prepare(misat_kv* kv) {
   if (cudaMalloc(&p, head + slots * kTile * (sizeof(float2) + dp * sizeof(float))) != cudaSuccess) return MISAT_ERR_OOM;
   kv->err = reinterpret_cast<int32_t*>(p);
   kv->ctr = reinterpret_cast<unsigned*>(p + 256);
+  kv->head = head;
   kv->ws_ml = reinterpret_cast<float2*>(p + head);
   kv->ws_o = reinterpret_cast<float4*>(p + head + slots * kTile * sizeof(float2));
   return cudaMemset(p, 0, head) == cudaSuccess ? MISAT_OK : MISAT_ERR_CUDA;

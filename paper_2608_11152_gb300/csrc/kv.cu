@@ -74,7 +74,9 @@ int misat_kv_sync(misat_kv* kv, void* cuda_stream) {
   if (cudaMemcpyAsync(&err, kv->err, sizeof(err), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
       cudaStreamSynchronize(st) != cudaSuccess)
     return MISAT_ERR_CUDA;
-  if (err && (cudaMemsetAsync(kv->err, 0, sizeof(err), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+  // A call that gave up inside leaves arrivals of its parts behind; they are cleared with the error.
+  const size_t bytes = err == MISAT_ERR_INTERNAL ? kv->head : sizeof(err);
+  if (err && (cudaMemsetAsync(kv->err, 0, bytes, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
     return MISAT_ERR_CUDA;
   return err;
 }

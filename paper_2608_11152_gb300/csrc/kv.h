@@ -31,6 +31,7 @@ struct misat_kv {
   float4* ws_o;
   float2* ws_ml;
   unsigned* ctr;
+  size_t head;   // bytes of the error word and the arrivals
   int32_t* err;  // sticky; in front of the workspace above, which is one allocation with it
 };
 

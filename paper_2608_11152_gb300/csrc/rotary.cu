@@ -260,7 +260,7 @@ void launch_rotate_t(RotArgs& a, int layout, int num_sms, cudaStream_t st) {
   a.heads_per_cta = hpc;
   a.unit_threads.set(unit_threads);
   a.groups.set(groups);
-  const dim3 grid((a.n_tokens + tok - 1) / tok, (heads + hpc - 1) / hpc);
+  const dim3 grid((a.n_tokens - 1) / tok + 1, (heads - 1) / hpc + 1);
   const size_t smem = sizeof(float2) * tok * (a.rot / 2);
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;

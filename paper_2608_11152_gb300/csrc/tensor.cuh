@@ -29,21 +29,19 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Waits for the phase of the given parity, for at most `limit` times kWaitCycles (about a second): returns false
-// then, or when another warp of the CTA has given up (*abort).  The caller leaves its role; the
+// Waits for the phase of the given parity, for at most `limit` times kWaitTicks of 64 cycles (about a second):
+// returns false then, or when another warp of the CTA has given up (*abort).  The caller leaves its role; the
 // kernel ends in order with an error recorded.  mbar_wait: a whole warp, with one result.
-constexpr uint32_t kWaitCycles = 2000000000u;
+constexpr uint32_t kWaitTicks = 2000000000u / 64;
+__device__ __forceinline__ uint32_t ticks() { return (uint32_t)(clock64() >> 6); }
 __device__ __forceinline__ bool mbar_wait_one(uint32_t bar, uint32_t parity, volatile int* abort, int limit = 1) {
   if (mbar_try(bar, parity)) return true;
-  uint32_t t0 = (uint32_t)clock();
+  const uint32_t t0 = ticks();
   while (!mbar_try(bar, parity)) {
     if (*abort) return false;
-    if ((uint32_t)clock() - t0 > kWaitCycles) {
-      if (--limit == 0) {
-        *abort = 1;
-        return false;
-      }
-      t0 = (uint32_t)clock();
+    if (ticks() - t0 > (uint32_t)limit * kWaitTicks) {
+      *abort = 1;
+      return false;
     }
   }
   return true;

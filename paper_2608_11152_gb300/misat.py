@@ -563,7 +563,8 @@ def _torch_calls():
 
 
 class Rope:
-    """Rotary position embedding on the current CUDA device (misat_rope_*, misat_rotary)."""
+    """Rotary position embedding on the current CUDA device (misat_rope_*, misat_rotary).  Autograd does not
+    record these calls: backward() is the gradient."""
 
     def __init__(self, rot_dim, *, base=10000.0, layout=ROPE_HALF, scaling=ROPE_SCALE_NONE, factor=1.0, orig_len=0.0,
                  beta_slow=1.0, beta_fast=32.0, attn_factor=1.0):
