@@ -12,9 +12,9 @@
 // multiply (the matrix instruction takes one type); l adds them unrounded.  The result is rounded once.
 //
 // What bounds it, and what it does: a step of single tokens reads the cache once, at 7.0 TB/s (256 sequences
-// of 512 to 16,000 tokens, 8 kv heads of 128: 1.19 to 1.23 ms for 8.4 GB); a chunk is the products and the chain of scores,
-// exponentials and product of each stream, at 1,260 to 1,440 TFLOP/s of 1,887 (2,048 tokens over
-// 129,024, 32 heads: 3.03 to 3.45 ms on different GPUs, power-capped at some 1.55 GHz).
+// of 512 to 16,000 tokens, 8 kv heads of 128: 1.19 to 1.23 ms for 8.4 GB); a chunk is the products and the
+// chain of scores, exponentials and product of each stream, at 1,260 to 1,440 TFLOP/s of 1,887 (2,048 tokens
+// over 129,024, 32 heads: 3.03 to 3.45 ms on different GPUs, power-capped at some 1.55 GHz).
 //
 // Two streams of such tiles share a CTA, so that one's matrix products run under the other's
 // exponentials.  An item of more than 128 rows gives each stream half of its rows, and both read the same
