@@ -573,7 +573,9 @@ int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, in
  * h / (n_q_heads / n_kv_heads):
  *   out = sum_j softmax_j(scale q.k_j) v_j,   lse = log sum_j exp(scale q.k_j)
  * lse is optional, [n_tokens][n_q_heads] 32-bit.  Scores, maxima, sums and the output's sum
- * are held in 32 bits; the weights are rounded to the pool's dtype for the product with v.
+ * are held in 32 bits; the weights are rounded to the pool's dtype for the product with v.  (In
+ * float16 a weight keeps its 11 bits down to 2^-25 of the row's largest, and one below that is off
+ * by at most 2^-36 of the largest.)
  * A token that sees no key (a position below zero) gets zeros, and -infinity in lse.  Slots
  * past kv_len are never used, whatever they hold; a key that only some new tokens of a
  * sequence see has to be finite for all of them (0 times infinity is NaN).
