@@ -576,9 +576,10 @@ int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, in
  * are held in 32 bits; the weights are rounded to the pool's dtype for the product with v.  (In
  * float16 a weight keeps its 11 bits down to 2^-25 of the row's largest, and one below that is off
  * by at most 2^-36 of the largest.)
- * A token that sees no key (a position below zero) gets zeros, and -infinity in lse.  Slots
- * past kv_len are never used, whatever they hold; a key that only some new tokens of a
- * sequence see has to be finite for all of them (0 times infinity is NaN).
+ * A token that sees no key (a position below zero) gets zeros, and -infinity in lse; one whose
+ * scores are all -infinity gets NaN (0 / 0), and -infinity in lse; a score of +infinity or NaN makes
+ * both NaN.  Slots past kv_len are never used, whatever they hold; a key that only some new tokens
+ * of a sequence see has to be finite for all of them (0 times infinity is NaN).
  * The result does not depend on timing: the same call gives the same bits.  [async]
  * Errors: INVALID_ARG, CUDA; INVALID_ARG later (see above; what the skipped sequences' rows
  * of out and lse then hold is not specified). */

@@ -947,6 +947,9 @@ struct Softmax {
     return ok;
   }
 
+  __device__ __forceinline__ int position(const Segment& g, int t0, int r) const {
+    return g.s.len - g.s.n + g.t0 + t0 + r / a.group;
+  }
   __device__ __forceinline__ T* out_row(const Segment& g, int t0, int r) const {
     const int t = r / a.group;
     return static_cast<T*>(a.out.p) + (int64_t)(g.s.begin + g.t0 + t0 + t) * a.out.ts +
@@ -973,8 +976,10 @@ struct Softmax {
   }
 
   // Results of a tile, or its partial sums.  join: O, m and l of stream 1 belong to the same rows.
+  // seen: the row sees a key (where it does and l is zero all its scores are -infinity, and 0 / 0 is the result).
   // out: the row's first element.
-  __device__ __forceinline__ void finish(const Segment& g, int t0, int rows, bool join, float m, float l, T* out) {
+  __device__ __forceinline__ void finish(const Segment& g, int t0, int rows, bool join, bool seen, float m, float l,
+                                         T* out) {
     const bool whole = g.whole;
     float w0 = 1.f, w1 = 0.f;
     if (join) {
@@ -990,7 +995,7 @@ struct Softmax {
     int slot = 0;
     if (!whole) slot = (blockIdx.x * 2 + (g.first >= c->per * blockIdx.x)) * 2 + st;
     if (whole) {
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      const float inv = seen ? 1.f / l : 0.f;
       w0 *= inv;
       w1 *= inv;
     }
@@ -1096,7 +1101,7 @@ struct Softmax {
         }
         top = next;
       }
-      const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+      const float inv = position(g, t0, r) >= 0 ? 1.f / sum : 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] *= inv;
       put8(out_row(g, t0, r) + g8 * 8, x);
@@ -1171,7 +1176,7 @@ struct Softmax {
       }
       if (st == 0 && (join || both)) o1_phase ^= 1;
       tc_fence_after();
-      finish(g, t0, rows, join, m, l, out);
+      finish(g, t0, rows, join, pos >= 0, m, l, out);
       tc_fence_before();
       if (join) {
         __syncwarp();

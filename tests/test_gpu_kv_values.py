@@ -60,3 +60,68 @@ def test_attend_maxima_that_move_in_float16(order):
     pool.sync()
     ref.assert_within("out", out, want[0], want[1] + L * F16_STEP * s.vb.nan_to_num().abs().max().item())
     ref.assert_within("lse", lse, want[2], want[3])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,L", [(1, 30), (3, 300), (1, 5000), (150, 400)])
+def test_attend_infinite_and_nan_values_that_are_seen(n, L, dtype):
+    """The definition's infinities and NaN: in the rows that see them, and in no other."""
+    d, hq = 64, 4
+    inf, nan = float("inf"), float("nan")
+    s = Step([(n, L), (2, 40)], 1, d, dtype)
+    q = rand((s.T, hq, d), dtype, 3)
+    pool = s.pool(hq)
+
+    def call(q):
+        out, lse = pool.attend(s.batch(pool), q, return_lse=True)
+        pool.sync()
+        return out, lse
+
+    good, good_lse = call(q)
+    # every score of a row is minus infinity: 0 / 0 in each element, and minus infinity as the sum's logarithm
+    x = q.clone()
+    s.kb[..., 5] = s.kb[..., 5].abs() + 1
+    good, good_lse = call(q)
+    x[0, 1, 5] = -inf
+    out, lse = call(x)
+    assert out[0, 1].isnan().all() and lse[0, 1].item() == -inf
+    keep = torch.ones((s.T, hq), dtype=torch.bool, device="cuda")
+    keep[0, 1] = False
+    assert torch.equal(out[keep], good[keep]) and torch.equal(lse[keep], good_lse[keep])
+    # a score of plus infinity, and a NaN in a query
+    for bad in (inf, nan):
+        x = q.clone()
+        x[0, 1, 5] = bad
+        out, lse = call(x)
+        assert out[0, 1].isnan().all() and not lse[0, 1].isfinite()
+        assert torch.equal(out[keep], good[keep]) and torch.equal(lse[keep], good_lse[keep])
+    # one key that scores minus infinity takes no weight: as if it were not there
+    p = L // 2
+    at = (int(s.table[0, p // 16]), 0, p % 16)
+    kept = s.kb[at].clone()
+    x = q.clone()
+    x[:n, :, 7] = 1
+    s.kb[at][7] = -inf
+    out, lse = call(x)
+    key = ref.gather(s.kb, s.table[0], L)[:, 0].double()
+    val = ref.gather(s.vb, s.table[0], L)[:, 0].double()
+    see = torch.arange(L, device="cuda")[None] <= torch.arange(L - n, L, device="cuda")[:, None]
+    z = torch.einsum("nhd,ld->nhl", x[:n].double(), key) / d ** 0.5
+    z = torch.where(see[:, None], z, -inf).softmax(-1)
+    u = ref.U[dtype]
+    want = torch.einsum("nhl,ld->nhd", z, val)
+    size = torch.einsum("nhl,ld->nhd", z, val.abs())
+    xa = torch.einsum("nhd,ld->nhl", x[:n].double().abs(), key.abs().nan_to_num(0, 0, 0)).amax(-1) / d ** 0.5
+    tol = u * (1 + 2.0 ** -10) * (size + want.abs()) + (
+        (L / 16 + 8) * 2.0 ** -23 + 2 * ((d + 16) * 2.0 ** -23 * xa[..., None] + 2.0 ** -20)) * size + ref.TINY[dtype]
+    ref.assert_within("out", out[:n], want, tol + L * F16_STEP * val.abs().max().item())
+    s.kb[at] = kept
+    # an infinite value that has weight
+    kept = s.vb[at].clone()
+    s.vb[at][9] = inf
+    out, _ = call(q)
+    rows = see[:, p]
+    assert (out[:n, :, 9][rows] == inf).all()
+    other = torch.arange(d, device="cuda") != 9
+    assert torch.equal(out[..., other], good[..., other])
+    s.vb[at] = kept
