@@ -25,7 +25,7 @@ CALLS = os.path.join(HERE, "_calls.so")
 CALLS_SOURCE = "torch_calls.cpp"
 SOURCES = ["api.cu", "hash.cu", "probe.cu", "route.cu", "select.cu", "commit.cu", "evict.cu", "gindex.cu",
            "overload.cu", "stage.cu", "rotary.cu", "kv.cu", "attend.cu"]
-HEADERS = ["common.cuh", "gindex.cuh", "kernels.h", "tick_scale.h", "kv.h", "tensor.cuh"]
+HEADERS = ["common.cuh", "gindex.cuh", "kernels.h", "tick_scale.h", "kv.h", "runs.cuh", "tensor.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
