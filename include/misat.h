@@ -477,7 +477,8 @@ int misat_recheck_delays(int32_t n, const uint64_t* group, const uint8_t* held, 
  *   - Whole numbers found malformed on the device (offsets out of order, a length beyond its
  *     block table, a block outside the pool) are sticky errors of the pool, returned by
  *     misat_kv_sync; the sequences concerned are skipped, and nothing outside the buffers
- *     passed is read or written. */
+ *     passed is read or written.  That holds too where offsets, lengths or tables change while a
+ *     call runs; what the call gives then is not specified. */
 #define MISAT_BF16 0
 #define MISAT_F16 1
 #define MISAT_F32 2

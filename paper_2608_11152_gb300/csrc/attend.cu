@@ -441,8 +441,8 @@ struct Softmax {
 
   // The item is split between CTAs c0..c1: the last of them to arrive adds the parts.
   __device__ __forceinline__ bool arrive(const Segment& g, int t0, int rows) {
-    const int64_t per = c->per;
-    const int c0 = (int)div_down(g.first, per), c1 = (int)div_down(g.last - 1, per);
+    const Parts parts = parts_of(a, g, c->per);
+    const int c0 = parts.first, c1 = parts.last;
     const int wt = threadIdx.x & 127;
     __threadfence();
     if (!wg_sync()) return false;

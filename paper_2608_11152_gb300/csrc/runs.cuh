@@ -31,6 +31,11 @@ struct AttendArgs {
 };
 
 // ---- what there is to do ----
+//
+// Lengths and offsets are read more than once, and a call whose lengths change while it runs still has to stay
+// inside the buffers.  Every read is checked by itself (load_seq); what was worked out from an earlier read (the
+// place of a run, the items before a sequence, the last CTA of an item) is checked against the later one where it is
+// used.  Such a call's run ends early, with an error recorded.
 
 struct Seq {
   int begin, n, len;  // first new token, new tokens, tokens in all
@@ -84,6 +89,32 @@ struct Segment {
   __device__ __forceinline__ int block(int step) const { return j0 + (both() ? step / 2 : step); }
 };
 
+// x / d.  Counts of blocks fit 31 bits but for the wildest batches; those take 63 steps instead of the
+// hundreds of instructions that a 64-bit division is at every place of use.
+__device__ __forceinline__ int64_t div_down(int64_t x, int64_t d) {
+  if ((x >> 31) == 0 && (d >> 31) == 0) return (uint32_t)x / (uint32_t)d;
+  uint64_t q = 0, r = 0;
+#pragma unroll 1
+  for (int i = 62; i >= 0; --i) {
+    r = r << 1 | ((uint64_t)x >> i & 1);
+    if (r >= (uint64_t)d) {
+      r -= (uint64_t)d;
+      q |= (uint64_t)1 << i;
+    }
+  }
+  return (int64_t)q;
+}
+
+// The CTAs that have parts of a split item, from the length of a run.
+struct Parts {
+  int first, last;
+};
+__device__ __forceinline__ Parts parts_of(const AttendArgs& a, const Segment& g, int64_t per) {
+  const int64_t last = div_down(g.last - 1, per);
+  if (last >= gridDim.x) set_error(a.err, MISAT_ERR_INVALID_ARG);  // more blocks than were counted
+  return {(int)div_down(g.first, per), (int)min(last, (int64_t)gridDim.x - 1)};
+}
+
 // The items in the order in which their blocks are dealt out.  Natural: by sequence, kv head, tile.
 // In columns (`cols` > 0): item i is in row i / cols and column i % cols of a table with as many rows as
 // a CTA has items, and the order is down the columns.  A CTA's run is about one column, so the CTAs work
@@ -102,6 +133,11 @@ struct Walk {
   int item, items;  // in columns: the item's number, all items
   int64_t left, at;
   Seq s;
+  // The lengths are not the ones that the run was worked out from.
+  __device__ __forceinline__ void stop(const AttendArgs& a) {
+    set_error(a.err, MISAT_ERR_INVALID_ARG);
+    left = 0;
+  }
   // In columns: the sequence, head and tile of the item, from the number of items before each sequence.
   __device__ __forceinline__ void locate(const AttendArgs& a, const int* before) {
     int lo = 0, hi = a.b.n;
@@ -113,9 +149,10 @@ struct Walk {
     }
     b = lo;
     s = load_seq(a, b);
-    const int tiles = n_items(a, s);
-    h = (item - before[b]) / tiles;
-    tile = item - before[b] - h * tiles;
+    const int tiles = n_items(a, s), i = item - before[b];
+    h = i / max(tiles, 1);
+    tile = i - h * tiles;
+    if (tiles == 0 || h >= a.hkv || off >= item_cost(a, s, tile)) stop(a);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a, const int* before, Segment& g) {
     if (left <= 0) return false;
@@ -147,15 +184,17 @@ struct Walk {
     }
     if (left <= 0) return true;
     if (cols > 0) {
-      item = item + cols < items ? item + cols : item % cols + 1;
-      locate(a, before);
+      const int next_row = item + cols, next_col = item % cols + 1;
+      item = next_row < items ? next_row : next_col;
+      if (next_row >= items && next_col == cols) stop(a);
+      else locate(a, before);
     } else if (++tile * 2 * a.tok >= s.n) {
       tile = 0;
       if (++h == a.hkv) {
         h = 0;
         do {
-          if (b + 1 >= a.b.n) {  // fewer blocks than were counted: the lengths changed under the call
-            left = 0;
+          if (b + 1 >= a.b.n) {  // fewer blocks than were counted
+            stop(a);
             break;
           }
           s = load_seq(a, ++b);
@@ -258,22 +297,6 @@ __device__ __forceinline__ void feed(const AttendArgs& a, Control* c, Walk w) {
 }
 
 // ---- the run of each CTA ----
-// x / d.  Counts of blocks fit 31 bits but for the wildest batches; those take 63 steps instead of the
-// hundreds of instructions that a 64-bit division is at every place of use.
-__device__ __forceinline__ int64_t div_down(int64_t x, int64_t d) {
-  if ((x >> 31) == 0 && (d >> 31) == 0) return (uint32_t)x / (uint32_t)d;
-  uint64_t q = 0, r = 0;
-#pragma unroll 1
-  for (int i = 62; i >= 0; --i) {
-    r = r << 1 | ((uint64_t)x >> i & 1);
-    if (r >= (uint64_t)d) {
-      r -= (uint64_t)d;
-      q |= (uint64_t)1 << i;
-    }
-  }
-  return (int64_t)q;
-}
-
 __device__ __forceinline__ Cost cost_of(const AttendArgs& a, const Seq& s) {
   Cost r{0, n_items(a, s), 0};
 #pragma unroll 1
@@ -375,7 +398,12 @@ __device__ __forceinline__ bool find_run_small(const AttendArgs& a, Control* c, 
     if (lane >= o) before += t;
   }
   before -= v;
-  if (before <= lo && lo < before + v) {
+  const bool mine_begins = before <= lo && lo < before + v;
+  if (!__any_sync(0xffffffffu, mine_begins)) {  // (offsets that overlap: sums beyond 32 bits)
+    set_error(a.err, MISAT_ERR_INVALID_ARG);
+    return false;
+  }
+  if (mine_begins) {
     const int h = (uint32_t)(lo - before) / (uint32_t)head;
     int rest = lo - before - h * head, t = 0;
     if (whole) {
@@ -483,7 +511,8 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, Control* c, Seq* s
   }
   __syncthreads();
   w = c->start;
-  return true;
+  if (w.left == 0 && tid == 0) set_error(a.err, MISAT_ERR_INVALID_ARG);  // fewer blocks than were counted
+  return w.left > 0;
 }
 
 // ---- keys and values ----
