@@ -588,8 +588,9 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
                     int64_t q_head_stride, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                     int32_t window, void* cuda_stream);
 
-/* Wait for the stream and return the pool's sticky device error (0 if none), then clear it.
- * [sync] */
+/* Wait for the stream and return the pool's sticky device error (0 if none), then clear it, and
+ * what a call that ended early left in the workspace (INTERNAL if there is some without an error).
+ * The pool's calls on other streams are to be finished.  [sync] */
 int misat_kv_sync(misat_kv* kv, void* cuda_stream);
 
 /* Wait for the stream and return the sticky device error (0 if none), then clear it and

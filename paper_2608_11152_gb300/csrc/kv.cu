@@ -1,5 +1,6 @@
 // Pools of KV blocks: the handle behind misat_kv_* and the checks of the attention call.
 #include <cmath>
+#include <memory>
 #include <new>
 
 #include "kv.h"
@@ -70,13 +71,18 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
 int misat_kv_sync(misat_kv* kv, void* cuda_stream) {
   if (!kv || !on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  int32_t err = 0;
-  if (cudaMemcpyAsync(&err, kv->err, sizeof(err), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+  // The error word, and the arrivals behind it: zero between calls, unless one gave up inside or saw lengths
+  // change, whatever error the word holds of an earlier call.
+  std::unique_ptr<int32_t[]> head(new (std::nothrow) int32_t[kv->head / sizeof(int32_t)]);
+  if (!head) return MISAT_ERR_OOM;
+  if (cudaMemcpyAsync(head.get(), kv->err, kv->head, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
       cudaStreamSynchronize(st) != cudaSuccess)
     return MISAT_ERR_CUDA;
-  // A call that gave up inside leaves arrivals of its parts behind; they are cleared with the error.
-  const size_t bytes = err == MISAT_ERR_INTERNAL ? kv->head : sizeof(err);
-  if (err && (cudaMemsetAsync(kv->err, 0, bytes, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+  const size_t arrivals = reinterpret_cast<char*>(kv->ctr) - reinterpret_cast<char*>(kv->err);
+  int32_t err = head[0];
+  for (size_t i = arrivals / sizeof(int32_t); err == 0 && i < kv->head / sizeof(int32_t); ++i)
+    if (head[i]) err = MISAT_ERR_INTERNAL;
+  if (err && (cudaMemsetAsync(kv->err, 0, kv->head, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
     return MISAT_ERR_CUDA;
   return err;
 }
