@@ -649,7 +649,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         is.run();
         is.drain();
       } else if (warp == 8) {
-        load_queries<T, DP>(a, &map_q, smem, c);
+        QueryLoader<DP> ql{a, &map_q, smem, c};
+        ql.run();
+        if (*(volatile int*)&c->abort) ql.drain();
       } else if (warp == 11) {
         if (a.small && !find_run_small(a, c, w)) w.left = 0;
         feed(a, c, w);

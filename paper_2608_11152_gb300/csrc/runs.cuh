@@ -602,46 +602,61 @@ struct QuerySlots {
   }
 };
 
-template <class T, int DP>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, const CUtensorMap* map, char* smem, Control* c) {
+template <int DP>
+struct QueryLoader {
   using L = Layout<DP>;
-  const int lane = threadIdx.x & 31;
-  QuerySlots qs;
-  Feed feed{c};
-  for (; const Segment* g = feed.next(); feed.done()) {
-    if (g->nb == 0) continue;
-    for (int st = 0; st < (g->both() ? 2 : 1); ++st) {
-      const int slot = qs.slot(*g, st);
-      const uint32_t full = smem_u32(&c->q_full[slot]);
-      if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort, kItemLimit)) return;
-      const int first = g->pair ? st * a.tok : 0;  // token of the item
-      const int token = g->s.begin + g->t0 + first, head = g->head(st) * a.group;
-      char* dst = smem + L::kQ + slot * L::kStage;
-      // Row r of a tile is token r / group and head r % group: the order of a box of heads and tokens.
-      if (a.map_q) {
-        if (elect_one()) {
-          mbar_expect(full, DP * 2 * a.group * a.tok);
-          for (int x = 0; x < DP; x += 64)
-            tma_load_3d(smem_u32(dst) + x / 64 * L::kHalf, map, full, x, head, token);
+  const AttendArgs& a;
+  const CUtensorMap* map;
+  char* smem;
+  Control* c;
+  uint32_t issued = 0;  // bit per tile: the parity of the copies issued to it
+
+  __device__ __forceinline__ void run() {
+    const int lane = threadIdx.x & 31;
+    QuerySlots qs;
+    Feed feed{c};
+    for (; const Segment* g = feed.next(); feed.done()) {
+      if (g->nb == 0) continue;
+      for (int st = 0; st < (g->both() ? 2 : 1); ++st) {
+        const int slot = qs.slot(*g, st);
+        const uint32_t full = smem_u32(&c->q_full[slot]);
+        if (!mbar_wait(smem_u32(&c->q_empty[slot]), qs.phase(slot) ^ 1, &c->abort, kItemLimit)) return;
+        const int first = g->pair ? st * a.tok : 0;  // token of the item
+        const int token = g->s.begin + g->t0 + first, head = g->head(st) * a.group;
+        char* dst = smem + L::kQ + slot * L::kStage;
+        issued ^= 1u << slot;
+        // Row r of a tile is token r / group and head r % group: the order of a box of heads and tokens.
+        if (a.map_q) {
+          if (elect_one()) {
+            mbar_expect(full, DP * 2 * a.group * a.tok);
+            for (int x = 0; x < DP; x += 64)
+              tma_load_3d(smem_u32(dst) + x / 64 * L::kHalf, map, full, x, head, token);
+          }
+          continue;
         }
-        continue;
+        // Rows that no map can describe: an element at a time; elements past d are zeros.
+        const int rows = min(a.tok, g->nt - first) * a.group;
+        for (int i = lane; i < rows * DP; i += 32) {
+          const int r = i / DP, e = i % DP, t = r / a.group;
+          const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (int64_t)(token + t) * a.q.ts +
+                              (int64_t)(head + r - t * a.group) * a.q.hs;
+          *reinterpret_cast<uint16_t*>(dst + e / 64 * L::kHalf + r * 128 + ((e / 8 & 7) ^ (r & 7)) * 16 + e % 8 * 2) =
+              e < a.d ? q[e] : 0;
+        }
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full);
       }
-      // Rows that no map can describe: an element at a time; elements past d are zeros.
-      const int rows = min(a.tok, g->nt - first) * a.group;
-      for (int i = lane; i < rows * DP; i += 32) {
-        const int r = i / DP, e = i % DP, t = r / a.group;
-        const uint16_t* q = static_cast<const uint16_t*>(a.q.p) + (int64_t)(token + t) * a.q.ts +
-                            (int64_t)(head + r - t * a.group) * a.q.hs;
-        *reinterpret_cast<uint16_t*>(dst + e / 64 * L::kHalf + r * 128 + ((e / 8 & 7) ^ (r & 7)) * 16 + e % 8 * 2) =
-            e < a.d ? q[e] : 0;
-      }
-      fence_async_shared();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(full);
+      qs.step(*g);
     }
-    qs.step(*g);
   }
-}
+  // After a wait that ran out: the copies still in flight land before the CTA's shared memory is given back; they are
+  // waited for, again for a bounded time.
+  __device__ __forceinline__ void drain() {
+    int go_on = 0;
+    for (int i = 0; i < 2; ++i) mbar_wait(smem_u32(&c->q_full[i]), (issued >> i & 1) ^ 1, &go_on);
+  }
+};
 
 }  // namespace runs
 }  // namespace misat

@@ -103,19 +103,37 @@ struct KvBatch {
   int64_t stride;
 };
 
-// ---- barriers and copies, for the warp that loads queries: one thread, and barriers that fail when told to ----
-struct Bar {
-  int issued, waited;  // copies on their way to it, copies waited for
+// ---- barriers and copies, for the warp that loads queries: waits that pass until one runs out ----
+struct Copies {
+  uint32_t bar;
+  int issued;  // phases that copies were issued for
+  bool flying;
 };
-static std::vector<Bar> g_bars;
-static int g_passes;  // waits that pass before one runs out
+static Copies g_copies[2];
+static thread_local int t_waits;
+static int g_passes;  // waits of the warp that pass
+static volatile int* g_abort;
 static uint32_t smem_u32(const void* p) { return (uint32_t)(uintptr_t)p; }
-static bool mbar_wait(uint32_t, uint32_t, volatile int*, int = 1) { return true; }
+static bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort, int = 1) {
+  if (abort == g_abort && t_waits++ >= g_passes) {
+    *abort = 1;
+    return false;
+  }
+  for (Copies& c : g_copies)  // the copies of phase k land before a wait for its parity, k & 1, returns
+    if (c.bar == bar && c.issued > 0 && (((c.issued - 1) & 1) == (int)parity)) c.flying = false;
+  return true;
+}
 static void mbar_arrive(uint32_t) {}
-static void mbar_expect(uint32_t, uint32_t) {}
+static void mbar_expect(uint32_t bar, uint32_t) {
+  for (Copies& c : g_copies)
+    if (c.bar == bar) ++c.issued;
+}
 static bool elect_one() { return (threadIdx.x & 31) == 0; }
 static void fence_async_shared() {}
-static void tma_load_3d(uint32_t, const void*, uint32_t, int, int, int) {}
+static void tma_load_3d(uint32_t, const void*, uint32_t bar, int, int, int) {
+  for (Copies& c : g_copies)
+    if (c.bar == bar) c.flying = true;
+}
 }  // namespace misat
 using namespace misat;
 #include "runs.cuh"
@@ -196,4 +214,42 @@ extern "C" int deal(int n, const int32_t* off_x, const int32_t* off_y, const int
   *seen = check.parts;
   *error = err;
   return check.bad + g_outside;
+}
+
+// The warp that loads queries, where its wait after `passes` others runs out; part k is a pair, one of two heads or
+// neither by digit k of `kinds` (base 3), and the tiles are free when they are asked for.  Returns the tiles whose
+// copies are in flight when it ends.
+extern "C" int queries(int passes, int kinds) {
+  auto c = std::make_unique<Control>();
+  memset((void*)c.get(), 0, sizeof(Control));
+  AttendArgs a{};
+  a.map_q = true;
+  a.group = 4;
+  a.tok = 32;
+  for (int k = 0; k < kSegs; ++k, kinds /= 3) {
+    Segment& g = c->seg[k];
+    g.nb = 3;
+    g.nt = 1;
+    g.pair = kinds % 3 == 1;
+    g.twin = kinds % 3 == 2;
+  }
+  for (int i = 0; i < 2; ++i) g_copies[i] = {smem_u32(&c->q_full[i]), 0, false};
+  g_passes = passes;
+  g_abort = &c->abort;
+  Warp warp;
+  CUtensorMap map;
+  std::vector<char> smem(Layout<128>::kCtl);
+  std::vector<std::thread> threads;
+  for (int t = 0; t < 32; ++t)
+    threads.emplace_back([&, t] {
+      threadIdx = {256u + t, 0, 0};
+      warp_ = &warp;
+      t_waits = 0;
+      QueryLoader<128> ql{a, &map, smem.data(), c.get()};
+      ql.run();
+      __syncwarp();
+      if (*g_abort) ql.drain();
+    });
+  for (auto& t : threads) t.join();
+  return g_copies[0].flying + g_copies[1].flying;
 }

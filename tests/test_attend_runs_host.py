@@ -92,3 +92,10 @@ def test_steady_lengths_are_dealt_without_an_error(so, new, lens, group, hkv, gr
     lib = ctypes.CDLL(so)
     bad, seen, error = _deal(lib, (new, lens), (new, lens), group, hkv, 0, grid, 1 << 40)
     assert bad == 0 and error == 0 and seen >= sum(1 for x in new if x) * hkv // 2
+
+
+@pytest.mark.parametrize("passes", range(18))
+def test_query_copies_in_flight_are_waited_for_when_a_wait_runs_out(so, passes):
+    lib = ctypes.CDLL(so)
+    for kinds in range(81):
+        assert lib.queries(passes, kinds) == 0, (passes, kinds)
