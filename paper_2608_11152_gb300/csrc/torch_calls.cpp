@@ -27,6 +27,7 @@ struct Rope {
 struct Pool {
   misat_kv* h;
   c10::DeviceIndex device;
+  at::Tensor k_blocks, v_blocks;
   at::ScalarType dtype;
   int64_t hq, hkv, d;
   cudaStream_t last;  // of the last call outside a capture
@@ -92,6 +93,10 @@ const at::Tensor& heads(PyObject* o, const char* name, at::ScalarType dtype, c10
 at::Tensor fresh(at::IntArrayRef size, at::ScalarType dtype, c10::DeviceIndex device) {
   return at::Tensor(at::detail::empty_cuda(size, dtype, at::Device(at::kCUDA, device), std::nullopt));
 }
+// Autograd finds out by its version that a tensor it has saved was written.
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 int code_of(at::ScalarType t) {
   return t == at::kBFloat16 ? MISAT_BF16 : t == at::kHalf ? MISAT_F16 : t == at::kFloat ? MISAT_F32 : -1;
 }
@@ -145,13 +150,13 @@ PyObject* rope_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MISAT_END
 }
 
-// (handle, device, k_blocks, q heads)
+// (handle, device, k_blocks, v_blocks, q heads)
 PyObject* pool_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MISAT_TRY
-  if (!count(n, 4)) return nullptr;
-  const at::Tensor& k = tensor(a[2], "k_blocks");
-  Pool p{static_cast<misat_kv*>(PyLong_AsVoidPtr(a[0])), (c10::DeviceIndex)PyLong_AsLong(a[1]), k.scalar_type(),
-         PyLong_AsLong(a[3]), k.size(1), k.size(3), nullptr, false};
+  if (!count(n, 5)) return nullptr;
+  const at::Tensor &k = tensor(a[2], "k_blocks"), &v = tensor(a[3], "v_blocks");
+  Pool p{static_cast<misat_kv*>(PyLong_AsVoidPtr(a[0])), (c10::DeviceIndex)PyLong_AsLong(a[1]), k, v, k.scalar_type(),
+         PyLong_AsLong(a[4]), k.size(1), k.size(3), nullptr, false};
   return PyErr_Occurred() ? nullptr : new_state(p);
   MISAT_END
 }
@@ -214,6 +219,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
                               PyObject_IsTrue(a[4]) == 1, c10::cuda::getCurrentCUDAStream(r->device).stream());
   if (rc != MISAT_OK) return fail(rc, "misat_rotary");
   if (given) {
+    written(out);
     Py_INCREF(a[3]);
     return a[3];
   }
@@ -249,6 +255,9 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                  has_q ? q.stride(1) : 0, has_q ? out.data_ptr() : nullptr, has_q ? out.stride(0) : 0,
                                  has_q ? out.stride(1) : 0, ordered(p));
   if (rc != MISAT_OK) return fail(rc, "misat_kv_append");
+  written(p->k_blocks);
+  written(p->v_blocks);
+  if (given) written(out);
   if (has_q && !given) return THPVariable_Wrap(out);
   PyObject* r = given ? a[5] : Py_None;
   Py_INCREF(r);
@@ -278,6 +287,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
           : misat_kv_attend(p->h, &b->b, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0),
                             out.stride(1), with_lse ? lse.data_ptr<float>() : nullptr, (int32_t)window, ordered(p));
   if (rc != MISAT_OK) return fail(rc, "misat_kv_attend");
+  if (given) written(out);
   PyObject* o = a[3];
   if (given) Py_INCREF(o);
   else o = THPVariable_Wrap(out);

@@ -649,7 +649,7 @@ class KvPool:
         h = _p()
         _ck(_lib.misat_kv_create(C.byref(cfg), C.byref(h)), "misat_kv_create")
         self._h = h
-        self._state = calls.pool_state(h.value, self.device.index, k_blocks, self.n_q_heads)
+        self._state = calls.pool_state(h.value, self.device.index, k_blocks, v_blocks, self.n_q_heads)
         self._append, self._attend, self._sync = calls.append, calls.attend, calls.sync
 
     def close(self):

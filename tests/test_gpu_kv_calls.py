@@ -1,0 +1,47 @@
+"""The KV operators' calls on torch tensors: what they tell torch, and what they refuse."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests.test_gpu_kv import BF16, Step, misat, rand  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def test_tensors_that_are_written_have_a_new_version():
+    m = misat()
+    s = Step([(2, 20), (1, 5)], 2, 32, BF16)
+    rope = m.Rope(32)
+    pool = s.pool(4, rope=rope)
+    batch = s.batch(pool)
+    q, k, v = rand((3, 4, 32), BF16, 1), rand((3, 2, 32), BF16, 2), rand((3, 2, 32), BF16, 3)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+
+    def newer(call, *tensors):
+        before = [t._version for t in tensors]
+        others = [t._version for t in (k, v)]
+        call()
+        assert all(t._version > b for t, b in zip(tensors, before))
+        assert [t._version for t in (k, v)] == others
+
+    out = torch.empty_like(q)
+    newer(lambda: rope.rotate(q, pos, out=q), q)
+    newer(lambda: rope.backward(q, pos, out=out), out)
+    newer(lambda: pool.append(batch, k, v), s.kb, s.vb)
+    newer(lambda: pool.append(batch, k, v, q=q, q_out=q), q, s.kb, s.vb)
+    newer(lambda: pool.attend(batch, q, out=out), out)
+    # a value that a gradient needs and that is then rotated in place is noticed
+    x = rand((3, 4, 32), torch.float32, 4).requires_grad_()
+    y = x * 1.0
+    z = (y * y).sum()
+    rope.rotate(y, pos, out=y)
+    with pytest.raises(RuntimeError, match="inplace"):
+        z.backward()
+    # tensors without a version are written as before
+    with torch.inference_mode():
+        a = rand((3, 4, 32), BF16, 5)
+    b = a.clone()
+    rope.rotate(a, pos, out=a)
+    assert torch.equal(a, rope.rotate(b, pos))
+    pool.sync()
