@@ -36,6 +36,7 @@ struct Pool {
 struct Batch {
   misat_kv_batch b;
   int64_t hq, hkv, d;
+  c10::DeviceIndex device;
 };
 
 template <class S>
@@ -190,7 +191,7 @@ PyObject* batch_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return fail(MISAT_ERR_INVALID_ARG, "misat_kv_batch");
   Batch b{{(int32_t)seqs, (int32_t)tokens, (int32_t)max_q, off.data_ptr<int32_t>(), len.data_ptr<int32_t>(),
            table.data_ptr<int32_t>(), stride},
-          p->hq, p->hkv, p->d};
+          p->hq, p->hkv, p->d, p->device};
   return new_state(b);
   MISAT_END
 }
@@ -228,8 +229,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 bool same_heads(const Pool* p, const Batch* b) {
-  if (p->hq == b->hq && p->hkv == b->hkv && p->d == b->d) return true;
-  PyErr_SetString(PyExc_ValueError, "batch: made for other numbers of heads or another head_dim");
+  if (p->hq == b->hq && p->hkv == b->hkv && p->d == b->d && p->device == b->device) return true;
+  PyErr_SetString(PyExc_ValueError, "batch: made for other numbers of heads, another head_dim or another device");
   return false;
 }
 

@@ -605,7 +605,7 @@ class Rope:
 
 class KvBatch:
     """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer.  It serves
-    every pool of the same heads."""
+    every pool of the same heads on its device, and has to stay while a graph that holds a call with it is replayed."""
 
     def __init__(self, pool, q_off, kv_len, block_table, n_tokens, max_q):
         self._state = _torch_calls().batch_state(pool._state, q_off, kv_len, block_table, int(n_tokens), int(max_q))

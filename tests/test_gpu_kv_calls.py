@@ -45,3 +45,17 @@ def test_tensors_that_are_written_have_a_new_version():
     rope.rotate(a, pos, out=a)
     assert torch.equal(a, rope.rotate(b, pos))
     pool.sync()
+
+
+def test_a_batch_of_another_device_is_refused():
+    m = misat()
+    s = Step([(2, 20), (1, 5)], 2, 32, BF16)
+    pool = s.pool(4)
+    batch = s.batch(pool)
+    calls = m._torch_calls()
+    other = calls.pool_state(pool._h.value, 1, s.kb, s.vb, 4)  # (looked at, never launched with)
+    k = rand((3, 2, 32), BF16, 1)
+    with pytest.raises(ValueError, match="^batch: "):
+        calls.append(other, batch._state, k, k, None, None)
+    with pytest.raises(ValueError, match="^batch: "):
+        calls.attend(other, batch._state, k, None, 0, False)
