@@ -571,6 +571,7 @@ class Rope:
         import torch
 
         self._h = None
+        self._pools = 0  # open pools that apply it
         self.rot_dim = int(rot_dim)
         cfg = misat_rope_config(self.rot_dim, layout, scaling, base, factor, orig_len, beta_slow, beta_fast,
                                 attn_factor)
@@ -583,7 +584,10 @@ class Rope:
         self._rotary = calls.rotary
 
     def close(self):
+        """Frees the frequencies; MisatError (ERR_STATE) while an open KvPool applies them."""
         if getattr(self, "_h", None):
+            if self._pools:
+                raise MisatError(ERR_STATE, "Rope.close")
             self._state = None
             _lib.misat_rope_destroy(self._h)
             self._h = None
@@ -638,6 +642,8 @@ class KvPool:
         if code is None or k_blocks.device != self.device or v_blocks.device != self.device or \
                 v_blocks.dtype != k_blocks.dtype:
             raise ValueError(f"k_blocks, v_blocks: one floating-point dtype on {self.device} expected")
+        if rope is not None and not rope._h:
+            raise ValueError("rope: closed")
         calls = _torch_calls()
         self.dtype = k_blocks.dtype
         self.n_blocks, self.n_kv_heads, _, self.head_dim = k_blocks.shape
@@ -649,6 +655,8 @@ class KvPool:
         h = _p()
         _ck(_lib.misat_kv_create(C.byref(cfg), C.byref(h)), "misat_kv_create")
         self._h = h
+        if rope is not None:
+            rope._pools += 1
         self._state = calls.pool_state(h.value, self.device.index, k_blocks, v_blocks, self.n_q_heads)
         self._append, self._attend, self._sync = calls.append, calls.attend, calls.sync
 
@@ -657,6 +665,8 @@ class KvPool:
             self._state = None
             _lib.misat_kv_destroy(self._h)
             self._h = None
+            if self.rope is not None:
+                self.rope._pools -= 1
 
     def __del__(self):
         try:

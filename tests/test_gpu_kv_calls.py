@@ -59,3 +59,25 @@ def test_a_batch_of_another_device_is_refused():
         calls.append(other, batch._state, k, k, None, None)
     with pytest.raises(ValueError, match="^batch: "):
         calls.attend(other, batch._state, k, None, 0, False)
+
+
+def test_a_rotation_stays_while_a_pool_applies_it():
+    m = misat()
+    s = Step([(2, 20), (1, 5)], 2, 32, BF16)
+    rope = m.Rope(32)
+    pools = [s.pool(4, rope=rope) for _ in range(2)]
+    q, k = rand((3, 4, 32), BF16, 1), rand((3, 2, 32), BF16, 2)
+    want = pools[0].append(s.batch(pools[0]), k, k, q=q)
+    for pool in pools:
+        with pytest.raises(m.MisatError) as e:
+            rope.close()
+        assert e.value.code == m.ERR_STATE
+        assert torch.equal(pool.append(s.batch(pool), k, k, q=q), want)
+        pool.close()
+        pool.close()
+    rope.close()
+    rope.close()
+    with pytest.raises(ValueError, match="rope"):  # not a pool without a rotation
+        s.pool(4, rope=rope)
+    with pytest.raises(ValueError):
+        rope.rotate(q, torch.zeros(3, dtype=torch.int32, device="cuda"))
