@@ -102,20 +102,26 @@ int code_of(at::ScalarType t) {
   return t == at::kBFloat16 ? MISAT_BF16 : t == at::kHalf ? MISAT_F16 : t == at::kFloat ? MISAT_F32 : -1;
 }
 
+bool capturing(cudaStream_t st) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusActive;
+  return cudaStreamIsCapturing(st, &status) != cudaSuccess || status != cudaStreamCaptureStatusNone;
+}
 // The current stream; a pool's calls share its workspace, so a change of stream waits for the calls on
 // the last one.  Under capture nothing is recorded: whoever replays the graph orders it with other calls.
+// Where the last stream cannot be waited for (it is being captured, or gone), the call is an error.
 cudaStream_t ordered(Pool* p) {
   const cudaStream_t st = c10::cuda::getCurrentCUDAStream(p->device).stream();
-  if (p->called && st == p->last) return st;
-  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(st, &capturing) == cudaSuccess && capturing != cudaStreamCaptureStatusNone) return st;
+  if ((p->called && st == p->last) || capturing(st)) return st;
   if (p->called) {
-    cudaEvent_t e;
-    if (cudaEventCreateWithFlags(&e, cudaEventDisableTiming) == cudaSuccess) {
-      if (cudaEventRecord(e, p->last) == cudaSuccess) cudaStreamWaitEvent(st, e, 0);
-      cudaEventDestroy(e);
+    cudaEvent_t e = nullptr;
+    bool ok = !capturing(p->last) && cudaEventCreateWithFlags(&e, cudaEventDisableTiming) == cudaSuccess;
+    ok = ok && cudaEventRecord(e, p->last) == cudaSuccess && cudaStreamWaitEvent(st, e, 0) == cudaSuccess;
+    if (e) cudaEventDestroy(e);
+    if (!ok) {
+      cudaGetLastError();
+      fail(MISAT_ERR_STATE, "KvPool: the stream of its last call cannot be waited for");
+      throw Raised{};
     }
-    cudaGetLastError();
   }
   p->called = true;
   p->last = st;

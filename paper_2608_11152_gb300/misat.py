@@ -627,7 +627,8 @@ class KvPool:
     k_blocks, v_blocks: [n_blocks, n_kv_heads, 16, head_dim], contiguous, bfloat16 or float16; the
     caller's memory.  rope: a Rope that append() applies, or None.  scale: factor on q.k
     (1 / sqrt(head_dim)).  Calls run on the current stream; the pool orders its own calls when that
-    stream changes."""
+    stream changes (which has to exist until the next call).  Calls that are captured into a graph use the pool's
+    workspace when the graph is replayed: the caller orders a replay with the pool's other calls and replays."""
 
     def __init__(self, k_blocks, v_blocks, *, n_q_heads, rope=None, scale=0.0, max_batch=1 << 20):
         import torch

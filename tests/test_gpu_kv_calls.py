@@ -81,3 +81,29 @@ def test_a_rotation_stays_while_a_pool_applies_it():
         s.pool(4, rope=rope)
     with pytest.raises(ValueError):
         rope.rotate(q, torch.zeros(3, dtype=torch.int32, device="cuda"))
+
+
+def test_a_call_that_cannot_be_ordered_behind_the_last_one_is_an_error():
+    m = misat()
+    s = Step([(1, 3000), (4, 20)], 2, 32, BF16)
+    pool = s.pool(4)
+    batch = s.batch(pool)
+    q = rand((5, 4, 32), BF16, 1)
+    out, side = torch.empty_like(q), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = pool.attend(batch, q)
+    torch.cuda.synchronize()
+    graph, third = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side, capture_error_mode="relaxed"):
+        in_graph = pool.attend(batch, q)
+        with torch.cuda.stream(third), pytest.raises(m.MisatError) as e:
+            pool.attend(batch, q, out=out)
+    assert e.value.code == m.ERR_STATE
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(in_graph, want)
+    with torch.cuda.stream(third):  # and again once the capture is over
+        pool.attend(batch, q, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
