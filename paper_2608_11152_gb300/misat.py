@@ -555,7 +555,11 @@ def _torch_calls():
     if _calls is None:
         import torch  # noqa: F401
 
-        from . import _calls as module
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise ImportError("_calls.so is missing or made for another PyTorch: build it where PyTorch, g++ and Python's "
+                              "headers are (python -c 'import __graft_entry__ as g; g.build()')") from e
 
         module.init(MisatError)
         _calls = module
