@@ -581,6 +581,8 @@ int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, in
  * scores are all -infinity gets NaN (0 / 0), and -infinity in lse; a score of +infinity or NaN makes
  * both NaN.  Slots past kv_len are never used, whatever they hold; a key that only some new tokens
  * of a sequence see has to be finite for all of them (0 times infinity is NaN).
+ * out may be q itself (same pointer and strides) but not overlap it otherwise: a row is written when
+ * all parts of its item have read their queries.
  * The result does not depend on timing: the same call gives the same bits.  [async]
  * Errors: INVALID_ARG, CUDA; INVALID_ARG later (see above; what the skipped sequences' rows
  * of out and lse then hold is not specified). */

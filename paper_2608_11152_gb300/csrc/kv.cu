@@ -61,7 +61,7 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
   if (!batch_ok(kv, batch) || window < 0) return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) ||
-      (reinterpret_cast<uintptr_t>(lse) & 3) || !on_device(kv->device))
+      !in_place_ok(q, q_ts, q_hs, out, o_ts, o_hs, batch->n_tokens, kv->hq) || (reinterpret_cast<uintptr_t>(lse) & 3) || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
   launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, window,
                 static_cast<cudaStream_t>(cuda_stream));

@@ -63,6 +63,11 @@ inline bool heads_ok(const void* p, int64_t ts, int64_t hs, int elem) {
 inline bool result_ok(const void* p, int64_t ts, int64_t hs, int elem, int n_tokens, int n_heads) {
   return heads_ok(p, ts, hs, elem) && (n_tokens <= 1 || ts > 0) && (n_heads <= 1 || hs > 0);
 }
+// A result at its input's address is the input itself: the same strides, where there is more than one to step over.
+inline bool in_place_ok(const void* x, int64_t ts, int64_t hs, const void* out, int64_t o_ts, int64_t o_hs, int n_tokens,
+                        int n_heads) {
+  return x != out || ((n_tokens <= 1 || ts == o_ts) && (n_heads <= 1 || hs == o_hs));
+}
 inline bool batch_ok(const misat_kv* kv, const misat_kv_batch* b) {
   if (!kv || !b || b->n < 0 || b->n > kv->max_batch || b->n_tokens < 0 || b->max_q < 0 || b->table_stride < 0)
     return false;

@@ -359,7 +359,7 @@ int misat_rotary(const misat_rope* r, int32_t dtype, int32_t n_tokens, int32_t n
   const int elem = dtype == MISAT_F32 ? 4 : 2;
   if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions)
     return MISAT_ERR_INVALID_ARG;
-  if (x == out && (x_ts != o_ts || x_hs != o_hs)) return MISAT_ERR_INVALID_ARG;
+  if (!in_place_ok(x, x_ts, x_hs, out, o_ts, o_hs, n_tokens, n_heads)) return MISAT_ERR_INVALID_ARG;
   if (!on_device(r->device)) return MISAT_ERR_INVALID_ARG;
   RotArgs a{};
   a.n_tokens = n_tokens;
@@ -383,7 +383,7 @@ int misat_kv_append(misat_kv* kv, const misat_kv_batch* batch, const void* k, in
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!heads_ok(k, k_ts, k_hs, 2) || !heads_ok(v, v_ts, v_hs, 2)) return MISAT_ERR_INVALID_ARG;
   if (q && (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(q_out, qo_ts, qo_hs, 2, batch->n_tokens, kv->hq) ||
-            (q == q_out && (q_ts != qo_ts || q_hs != qo_hs))))
+            !in_place_ok(q, q_ts, q_hs, q_out, qo_ts, qo_hs, batch->n_tokens, kv->hq)))
     return MISAT_ERR_INVALID_ARG;
   if (!on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
   RotArgs a{};

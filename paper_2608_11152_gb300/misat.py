@@ -691,7 +691,8 @@ class KvPool:
 
     def attend(self, batch, q, out=None, window=0, return_lse=False):
         """Attention of the new tokens' q [n_tokens, q heads, head_dim] over the cached tokens up to
-        and including each; window > 0: over the last `window` of them.  Returns out, or (out, lse)."""
+        and including each; window > 0: over the last `window` of them.  out may be q.  Returns out, or
+        (out, lse)."""
         return self._attend(self._state, batch._state, q, out, window, return_lse)
 
     def sync(self):

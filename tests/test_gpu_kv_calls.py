@@ -107,3 +107,55 @@ def test_a_call_that_cannot_be_ordered_behind_the_last_one_is_an_error():
         pool.attend(batch, q, out=out)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("odd", [0, 3])
+@pytest.mark.parametrize("seqs,hq,hkv,d", [
+    ([(1, 40000), (2, 20000)], 8, 2, 128),             # items split between processors
+    ([(300, 900), (129, 5000), (1, 7)], 4, 4, 64),     # two tiles of an item
+    ([(1, 40 + i) for i in range(333)], 8, 8, 64),     # two heads of an item at a time
+    ([(77, 50), (300, 1200)] * 40, 6, 3, 72)])         # many items, rows without keys among them
+def test_attend_into_its_queries(seqs, hq, hkv, d, odd):
+    s = Step(seqs, hkv, d, BF16)
+    pool = s.pool(hq)
+    batch = s.batch(pool)
+    wide = rand((s.T, hq * d + 8), BF16, 3)
+    q = wide[:, odd:odd + hq * d].view(s.T, hq, d)
+    keep = wide.clone()
+    want, want_lse = pool.attend(batch, q, return_lse=True)
+    out, lse = pool.attend(batch, q, out=q, return_lse=True)
+    pool.sync()
+    assert out is q and torch.equal(q, want) and torch.equal(lse, want_lse)
+    assert torch.equal(wide[:, :odd], keep[:, :odd]) and torch.equal(wide[:, odd + hq * d:], keep[:, odd + hq * d:])
+
+
+def test_results_at_the_address_of_their_input_with_other_strides():
+    m = misat()
+    x = rand((4096,), BF16, 1)
+    y = x.clone()
+    rope = m.Rope(32)
+
+    def step(n):
+        s = Step([(n, 20)], 2, 32, BF16)
+        pool = s.pool(4, rope=rope)
+        return pool, s.batch(pool), rand((n, 2, 32), BF16, 2)
+
+    pool, batch, k = step(3)
+    pos = torch.arange(3, dtype=torch.int32, device="cuda")
+    a, b, c = (x.as_strided((3, 4, 32), t) for t in ((128, 32, 1), (256, 32, 1), (128, 64, 1)))
+    for other in (b, c):
+        for call in (lambda: rope.rotate(a, pos, out=other), lambda: pool.append(batch, k, k, q=a, q_out=other),
+                     lambda: pool.attend(batch, a, out=other)):
+            with pytest.raises(m.MisatError) as e:
+                call()
+            assert e.value.code == m.ERR_INVALID_ARG
+    assert torch.equal(x, y)
+    # a single token's stride is not stepped over
+    pool, batch, k = step(1)
+    one, same = x.as_strided((1, 4, 32), (999, 32, 1)), x.as_strided((1, 4, 32), (128, 32, 1))
+    want = rope.rotate(one.clone(), pos[1:2])
+    assert torch.equal(rope.rotate(one, pos[1:2], out=same), want)
+    want = pool.append(batch, k, k, q=one.clone())
+    assert torch.equal(pool.append(batch, k, k, q=one, q_out=same), want)
+    want = pool.attend(batch, one.clone())
+    assert torch.equal(pool.attend(batch, one, out=same), want)
