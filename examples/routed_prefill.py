@@ -63,7 +63,8 @@ class Instance:
         batch = self.pool.batch(torch.from_numpy(off).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"),
                                 table, n_tokens=int(off[-1]), max_q=max(len(x) for x in new))
         q, k, v = self.layer.qkv(torch.from_numpy(np.concatenate(new)).cuda())
-        return self.pool.attend(batch, self.pool.append(batch, k, v, q=q)), off
+        self.q = self.pool.append(batch, k, v, q=q)
+        return self.pool.attend(batch, self.q), off
 
 
 def plain(layer, tokens):
@@ -82,8 +83,10 @@ def plain(layer, tokens):
     return torch.einsum("hgl,lhd->hgd", x.softmax(-1), v).reshape(HQ, D)
 
 
-def run(instance=0, decode=4, checks=3):
-    """Routes the workload's batches; returns counts and the largest difference from plain()."""
+def run(instance=0, decode=4, checks=3, inspect=None):
+    """Routes the workload's batches; returns counts and the largest difference from plain().  After each step,
+    inspect(engine, tables, tokens, new, out) gets the sequences' block tables and tokens, how many of these were
+    new, and the outputs of the new ones."""
     sc = wl.config1()
     r = misat.Router(sc.cap_blocks, max_batch=sc.max_batch, max_tokens=sc.max_tokens,
                      protected_frac_q16=sc.protected_frac_q16, mode=sc.mode, hold_delay_q=sc.hold_delay_q,
@@ -108,6 +111,8 @@ def run(instance=0, decode=4, checks=3):
             tables = [[engine.where[int(k)] for k in keys[first[q]:first[q] + h]] for q, h in zip(mine, held)]
             lens = [len(p) for p in prompts]
             o, off = engine.step(tables, lens, [p[h * BLOCK:] for p, h in zip(prompts, held)])
+            if inspect:
+                inspect(engine, tables, prompts, np.diff(off).tolist(), o)
             for q, t in zip(mine, tables):
                 for j, k in enumerate(keys[first[q]:first[q + 1]]):
                     engine.where.setdefault(int(k), t[j])
@@ -129,6 +134,8 @@ def run(instance=0, decode=4, checks=3):
                 token = [np.array([(7919 * (s + 1) + 31 * i) % wl.VOCAB], np.int32) for i in range(len(mine))]
                 grown = [np.concatenate((p, t)) for p, t in zip(grown, token)]
                 o, _ = engine.step(tails, [len(p) for p in grown], token)
+                if inspect:
+                    inspect(engine, tails, grown, [1] * len(mine), o)
                 stats["decoded"] += len(mine)
             if decode:
                 d = (o[0].float() - plain(engine.layer, grown[0])).abs().max().item()
