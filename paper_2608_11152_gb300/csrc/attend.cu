@@ -49,7 +49,7 @@ constexpr int kRegsIssue = 88, kRegsSoftmax = 208;  // 128 * 88 + 256 * 208 = 38
 // The weights in 16 bits are 2^(kFactor + c (s - m)): O and l carry the factor 2^kFactor, which the result does not
 // see and the log-sum-exp takes off; O and l are rescaled when a score passes m by more than 2^kRescale.
 // bfloat16 has the exponents of 32 bits and needs no factor.  float16 holds 2^-14 to 2^16 in full precision and
-// rounds to zero below 2^-25: with 65,000 as the largest weight, one that is 2^-25 of its row's reference keeps its
+// rounds to zero below 2^-25: with 61,000 as the largest weight, one that is 2^-25 of its row's reference keeps its
 // 11 bits, and zero is what is below 2^-36 of it.  (With 2^8 as the largest weight and no factor, 131,072 keys 18
 // below one that takes most of the weight added up to 1.4% too little.)  The narrower range means more rescales: 97
 // prompts of 512 to 2,048 tokens under a window, scores of standard deviation 1, take 954 us, 940 with a factor of
@@ -60,7 +60,7 @@ struct Weights {
 };
 template <>
 struct Weights<__half> {
-  static constexpr float kRescale = 4.99f, kFactor = 11.f, kOff = 0x1p-11f;
+  static constexpr float kRescale = 4.9f, kFactor = 11.f, kOff = 0x1p-11f;
 };
 
 // ---- matrix instructions ----
@@ -286,10 +286,16 @@ struct Softmax {
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     // While a row has seen no key (a window that begins inside the block), its O and l are zeros of any scale.
     if (fresh || m == -INFINITY) m = top;
-    if (!fresh) {
-      const bool need = top > m && !((top - m) * a.c <= Weights<T>::kRescale);
-      if (__any_sync(0xffffffffu, need)) {
-        const float f = need ? exp2_approx((m - top) * a.c) : 1.f;
+    const bool need = !fresh && top > m && !((top - m) * a.c <= Weights<T>::kRescale);
+    const float from = m;
+    if (need) m = top;
+    float ref = m == -INFINITY ? 0.f : fmaf(-m, a.c, Weights<T>::kFactor);
+    // Where c m has few bits behind the point, the weights' exponents do not come out of c s - c m: m is taken off the
+    // scores first, which is exact near it.  (The rounding of c m would pass float16's largest weight.)
+    const bool far = fabsf(ref) >= 0x1p20f;
+    if (__any_sync(0xffffffffu, need || far)) {
+      if (!fresh) {
+        const float f = need ? exp2_approx((from - top) * a.c) : 1.f;
         const uint64_t f2 = pack2(f, f);
 #pragma unroll 1
         for (int q = 0; q < DP / 16; ++q) {
@@ -306,15 +312,25 @@ struct Softmax {
           tmem_st16(tmem + col_o<DP>(st) + q * 16, o);
         }
         l *= f;
-        if (need) m = top;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld32_issue(r[q], tmem + col_s(st) + q * 32);
-        tmem_landed();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_tie(r[q]);
       }
+      const float off = far ? m : 0.f;
+#pragma unroll 1
+      for (int q = __any_sync(0xffffffffu, far) ? 0 : 4; q < 4; ++q) {
+        uint32_t x[32];
+        __syncwarp();
+        tmem_ld32(x, tmem + col_s(st) + q * 32);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) - off);
+        tmem_st32(tmem + col_s(st) + q * 32, x);
+      }
+      tc_wait_st();
+      if (far) ref = Weights<T>::kFactor;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_ld32_issue(r[q], tmem + col_s(st) + q * 32);
+      tmem_landed();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_tie(r[q]);
     }
-    const float ref = m == -INFINITY ? 0.f : fmaf(-m, a.c, Weights<T>::kFactor);
     const uint64_t c2 = pack2(a.c, a.c), ref2 = pack2(ref, ref);
     uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll

@@ -125,3 +125,38 @@ def test_attend_infinite_and_nan_values_that_are_seen(n, L, dtype):
     other = torch.arange(d, device="cuda") != 9
     assert torch.equal(out[..., other], good[..., other])
     s.vb[at] = kept
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,L", [(1, 700), (20, 700), (1, 9000)])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+@pytest.mark.parametrize("size", [2.0 ** 5, 2.0 ** 9, 2.0 ** 12])
+def test_attend_scores_far_from_zero(size, order, n, L, dtype):
+    """Scores up to 2^28, far enough apart that a row is the mean of the values of its highest 128 keys; the exponent
+    of a weight is the small difference of two large numbers."""
+    d = 64
+
+    def k0(pos):  # whole blocks of one score, a step of the type's last place between them
+        step = (pos // 128).double() / (L // 128)
+        x = 32768 + (32767.0 if dtype == F16 else 32768.0 - 256) * (step if order == "rising" else 1 - step)
+        unit = 32 if dtype == F16 else 256
+        return ((x // unit) * unit).float()
+
+    s, q = one_head([(n, L)], 2, d, dtype, k0)
+    s.kb[..., 1:] = 0
+    q[..., 0] = size * d ** 0.5
+    pool = s.pool(2)
+    out, lse = pool.attend(s.batch(pool), q, return_lse=True)
+    pool.sync()
+    x = ref.gather(s.kb, s.table[0], L)[:, 0, 0].double() * size
+    v = ref.gather(s.vb, s.table[0], L)[:, 0].double()
+    see = torch.arange(L, device="cuda")[None] <= torch.arange(L - n, L, device="cuda")[:, None]
+    z = torch.where(see, x[None], -float("inf"))
+    p = z.softmax(-1)
+    want, size_v = (p @ v)[:, None].expand(n, 2, d), (p @ v.abs())[:, None].expand(n, 2, d)
+    u = ref.U[dtype]
+    # weights and result rounded once, sums of up to 9,000 terms in 32 bits; a step of scores is 2^10 at least
+    tol = u * (1 + 2.0 ** -10) * (size_v + want.abs()) + (L / 16 + 80) * 2.0 ** -23 * size_v + ref.TINY[dtype]
+    ref.assert_within("out", out, want, tol)
+    top = torch.logsumexp(z, -1)[:, None].expand(n, 2)
+    ref.assert_within("lse", lse, top, 2.0 ** -22 * top)
