@@ -491,7 +491,8 @@ int misat_recheck_delays(int32_t n, const uint64_t* group, const uint8_t* held, 
  *   BY_PARTS  f_i (g + (1 - g) / factor) with g = clamp((r_i - beta_slow) /
  *             (beta_fast - beta_slow), 0, 1) and r_i = orig_len f_i / (2 pi), the turns that
  *             the pair makes over the original length: slow pairs are interpolated, fast ones
- *             kept. */
+ *             kept.  The blend is linear in the turns r_i; one that is linear in the pair's index
+ *             i between two rounded indices gives other frequencies. */
 #define MISAT_ROPE_HALF 0        /* pair i = elements i and i + rot_dim / 2 */
 #define MISAT_ROPE_INTERLEAVED 1 /* pair i = elements 2i and 2i + 1 */
 #define MISAT_ROPE_SCALE_NONE 0
@@ -513,7 +514,7 @@ typedef struct misat_rope_config {
 int misat_rope_create(const misat_rope_config* cfg, misat_rope** out);
 /* Frees them; no call that uses them, nor a pool made with them, may be pending.  [sync] */
 int misat_rope_destroy(misat_rope* rope);
-/* out = rotation of x (n_tokens x n_heads heads of head_dim >= rot_dim elements, at most 1024)
+/* out = rotation of x (n_tokens x n_heads heads, at most 65535, of head_dim >= rot_dim elements, at most 1024)
  * at positions[token]; the elements past rot_dim are copied.  backward != 0: the gradient of x
  * given the gradient of out, i.e. the transposed map (the turn the other way).  dtype:
  * MISAT_BF16, F16 or F32; computed in 32 bits and rounded once.  out may be x itself (same
@@ -527,8 +528,8 @@ int misat_rotary(const misat_rope* rope, int32_t dtype, int32_t n_tokens, int32_
 typedef struct misat_kv misat_kv;
 typedef struct misat_kv_config {
   int32_t n_blocks;    /* >= 1, n_blocks * n_kv_heads < 2^31 */
-  int32_t n_kv_heads;  /* >= 1 */
-  int32_t n_q_heads;   /* a multiple of n_kv_heads, at most 128 per kv head */
+  int32_t n_kv_heads;  /* 1..1024 */
+  int32_t n_q_heads;   /* a multiple of n_kv_heads, at most 128 per kv head and 32768 in all */
   int32_t head_dim;    /* a multiple of 8, 8..128 */
   int32_t dtype;       /* MISAT_BF16 or MISAT_F16: of the blocks and of every q, k, v, out */
   int32_t max_batch;   /* largest n of a misat_kv_batch, 1..2^20 */

@@ -14,7 +14,7 @@
 // What bounds it, and what it does: a step of single tokens reads the cache once, at 7.0 TB/s (256 sequences
 // of 512 to 16,000 tokens, 8 kv heads of 128: 1.19 to 1.23 ms for 8.4 GB); a chunk is the products and the
 // chain of scores, exponentials and product of each stream, at 1,260 to 1,440 TFLOP/s of 1,887 (2,048 tokens
-// over 129,024, 32 heads: 3.03 to 3.45 ms on different GPUs, power-capped at some 1.55 GHz).
+// over 129,024, 32 heads: 3.03 to 3.47 ms on different GPUs, power-capped at some 1.55 GHz).
 //
 // Two streams of such tiles share a CTA, so that one's matrix products run under the other's
 // exponentials.  An item of more than 128 rows gives each stream half of its rows, and both read the same
@@ -52,8 +52,8 @@ constexpr int kRegsIssue = 88, kRegsSoftmax = 208;  // 128 * 88 + 256 * 208 = 38
 // rounds to zero below 2^-25: with 61,000 as the largest weight, one that is 2^-25 of its row's reference keeps its
 // 11 bits, and zero is what is below 2^-36 of it.  (With 2^8 as the largest weight and no factor, 131,072 keys 18
 // below one that takes most of the weight added up to 1.4% too little.)  The narrower range means more rescales: 97
-// prompts of 512 to 2,048 tokens under a window, scores of standard deviation 1, take 954 us, 940 with a factor of
-// 2^10, 934 with 2^9, 930 with 2^8; one token over 131,072, 91 us with each.
+// prompts of 512 to 2,048 tokens under a window, scores of standard deviation 1, took 954 us with it, 940 with a factor
+// of 2^10, 934 with 2^9, 930 with 2^8; one token over 131,072, 91 us with each.
 template <class T>
 struct Weights {
   static constexpr float kRescale = 8.f, kFactor = 0.f, kOff = 1.f;

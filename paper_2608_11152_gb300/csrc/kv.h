@@ -8,9 +8,10 @@
 #include "common.cuh"
 
 // Frequencies of a rotation as fractions of a turn in 64-bit fixed point: the angle at position p
-// is (p * freq[i] mod 2^64) / 2^64 turns.  The product wraps at whole turns, so the angle is exact
-// to 2^-44 turns at any position below 2^20, where a 32-bit product of position and frequency has
-// lost all but a few bits.
+// is (p * freq[i] mod 2^64) / 2^64 turns.  The product wraps at whole turns, so nothing is lost in the
+// reduction: the angle is off by the frequency's own rounding in 64 bits (2^-54 turns times the position)
+// and the cut to 32 bits (2^-32 turns), below 2^-31 turns at any position below 2^20, where a 32-bit product of
+// position and frequency has lost all but a few bits.
 struct misat_rope {
   int device, num_sms;
   int32_t rot, layout;
