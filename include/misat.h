@@ -591,6 +591,129 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
                     int64_t q_head_stride, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                     int32_t window, void* cuda_stream);
 
+/* ---- a step on the device: block tables, normed heads, trees of drafted tokens ---- */
+
+/* The step of n sequences: each row of the block table is brought to the length after the step,
+ *   len = kv_len + new_tokens,  need = ceil(len / 16)
+ * A row with fewer than `need` blocks gets the missing ones from the front of a ring of free
+ * blocks; one with more gives those from max(need, shared) on to the ring's end (its first
+ * `shared` blocks are another's, a prefix's, and are dropped without being given back).  Blocks
+ * are taken and given in the order of the sequences and of the places in a row, so the result
+ * does not depend on timing; blocks given in a step can be taken from the next one on.
+ * state: [n] blocks in each row, then the ring's front (a place in [0, ring_size)) and the number
+ * of free blocks from there on.
+ * A step that cannot be made changes nothing, but for q_off (zeros), positions and slots (-1) and
+ * copies of what is not changed (state_out, kv_len_out): fewer free blocks than it takes (OOM),
+ * more given than the ring has room for, a negative or longer count than allowed, a row with
+ * fewer blocks than its kv_len tokens fill or too short for the step, offsets whose sum is not n_tokens (INVALID_ARG;
+ * all sticky, from misat_kv_sync). */
+typedef struct misat_kv_step {
+  int32_t n;                 /* sequences, 0..max_batch of the pool */
+  int32_t n_tokens;          /* sum of new_tokens, below 2^31 - 1 */
+  int32_t max_q;             /* at least the new tokens of any sequence */
+  int32_t columns;           /* blocks that a row of the table has room for */
+  int64_t table_stride;      /* >= columns */
+  int32_t ring_size;         /* >= 1; as many as there are blocks always suffice */
+  const int32_t* new_tokens; /* device [n], >= 0 */
+  const int32_t* kv_len;     /* [n] tokens before the step (after it at most 2^30) */
+  const int32_t* shared;     /* [n] or NULL (none) */
+  const int32_t* state;      /* [n + 2] */
+  int32_t* block_table;      /* [n][table_stride], read and written */
+  int32_t* ring;             /* [ring_size], read and written */
+  int32_t* state_out;        /* [n + 2], may be state */
+  int32_t* q_off;            /* [n + 1] */
+  int32_t* kv_len_out;       /* [n] tokens after the step, may be kv_len */
+  int32_t* positions;        /* [n_tokens] position of each new token */
+  int64_t* slots;            /* [n_tokens] its slot: 16 block + position % 16 */
+} misat_kv_step;
+/* work: device scratch of MISAT_KV_TABLES_WORK(n) bytes, 4-byte aligned, the call's own until it
+ * is finished.  Writes what a misat_kv_batch of this step takes.  [async]
+ * Errors: INVALID_ARG, CUDA; OOM and INVALID_ARG later. */
+#define MISAT_KV_TABLES_WORK(n) (16 * (int64_t)(n) + 32)
+int misat_kv_tables(misat_kv* kv, const misat_kv_step* step, void* work, int64_t work_bytes, void* cuda_stream);
+
+/* Norm of each head, and the rotation behind it:
+ *   y = R_p (x r (offset + weight)),   r = 1 / sqrt(mean x^2 + eps)
+ * over the head's head_dim elements, the sum of squares in 32 bits (elements beyond 2^60 in magnitude may overflow it).
+ * weight: [head_dim] for all heads (head_stride 0), or [heads][head_stride], of the tensor's dtype
+ * or of MISAT_F32. */
+typedef struct misat_head_norm {
+  const void* weight;
+  int64_t head_stride; /* elements; 0, or at least head_dim */
+  int32_t dtype;
+  float eps;           /* finite, > 0 */
+  float offset;        /* finite */
+} misat_head_norm;
+/* Like misat_rotary with the norm before the rotation; head_dim at most 256.  Values are rounded
+ * once.  Errors: INVALID_ARG, CUDA.  [async] */
+int misat_norm_rotary(const misat_rope* rope, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                      int32_t n_heads, int32_t head_dim, const void* x, int64_t x_token_stride, int64_t x_head_stride,
+                      const int32_t* positions, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                      void* cuda_stream);
+/* Gradients of misat_norm_rotary's x and weight, given the gradient of its result (grad):
+ *   g = R_p^T grad,  a = g (offset + weight),  dx = r a - x r^3 mean(a x),  dweight = sum g x r
+ * (the sum over tokens, and over heads where they share the weight; in 32 bits, in an order that
+ * depends on sizes and GPU alone, so the same call gives the same bits).  dx may be x or grad
+ * (same pointer and strides); dweight has the weight's dtype and shape, its rows dw_head_stride >=
+ * head_dim elements apart (not read where the heads share one).  work: device scratch of *bytes from misat_norm_rotary_work, 16-byte aligned, the call's own until it is
+ * finished.  Errors: INVALID_ARG, CUDA.  [async] */
+int misat_norm_rotary_work(const misat_rope* rope, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                           int32_t n_heads, int32_t head_dim, int64_t* bytes);
+int misat_norm_rotary_backward(const misat_rope* rope, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                               int32_t n_heads, int32_t head_dim, const void* x, int64_t x_token_stride,
+                               int64_t x_head_stride, const void* grad, int64_t g_token_stride, int64_t g_head_stride,
+                               const int32_t* positions, void* dx, int64_t dx_token_stride, int64_t dx_head_stride,
+                               void* dweight, int64_t dw_head_stride, void* work, int64_t work_bytes,
+                               void* cuda_stream);
+
+/* Trees of drafted tokens.  A sequence's new tokens are the nodes of its tree: parents[t] is the
+ * number of token t's parent within the sequence, smaller than its own; MISAT_KV_ROOT where the node
+ * follows the tokens before the tree; MISAT_KV_ABSENT where there is no such node (steps of a fixed
+ * shape).  A node at depth e (a root's is 0) is at position kv_len - new + e, in the slot of its
+ * number, kv_len - new + i. */
+#define MISAT_KV_TREE_NODES 1024 /* most new tokens of a sequence */
+#define MISAT_KV_ROOT (-1)
+#define MISAT_KV_ABSENT (-2)
+typedef struct misat_kv_draft {
+  const int32_t* depth; /* [n_tokens] */
+  const uint32_t* bits; /* [n_tokens][words]: bit j % 32 of word j / 32 is set where node j is the
+                           node itself or an ancestor that its window reaches */
+  int32_t words;        /* ceil(max_q / 32) of the batch */
+  int32_t window;       /* 0, or the last positions that a node sees, its own included */
+} misat_kv_draft;
+/* The plan of a step's trees: depth and bits as above, for misat_kv_append_norm and
+ * misat_kv_attend_tree of every layer.  An absent node has depth 0 and no bits.  A number that is no
+ * earlier node's that is there is a sticky error, and the node counts as absent.  [async]
+ * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES, words), CUDA; INVALID_ARG later. */
+int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* parents, int32_t window, int32_t* depth,
+                  uint32_t* bits, int32_t words, void* cuda_stream);
+
+/* misat_kv_append with norms of the queries' and the keys' heads before the rotation (each NULL: none),
+ * and with the positions of a tree's nodes (draft NULL: tokens in a row).  Nodes go into the slots of their
+ * numbers, absent ones at depth 0.  Errors as misat_kv_append's.  [async] */
+int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_head_norm* q_norm,
+                         const misat_head_norm* k_norm, const misat_kv_draft* draft, const void* k,
+                         int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                         int64_t v_head_stride, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                         void* q_out, int64_t qo_token_stride, int64_t qo_head_stride, void* cuda_stream);
+
+/* misat_kv_attend of a tree's nodes: a node sees the tokens before the tree (with a window those at positions
+ * above its own less the window) and the nodes of its bits.  An absent node gets zeros, and -infinity
+ * in lse.  kv_len below the new tokens leaves nodes below position zero, which see nothing.  As there, what only some nodes see has to be
+ * finite for all of them.  Errors as misat_kv_attend's.  [async] */
+int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_kv_draft* draft, const void* q,
+                         int64_t q_token_stride, int64_t q_head_stride, void* out, int64_t out_token_stride,
+                         int64_t out_head_stride, float* lse, void* cuda_stream);
+
+/* What is kept of the trees: for every sequence, keys and values of the nodes path[0] < path[1] < ... (the first
+ * n_keep of row b of path) move to the slots kv_len - new, kv_len - new + 1, ..., in place, and kv_len_out
+ * becomes kv_len - new + n_keep.  Where the path is a line of the tree these are the positions that the keys were rotated
+ * to.  The slots behind hold what they held.  A path that does not rise or leaves the tree is a sticky error: that
+ * sequence is left as it was.  No two rows of a batch may share the blocks of their new tokens.  kv_len_out must not be kv_len.
+ * [async]  Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES), CUDA; INVALID_ARG later. */
+int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path, int64_t path_stride,
+                  const int32_t* n_keep, int32_t* kv_len_out, void* cuda_stream);
+
 /* Wait for the stream and return the pool's sticky device error (0 if none), then clear it, and
  * what a call that ended early left in the workspace (INTERNAL if there is some without an error).
  * The pool's calls on other streams are to be finished.  [sync] */

@@ -26,8 +26,9 @@ CALLS = os.path.join(HERE, "_calls.so")
 CALLS_SOURCE = "torch_calls.cpp"
 CALLS_FOR = os.path.join(BUILD, "calls_for.txt")
 SOURCES = ["api.cu", "hash.cu", "probe.cu", "route.cu", "select.cu", "commit.cu", "evict.cu", "gindex.cu",
-           "overload.cu", "stage.cu", "rotary.cu", "kv.cu", "attend.cu"]
-HEADERS = ["common.cuh", "gindex.cuh", "kernels.h", "tick_scale.h", "kv.h", "runs.cuh", "tensor.cuh"]
+           "overload.cu", "stage.cu", "rotary.cu", "kv.cu", "attend.cu", "attend_tree.cu", "norm.cu", "tables.cu", "tree.cu"]
+HEADERS = ["common.cuh", "gindex.cuh", "kernels.h", "tick_scale.h", "kv.h", "runs.cuh", "tensor.cuh", "attend.cuh",
+           "rotary.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -7,6 +7,17 @@
 
 using namespace misat;
 
+namespace {
+
+bool attend_ok(const misat_kv* kv, const misat_kv_batch* batch, const void* q, int64_t q_ts, int64_t q_hs,
+               const void* out, int64_t o_ts, int64_t o_hs, const float* lse) {
+  return heads_ok(q, q_ts, q_hs, 2) && result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) &&
+         in_place_ok(q, q_ts, q_hs, out, o_ts, o_hs, batch->n_tokens, kv->hq) &&
+         (reinterpret_cast<uintptr_t>(lse) & 3) == 0 && on_device(kv->device);
+}
+
+}  // namespace
+
 extern "C" {
 
 int misat_kv_create(const misat_kv_config* c, misat_kv** out) {
@@ -60,10 +71,24 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
                     int64_t o_ts, int64_t o_hs, float* lse, int32_t window, void* cuda_stream) {
   if (!batch_ok(kv, batch) || window < 0) return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
-  if (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(out, o_ts, o_hs, 2, batch->n_tokens, kv->hq) ||
-      !in_place_ok(q, q_ts, q_hs, out, o_ts, o_hs, batch->n_tokens, kv->hq) || (reinterpret_cast<uintptr_t>(lse) & 3) || !on_device(kv->device))
+  if (!attend_ok(kv, batch, q, q_ts, q_hs, out, o_ts, o_hs, lse)) return MISAT_ERR_INVALID_ARG;
+  launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, window, nullptr,
+                static_cast<cudaStream_t>(cuda_stream));
+  return launch_status();
+}
+
+int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_kv_draft* draft, const void* q,
+                         int64_t q_ts, int64_t q_hs, void* out, int64_t o_ts, int64_t o_hs, float* lse,
+                         void* cuda_stream) {
+  if (!batch_ok(kv, batch) || !draft || draft->window < 0 || batch->max_q > MISAT_KV_TREE_NODES ||
+      draft->words != (batch->max_q + 31) / 32)
     return MISAT_ERR_INVALID_ARG;
-  launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, window,
+  if (batch->n_tokens == 0) return MISAT_OK;
+  if (!draft->depth || !draft->bits || draft->words == 0 ||
+      ((reinterpret_cast<uintptr_t>(draft->depth) | reinterpret_cast<uintptr_t>(draft->bits)) & 3) ||
+      !attend_ok(kv, batch, q, q_ts, q_hs, out, o_ts, o_hs, lse))
+    return MISAT_ERR_INVALID_ARG;
+  launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, draft->window, draft,
                 static_cast<cudaStream_t>(cuda_stream));
   return launch_status();
 }

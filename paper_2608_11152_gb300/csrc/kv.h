@@ -95,6 +95,12 @@ inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MISAT_OK
 // Maps of the attention kernel, and the pool's device memory; MISAT_OK or an error code.
 int attend_prepare(misat_kv* kv);
 void launch_attend(misat_kv* kv, const KvBatch& b, const Heads& q, const Heads& out, float* lse, int32_t window,
-                   cudaStream_t st);
+                   const misat_kv_draft* draft, cudaStream_t st);
+// The same kernel for trees of drafted tokens (attend_tree.cu).
+namespace runs {
+struct AttendArgs;
+}
+int attend_tree_prepare(const misat_kv* kv);
+void launch_attend_tree(const misat_kv* kv, const runs::AttendArgs& a, const CUtensorMap& map_q, cudaStream_t st);
 
 }  // namespace misat

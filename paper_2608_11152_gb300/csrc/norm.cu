@@ -1,0 +1,638 @@
+// Norm of each head with the rotation behind it, forward (into a tensor, or into blocks) and backward.
+//
+//   y = R_p (x r w),  r = 1 / sqrt(mean x^2 + eps)
+//   g = R_p^T dy,  a = g w,  dx = r (a - x r mean(a x r)),  dw = sum g x r          (w with its offset)
+//
+// One pass: a group of lanes holds a head of a token, so the sums over its elements are shuffles within the group and
+// the elements are read once.  A lane has the same unit of the same head (rotary's units: in the half layout two vectors
+// rot/2 apart or one past the rotated part, else one vector of whole pairs) of one token after the other: the weight,
+// and backward its gradient, stay in registers, and the tokens' cosines and sines come from shared memory, where they
+// are worked out once for all heads of the CTA.  Squares, sums and products are in 32 bits, results are rounded once.
+//
+// The weight's gradient is a sum over tokens (and heads): each CTA of a fixed grid writes the sum of its tokens, and a
+// second kernel adds these in order.
+#include <algorithm>
+#include <cmath>
+
+#include "kv.h"
+#include "rotary.cuh"
+
+using namespace misat;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTile = 32;   // tokens of a CTA at a time: their places are found by one warp
+constexpr int kMaxHead = 256;  // elements
+constexpr int kBackward = 2;   // CTAs of the gradient on an SM
+
+struct HeadWeight {
+  const void* p;  // nullptr: no norm
+  int64_t hs;
+  float eps, offset;
+  bool wide;  // 32 bits, else the tensor's type
+};
+
+struct NormArgs {
+  int32_t n_tokens, hq, hkv, d, rot;  // hkv = 0: plain rotation of hq heads
+  int32_t heads, first;               // rows of a token, and the first of them (queries, keys, values)
+  int32_t units, lane_bits, chunk, side, tile;  // lanes of a head; heads of a CTA, its tokens side by side and in all
+  int32_t turns;                      // 32-bit numbers of a token's cosines
+  FastDiv by_chunk;
+  const uint64_t* freq;
+  float attn, inv_d;
+  Heads x, out, k, v, dy;
+  HeadWeight wq, wk;
+  const int32_t* positions;
+  const int32_t* depth;
+  KvBatch b;
+  void* kb;
+  void* vb;
+  int32_t n_blocks;
+  int32_t* err;
+  float* parts;
+};
+
+// A lane's part of a head: UPL units of up to two vectors.
+template <class T, int VEC, bool HALF, int UPL>
+struct Part {
+  using V = Vec<T, VEC>;
+  static constexpr bool kPair = !HALF && VEC == 1;           // a unit is two neighbouring elements, moved one by one
+  static constexpr bool kTwo = HALF || kPair;                // a unit has a second vector
+  static constexpr int kStep = kPair ? 2 : VEC;              // elements a unit steps over
+  static constexpr int kPairs = HALF ? VEC : kPair ? 1 : VEC / 2;  // pairs of a unit
+  static constexpr int kElems = kTwo ? 2 * VEC : VEC;        // elements of a unit
+
+  int half, paired, units, d, lane, lanes;
+  __device__ __forceinline__ Part(const NormArgs& a, int lane)
+      : half(a.rot / 2), paired(HALF ? a.rot / 2 / VEC : (a.rot / 2 + kPairs - 1) / kPairs), units(a.units), d(a.d),
+        lane(lane), lanes(1 << a.lane_bits) {}
+
+  __device__ __forceinline__ int unit(int j) const { return lane + j * lanes; }
+  __device__ __forceinline__ bool has(int j) const { return unit(j) < units; }
+  // First element of a unit, and of its second vector.
+  __device__ __forceinline__ int first(int j) const {
+    return HALF && unit(j) >= paired ? (unit(j) + paired) * VEC : unit(j) * kStep;
+  }
+  __device__ __forceinline__ int second(int j) const { return HALF ? unit(j) * VEC + half : unit(j) * 2 + 1; }
+  __device__ __forceinline__ bool has_second(int j) const {
+    return HALF ? unit(j) < paired : kPair && unit(j) * 2 + 1 < d;
+  }
+  // Element i of a unit: the first vector's, then the second's.
+  __device__ __forceinline__ int element(int j, int i) const { return i < VEC ? first(j) + i : second(j) + i - VEC; }
+  __device__ __forceinline__ bool has_element(int j, int i) const { return has(j) && (i < VEC || has_second(j)); }
+
+  struct Raw {
+    V lo[UPL], hi[kTwo ? UPL : 1];
+  };
+  __device__ __forceinline__ void fetch(const T* p, Raw& r) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j) {
+      if (has(j)) r.lo[j] = *reinterpret_cast<const V*>(p + first(j));
+      if constexpr (kTwo)
+        if (has(j) && has_second(j)) r.hi[j] = *reinterpret_cast<const V*>(p + second(j));
+    }
+  }
+  __device__ __forceinline__ void put(T* p, const Raw& r) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j) {
+      if (has(j)) *reinterpret_cast<V*>(p + first(j)) = r.lo[j];
+      if constexpr (kTwo)
+        if (has(j) && has_second(j)) *reinterpret_cast<V*>(p + second(j)) = r.hi[j];
+    }
+  }
+  // In 32 bits; elements that are not there are zeros.
+  __device__ __forceinline__ void widen(const Raw& r, bool ok, float (&x)[UPL][kElems]) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j)
+#pragma unroll
+      for (int i = 0; i < kElems; ++i)
+        x[j][i] = ok && has_element(j, i) ? to_f(i < VEC ? r.lo[j].e[i] : r.hi[kTwo ? j : 0].e[i < VEC ? 0 : i - VEC])
+                                          : 0.f;
+  }
+  __device__ __forceinline__ void narrow(const float (&x)[UPL][kElems], Raw& r) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j)
+#pragma unroll
+      for (int i = 0; i < kElems; ++i) {
+        if (i < VEC) r.lo[j].e[i] = from_f<T>(x[j][i]);
+        else r.hi[kTwo ? j : 0].e[i - VEC] = from_f<T>(x[j][i]);
+      }
+  }
+
+  // Where pair p of a token's cosines is: eight of a unit are kept as two runs of four, so that neighbouring lanes
+  // read neighbouring 16 bytes.
+  static __device__ __forceinline__ int place(int p, int paired) {
+    if constexpr (kPairs == 8) return ((p % 8 / 4) * paired + p / 8) * 4 + p % 4;
+    else return p;
+  }
+  template <bool BACK>
+  __device__ __forceinline__ void turn_all(const float* cosines, const float* sines, float (&x)[UPL][kElems]) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j) {
+      if (unit(j) >= paired) continue;
+      alignas(16) float c[kPairs], s[kPairs];
+      if constexpr (kPairs >= 4) {
+#pragma unroll
+        for (int k = 0; k < kPairs; k += 4) {
+          const int at = place(unit(j) * kPairs + k, paired);
+          *reinterpret_cast<float4*>(c + k) = *reinterpret_cast<const float4*>(cosines + at);
+          *reinterpret_cast<float4*>(s + k) = *reinterpret_cast<const float4*>(sines + at);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+          c[k] = cosines[unit(j) * kPairs + k];
+          s[k] = sines[unit(j) * kPairs + k];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k) {
+        // The rotated part may end inside a vector: what is behind stays as it is (a product with zero would make
+        // NaN of an infinity).
+        if (!HALF && unit(j) * kPairs + k >= half) continue;
+        float& u = x[j][kTwo ? k : 2 * k];
+        float& w = x[j][kTwo ? VEC + k : 2 * k + 1];
+        const float a = u, b = w, sn = BACK ? -s[k] : s[k];
+        u = a * c[k] - b * sn;
+        w = a * sn + b * c[k];
+      }
+    }
+  }
+  __device__ __forceinline__ void load_weight(const HeadWeight& w, int head, float (&out)[UPL][kElems]) const {
+    const int64_t at = (int64_t)head * w.hs;
+#pragma unroll
+    for (int j = 0; j < UPL; ++j)
+#pragma unroll
+      for (int i = 0; i < kElems; ++i) {
+        out[j][i] = 1.f;
+        if (w.p && has_element(j, i))
+          out[j][i] = w.offset + (w.wide ? static_cast<const float*>(w.p)[at + element(j, i)]
+                                         : to_f(static_cast<const T*>(w.p)[at + element(j, i)]));
+      }
+  }
+  __device__ __forceinline__ float sum(float v) const {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
+};
+
+// The tile's cosines and sines: [tokens][2][turns].
+template <class P>
+__device__ __forceinline__ void fill_turns(const NormArgs& a, int nt, int paired, const int32_t* pos, float* out) {
+  const int half = a.rot / 2;
+  for (int i = threadIdx.x; i < nt * half; i += blockDim.x) {
+    const int t = i / half, p = i - t * half;
+    const float2 cs = turn(pos[t], __ldg(a.freq + p), a.attn, false);
+    float* o = out + (int64_t)t * 2 * a.turns + P::place(p, paired);
+    o[0] = cs.x;
+    o[a.turns] = cs.y;
+  }
+}
+
+template <class T, int VEC, bool HALF, int UPL>
+__global__ void __launch_bounds__(kThreads, 3) k_norm_rotate(const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) float s_turn[];
+  __shared__ int32_t s_pos[kMaxTile];
+  __shared__ int64_t s_slot[kMaxTile];  // element offset of the token's row of kv head 0, -1: skip
+  using P = Part<T, VEC, HALF, UPL>;
+  const int tid = threadIdx.x, group = tid >> a.lane_bits, side = a.by_chunk.div(group);
+  const P part(a, tid & ((1 << a.lane_bits) - 1));
+  const int t0 = blockIdx.x * a.tile, nt = min(a.tile, a.n_tokens - t0);
+  const int h = a.first + blockIdx.y * a.chunk + group - side * a.chunk;
+  const bool mine = side < a.side && h < a.first + a.heads;
+  const bool q = h < a.hq, k = h < a.hq + a.hkv;
+  const Heads& src = q ? a.x : k ? a.k : a.v;
+  const int hh = q ? h : k ? h - a.hq : h - a.hq - a.hkv;
+  const T* in = static_cast<const T*>(src.p) + (int64_t)t0 * src.ts + (int64_t)hh * src.hs;
+  chain_wait();
+  typename P::Raw next;
+  if (mine && side < nt) part.fetch(in + side * src.ts, next);
+  const HeadWeight& hw = q ? a.wq : a.wk;
+  const bool normed = k && hw.p;
+  float w[UPL][P::kElems];
+  if (normed && mine) part.load_weight(hw, hh, w);
+  if (a.hkv == 0) {
+    if (tid < nt) {
+      s_pos[tid] = __ldcg(a.positions + t0 + tid);
+      s_slot[tid] = 0;
+    }
+  } else if (tid < 32) {
+    const int t = t0 + min(tid, nt - 1);
+    OffsetFinder find(a.b.q_off, a.b.n, t0);
+    const int b = find(t);
+    const int from = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
+    const int64_t pos = (int64_t)len - end + t;
+    const bool ok = from <= t && t < end && end - from <= a.b.max_q && len >= end - from && pos >= 0 &&
+                    len <= kMaxLen && pos < a.b.stride * kBlockTokens;
+    int64_t at = -1;
+    if (ok) {
+      const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
+      if (blk >= 0 && blk < a.n_blocks) at = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
+    }
+    if (tid < nt) {
+      if (at < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
+      s_pos[tid] = a.depth ? len - (end - from) + __ldcg(a.depth + t) : (int32_t)pos;
+      s_slot[tid] = at;
+    }
+  }
+  __syncthreads();
+  fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
+  __syncthreads();
+  for (int base = 0; base < nt; base += a.side) {
+    const int t = base + side;
+    const bool ok = mine && t < nt;
+    typename P::Raw raw = next;
+    if (mine && t + a.side < nt) part.fetch(in + (int64_t)(t + a.side) * src.ts, next);
+    float x[UPL][P::kElems];
+    part.widen(raw, ok, x);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < UPL; ++j)
+#pragma unroll
+      for (int i = 0; i < P::kElems; ++i) sum = fmaf(x[j][i], x[j][i], sum);
+    sum = part.sum(sum);
+    if (!ok || s_slot[t] < 0) continue;
+    if (k) {
+      if (normed) {
+        const float r = rsqrtf(fmaf(sum, a.inv_d, hw.eps));
+#pragma unroll
+        for (int j = 0; j < UPL; ++j)
+#pragma unroll
+          for (int i = 0; i < P::kElems; ++i) x[j][i] = x[j][i] * r * w[j][i];
+      }
+      const float* cs = s_turn + t * 2 * a.turns;
+      part.template turn_all<false>(cs, cs + a.turns, x);
+      part.narrow(x, raw);
+    }
+    T* o = q ? static_cast<T*>(a.out.p) + (int64_t)(t0 + t) * a.out.ts + (int64_t)h * a.out.hs
+             : static_cast<T*>(k ? a.kb : a.vb) + s_slot[t] + (int64_t)hh * kBlockTokens * a.d;
+    part.put(o, raw);
+  }
+}
+
+template <class T, int VEC, bool HALF, int UPL>
+__global__ void __launch_bounds__(kThreads, kBackward) k_norm_backward(const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) float s_turn[];
+  __shared__ int32_t s_pos[kMaxTile];
+  using P = Part<T, VEC, HALF, UPL>;
+  const int tid = threadIdx.x, group = tid >> a.lane_bits, side = a.by_chunk.div(group);
+  const P part(a, tid & ((1 << a.lane_bits) - 1));
+  const int h = blockIdx.y * a.chunk + group - side * a.chunk;
+  const bool mine = side < a.side && h < a.heads;
+  const int tiles = (a.n_tokens + a.tile - 1) / a.tile;
+  chain_wait();
+  float w[UPL][P::kElems], dw[UPL][P::kElems];
+#pragma unroll
+  for (int j = 0; j < UPL; ++j)
+#pragma unroll
+    for (int i = 0; i < P::kElems; ++i) dw[j][i] = 0.f;
+  if (mine) part.load_weight(a.wq, h, w);
+  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int t0 = tile * a.tile, nt = min(a.tile, a.n_tokens - t0);
+    const T* x_in = static_cast<const T*>(a.x.p) + (int64_t)t0 * a.x.ts + (int64_t)h * a.x.hs;
+    const T* g_in = static_cast<const T*>(a.dy.p) + (int64_t)t0 * a.dy.ts + (int64_t)h * a.dy.hs;
+    typename P::Raw next_x, next_g;
+    if (mine && side < nt) {
+      part.fetch(x_in + side * a.x.ts, next_x);
+      part.fetch(g_in + side * a.dy.ts, next_g);
+    }
+    if (tid < nt) s_pos[tid] = __ldcg(a.positions + t0 + tid);
+    __syncthreads();
+    fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
+    __syncthreads();
+    for (int base = 0; base < nt; base += a.side) {
+      const int t = base + side;
+      const bool ok = mine && t < nt;
+      typename P::Raw raw_x = next_x, raw_g = next_g;
+      if (mine && t + a.side < nt) {
+        part.fetch(x_in + (int64_t)(t + a.side) * a.x.ts, next_x);
+        part.fetch(g_in + (int64_t)(t + a.side) * a.dy.ts, next_g);
+      }
+      float x[UPL][P::kElems], g[UPL][P::kElems];
+      part.widen(raw_x, ok, x);
+      part.widen(raw_g, ok, g);
+      const float* cs = s_turn + (ok ? t : 0) * 2 * a.turns;
+      part.template turn_all<true>(cs, cs + a.turns, g);
+      float squares = 0.f, dot = 0.f;
+#pragma unroll
+      for (int j = 0; j < UPL; ++j)
+#pragma unroll
+        for (int i = 0; i < P::kElems; ++i) {
+          squares = fmaf(x[j][i], x[j][i], squares);
+          if (part.has_element(j, i)) dot = fmaf(g[j][i] * w[j][i], x[j][i], dot);
+        }
+      squares = part.sum(squares);
+      dot = part.sum(dot);
+      if (!ok) continue;
+      const float r = rsqrtf(fmaf(squares, a.inv_d, a.wq.eps)), m = r * dot * a.inv_d;
+#pragma unroll
+      for (int j = 0; j < UPL; ++j)
+#pragma unroll
+        for (int i = 0; i < P::kElems; ++i) {
+          const float u = x[j][i] * r;
+          dw[j][i] = fmaf(g[j][i], u, dw[j][i]);
+          x[j][i] = r * fmaf(-u, m, g[j][i] * w[j][i]);
+        }
+      part.narrow(x, raw_x);
+      part.put(static_cast<T*>(a.out.p) + (int64_t)(t0 + t) * a.out.ts + (int64_t)h * a.out.hs, raw_x);
+    }
+    __syncthreads();  // the next tile's turns come where these were read
+  }
+  // The CTA's sum: over its tokens side by side, and over its heads where they share the weight.
+  float* red = s_turn;  // [groups][d]
+  if (mine) {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j)
+#pragma unroll
+      for (int i = 0; i < P::kElems; ++i)
+        if (part.has_element(j, i)) red[group * a.d + part.element(j, i)] = dw[j][i];
+  }
+  __syncthreads();
+  const int heads = min(a.chunk, a.heads - (int)blockIdx.y * a.chunk);  // of this CTA
+  if (a.wq.hs == 0) {
+    for (int e = tid; e < a.d; e += blockDim.x) {
+      float v = 0.f;
+      for (int s = 0; s < a.side; ++s)
+        for (int i = 0; i < heads; ++i) v += red[(s * a.chunk + i) * a.d + e];
+      a.parts[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.d + e] = v;
+    }
+  } else {
+    for (int i = tid; i < heads * a.d; i += blockDim.x) {
+      float v = 0.f;
+      for (int s = 0; s < a.side; ++s) v += red[s * a.chunk * a.d + i];
+      a.parts[(int64_t)blockIdx.x * a.heads * a.d + (int64_t)blockIdx.y * a.chunk * a.d + i] = v;
+    }
+  }
+}
+
+// The weight's gradient: the parts of each element, in order.
+constexpr int kSumCols = 32, kSumRows = 8;
+struct SumArgs {
+  const float* parts;
+  void* out;
+  int64_t hs;
+  int32_t n_parts, cols, d, dtype;
+};
+__global__ void __launch_bounds__(kSumCols * kSumRows) k_norm_weight(const __grid_constant__ SumArgs a) {
+  __shared__ float s[kSumRows][kSumCols];
+  chain_wait();
+  const int c = blockIdx.x * kSumCols + threadIdx.x % kSumCols, row = threadIdx.x / kSumCols;
+  float v = 0.f;
+  if (c < a.cols)
+#pragma unroll 8
+    for (int p = row; p < a.n_parts; p += kSumRows) v += __ldcg(a.parts + (int64_t)p * a.cols + c);
+  s[row][threadIdx.x % kSumCols] = v;
+  __syncthreads();
+  if (row == 0 && c < a.cols) {
+#pragma unroll
+    for (int i = 1; i < kSumRows; ++i) v += s[i][threadIdx.x];
+    const int64_t at = (int64_t)(c / a.d) * a.hs + c % a.d;
+    if (a.dtype == MISAT_F32) static_cast<float*>(a.out)[at] = v;
+    else if (a.dtype == MISAT_BF16) static_cast<__nv_bfloat16*>(a.out)[at] = from_f<__nv_bfloat16>(v);
+    else static_cast<__half*>(a.out)[at] = from_f<__half>(v);
+  }
+}
+
+struct Grid {
+  int x, y, threads;
+  size_t smem;
+  bool vec;
+  int upl;
+};
+
+// How heads and tokens are laid over lanes and CTAs.
+Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int num_sms) {
+  const int n = 16 / elem;
+  Grid g{};
+  g.vec = vec;
+  if (vec) a.units = half_layout ? a.rot / 2 / n + (a.d - a.rot) / n : a.d / n;
+  else a.units = half_layout ? a.d - a.rot / 2 : (a.d + 1) / 2;
+  g.upl = vec ? (a.units > 32 ? 2 : 1) : 8;
+  a.lane_bits = 0;
+  while ((g.upl << a.lane_bits) < a.units) ++a.lane_bits;
+  // All heads of a token in one CTA where they fit, else equal parts of them; the rest of the CTA takes other tokens.
+  const int slots = kThreads >> a.lane_bits, chunks = (a.heads + slots - 1) / slots;
+  a.chunk = (a.heads + chunks - 1) / chunks;
+  a.side = std::min(slots / a.chunk, kMaxTile);
+  a.by_chunk.set(a.chunk);
+  g.y = (a.heads + a.chunk - 1) / a.chunk;
+  g.threads = ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
+  // As many tokens a CTA as leave several CTAs for each SM.
+  a.tile = a.side;
+  while (a.tile * 2 <= kMaxTile && (int64_t)((a.n_tokens - 1) / (a.tile * 2) + 1) * g.y >= (int64_t)num_sms * 8)
+    a.tile *= 2;
+  g.x = (a.n_tokens - 1) / a.tile + 1;
+  if (backward) g.x = std::min(g.x, std::max(1, num_sms * kBackward / g.y));
+  const int pairs = vec ? (half_layout ? n : n / 2) : 1;
+  a.turns = (a.rot / 2 + pairs - 1) / pairs * pairs;
+  g.smem = sizeof(float) * 2 * a.turns * a.tile;
+  if (backward) g.smem = std::max(g.smem, sizeof(float) * a.side * a.chunk * a.d);
+  return g;
+}
+
+// Whole 16-byte vectors wherever every row starts on such a boundary and no vector straddles the end of a head or
+// (half layout) of the rotated halves.
+bool whole_vectors(const NormArgs& a, int elem, bool half_layout) {
+  const int n = 16 / elem;
+  return aligned16(a.x, elem) && aligned16(a.out, elem) && aligned16(a.k, elem) && aligned16(a.v, elem) &&
+         aligned16(a.dy, elem) && a.d % n == 0 && (!half_layout || a.rot / 2 % n == 0);
+}
+
+template <class... P, class... A>
+void launch(void (*kernel)(P...), const Grid& g, cudaStream_t st, A&&... args) {
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(g.x, g.y);
+  lc.blockDim = dim3(g.threads);
+  lc.dynamicSmemBytes = g.smem;
+  lc.stream = st;
+  lc.attrs = &at;
+  lc.numAttrs = 1;
+  cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
+}
+
+template <class T, int VEC, int UPL>
+void launch_part(const NormArgs& a, const Grid& g, bool half_layout, bool backward, cudaStream_t st) {
+  if (backward) {
+    if (half_layout) launch(k_norm_backward<T, VEC, true, UPL>, g, st, a);
+    else launch(k_norm_backward<T, VEC, false, UPL>, g, st, a);
+  } else {
+    if (half_layout) launch(k_norm_rotate<T, VEC, true, UPL>, g, st, a);
+    else launch(k_norm_rotate<T, VEC, false, UPL>, g, st, a);
+  }
+}
+template <class T>
+void launch_t(const NormArgs& a, const Grid& g, bool half_layout, bool backward, cudaStream_t st) {
+  constexpr int VEC = 16 / sizeof(T);
+  if (!g.vec) return launch_part<T, 1, 8>(a, g, half_layout, backward, st);
+  if constexpr (sizeof(T) == 4)
+    if (g.upl == 2) return launch_part<T, VEC, 2>(a, g, half_layout, backward, st);
+  launch_part<T, VEC, 1>(a, g, half_layout, backward, st);
+}
+void launch_norm(const NormArgs& a, const Grid& g, int dtype, bool half_layout, bool backward, cudaStream_t st) {
+  if (dtype == MISAT_BF16) launch_t<__nv_bfloat16>(a, g, half_layout, backward, st);
+  else if (dtype == MISAT_F16) launch_t<__half>(a, g, half_layout, backward, st);
+  else launch_t<float>(a, g, half_layout, backward, st);
+}
+
+bool norm_ok(const misat_head_norm* n, int dtype, int heads, int d) {
+  if (!n) return false;
+  const bool empty = n->head_stride != 0 && heads == 0;
+  return (n->weight || empty) && (n->dtype == dtype || n->dtype == MISAT_F32) &&
+         (n->head_stride == 0 || n->head_stride >= d) && n->eps > 0 && std::isfinite(n->eps) && std::isfinite(n->offset) &&
+         reinterpret_cast<uintptr_t>(n->weight) % (n->dtype == MISAT_F32 ? 4 : 2) == 0;
+}
+HeadWeight weight_of(const misat_head_norm* n) {
+  if (!n) return {};
+  return {n->weight, n->head_stride, n->eps, n->offset, n->dtype == MISAT_F32};
+}
+
+bool sizes_ok(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens, int32_t n_heads,
+              int32_t head_dim) {
+  return r && dtype >= MISAT_BF16 && dtype <= MISAT_F32 && n_tokens >= 0 && n_heads >= 0 && n_heads <= 65535 &&
+         head_dim >= r->rot && head_dim <= kMaxHead && norm_ok(norm, dtype, n_heads, head_dim);
+}
+NormArgs rotary_args(const misat_rope* r, const misat_head_norm* norm, int32_t n_tokens, int32_t n_heads,
+                     int32_t head_dim) {
+  NormArgs a{};
+  a.n_tokens = n_tokens;
+  a.hq = a.heads = n_heads;
+  a.d = head_dim;
+  a.inv_d = 1.f / (float)head_dim;
+  a.rot = r->rot;
+  a.freq = r->freq;
+  a.attn = r->attn;
+  a.wq = weight_of(norm);
+  return a;
+}
+// Parts of the weight's gradient, and elements of one.
+int64_t parts_of(const NormArgs& a, const Grid& g) { return a.wq.hs == 0 ? (int64_t)g.x * g.y : g.x; }
+int64_t part_size(const NormArgs& a) { return a.wq.hs == 0 ? a.d : (int64_t)a.heads * a.d; }
+
+}  // namespace
+
+extern "C" {
+
+int misat_norm_rotary(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                      int32_t n_heads, int32_t head_dim, const void* x, int64_t x_ts, int64_t x_hs,
+                      const int32_t* positions, void* out, int64_t o_ts, int64_t o_hs, void* cuda_stream) {
+  if (!sizes_ok(r, norm, dtype, n_tokens, n_heads, head_dim)) return MISAT_ERR_INVALID_ARG;
+  if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
+  const int elem = dtype == MISAT_F32 ? 4 : 2;
+  if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions ||
+      !in_place_ok(x, x_ts, x_hs, out, o_ts, o_hs, n_tokens, n_heads) || !on_device(r->device))
+    return MISAT_ERR_INVALID_ARG;
+  NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
+  a.x = {const_cast<void*>(x), x_ts, x_hs};
+  a.out = {out, o_ts, o_hs};
+  a.positions = positions;
+  const bool half = r->layout == MISAT_ROPE_HALF;
+  const Grid g = plan(a, elem, half, whole_vectors(a, elem, half), false, r->num_sms);
+  launch_norm(a, g, dtype, half, false, static_cast<cudaStream_t>(cuda_stream));
+  return launch_status();
+}
+
+int misat_norm_rotary_work(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                           int32_t n_heads, int32_t head_dim, int64_t* bytes) {
+  if (!sizes_ok(r, norm, dtype, n_tokens, n_heads, head_dim) || !bytes) return MISAT_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
+  // The larger of the two layouts: which one it will be depends on the tensors' addresses.
+  for (const bool vec : {false, true}) {
+    NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
+    const bool half = r->layout == MISAT_ROPE_HALF;
+    const int elem = dtype == MISAT_F32 ? 4 : 2;
+    if (vec && !whole_vectors(a, elem, half)) continue;
+    const Grid g = plan(a, elem, half, vec, true, r->num_sms);
+    *bytes = std::max(*bytes, parts_of(a, g) * part_size(a) * (int64_t)sizeof(float));
+  }
+  return MISAT_OK;
+}
+
+int misat_norm_rotary_backward(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
+                               int32_t n_heads, int32_t head_dim, const void* x, int64_t x_ts, int64_t x_hs,
+                               const void* grad, int64_t g_ts, int64_t g_hs, const int32_t* positions, void* dx,
+                               int64_t dx_ts, int64_t dx_hs, void* dweight, int64_t dw_hs, void* work,
+                               int64_t work_bytes, void* cuda_stream) {
+  if (!sizes_ok(r, norm, dtype, n_tokens, n_heads, head_dim) ||
+      (!dweight && (n_heads > 0 || norm->head_stride == 0)) || (norm->head_stride && dw_hs < head_dim) ||
+      reinterpret_cast<uintptr_t>(dweight) % (norm->dtype == MISAT_F32 ? 4 : 2) || !on_device(r->device))
+    return MISAT_ERR_INVALID_ARG;
+  const int elem = dtype == MISAT_F32 ? 4 : 2;
+  const bool none = n_tokens == 0 || n_heads == 0;
+  if (!none && (!heads_ok(x, x_ts, x_hs, elem) || !heads_ok(grad, g_ts, g_hs, elem) ||
+                !result_ok(dx, dx_ts, dx_hs, elem, n_tokens, n_heads) || !positions ||
+                !in_place_ok(x, x_ts, x_hs, dx, dx_ts, dx_hs, n_tokens, n_heads) ||
+                !in_place_ok(grad, g_ts, g_hs, dx, dx_ts, dx_hs, n_tokens, n_heads) ||
+                (reinterpret_cast<uintptr_t>(work) & 15)))
+    return MISAT_ERR_INVALID_ARG;
+  NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  SumArgs s{static_cast<const float*>(work), dweight, norm->head_stride ? dw_hs : 0, 0, (int32_t)part_size(a), head_dim, norm->dtype};
+  if (!none) {
+    a.x = {const_cast<void*>(x), x_ts, x_hs};
+    a.dy = {const_cast<void*>(grad), g_ts, g_hs};
+    a.out = {dx, dx_ts, dx_hs};
+    a.positions = positions;
+    a.parts = static_cast<float*>(work);
+    const bool half = r->layout == MISAT_ROPE_HALF;
+    const Grid g = plan(a, elem, half, whole_vectors(a, elem, half), true, r->num_sms);
+    s.n_parts = (int32_t)parts_of(a, g);
+    if (!work || work_bytes < parts_of(a, g) * part_size(a) * (int64_t)sizeof(float)) return MISAT_ERR_INVALID_ARG;
+    launch_norm(a, g, dtype, half, true, st);
+  }
+  if (s.cols > 0) launch_chained(k_norm_weight, (s.cols + kSumCols - 1) / kSumCols, kSumCols * kSumRows, 0, st, s);
+  return launch_status();
+}
+
+int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_head_norm* q_norm,
+                         const misat_head_norm* k_norm, const misat_kv_draft* draft, const void* k, int64_t k_ts,
+                         int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs, const void* q, int64_t q_ts,
+                         int64_t q_hs, void* q_out, int64_t qo_ts, int64_t qo_hs, void* cuda_stream) {
+  if (!batch_ok(kv, batch) || (q_norm && !norm_ok(q_norm, kv->dtype, kv->hq, kv->d)) ||
+      (k_norm && !norm_ok(k_norm, kv->dtype, kv->hkv, kv->d)))
+    return MISAT_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0) return MISAT_OK;
+  if (!heads_ok(k, k_ts, k_hs, 2) || !heads_ok(v, v_ts, v_hs, 2) || (draft && !draft->depth))
+    return MISAT_ERR_INVALID_ARG;
+  if (q && (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(q_out, qo_ts, qo_hs, 2, batch->n_tokens, kv->hq) ||
+            !in_place_ok(q, q_ts, q_hs, q_out, qo_ts, qo_hs, batch->n_tokens, kv->hq)))
+    return MISAT_ERR_INVALID_ARG;
+  if (!on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
+  NormArgs a{};
+  a.n_tokens = batch->n_tokens;
+  a.hq = kv->hq;
+  a.hkv = kv->hkv;
+  a.first = q ? 0 : kv->hq;
+  a.heads = (q ? kv->hq : 0) + 2 * kv->hkv;
+  a.d = kv->d;
+  a.inv_d = 1.f / (float)kv->d;
+  a.attn = 1.f;
+  a.x = {const_cast<void*>(q), q_ts, q_hs};
+  if (q) a.out = {q_out, qo_ts, qo_hs};
+  a.k = {const_cast<void*>(k), k_ts, k_hs};
+  a.v = {const_cast<void*>(v), v_ts, v_hs};
+  a.wq = weight_of(q_norm);
+  a.wk = weight_of(k_norm);
+  bool half = true;
+  if (kv->rope) {
+    a.rot = kv->rope->rot;
+    a.freq = kv->rope->freq;
+    a.attn = kv->rope->attn;
+    half = kv->rope->layout == MISAT_ROPE_HALF;
+  }
+  a.depth = draft ? draft->depth : nullptr;
+  a.b = batch_view(batch);
+  a.kb = kv->kb;
+  a.vb = kv->vb;
+  a.n_blocks = kv->n_blocks;
+  a.err = kv->err;
+  const Grid g = plan(a, 2, half, whole_vectors(a, 2, half), false, kv->num_sms);
+  launch_norm(a, g, kv->dtype, half, false, static_cast<cudaStream_t>(cuda_stream));
+  return launch_status();
+}
+
+}  // extern "C"

@@ -18,6 +18,7 @@
 #include <new>
 
 #include "kv.h"
+#include "rotary.cuh"
 
 using namespace misat;
 
@@ -26,16 +27,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTok = 8;    // tokens of a CTA, a warp each
 constexpr int kHeads = 4;     // heads of a token that a thread goes through, at least, where there are many tokens
-
-// n / d for n * d < 2^32: m = ceil(2^32 / d) (d = 1 would need 33 bits and is the identity).
-struct FastDiv {
-  uint32_t d, m;
-  void set(uint32_t v) {
-    d = v;
-    m = v > 1 ? (uint32_t)((((uint64_t)1 << 32) + v - 1) / v) : 0;
-  }
-  __device__ __forceinline__ uint32_t div(uint32_t n) const { return d == 1 ? n : __umulhi(n, m); }
-};
 
 struct RotArgs {
   int32_t n_tokens, hq, hkv, d, rot;  // hkv = 0: plain rotation of hq heads
@@ -51,67 +42,6 @@ struct RotArgs {
   void* vb;
   int32_t n_blocks;
   int32_t* err;
-};
-
-template <class T>
-__device__ __forceinline__ float to_f(T x);
-template <>
-__device__ __forceinline__ float to_f(float x) { return x; }
-template <>
-__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-template <>
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <class T>
-__device__ __forceinline__ T from_f(float x);
-template <>
-__device__ __forceinline__ float from_f(float x) { return x; }
-template <>
-__device__ __forceinline__ __half from_f(float x) { return __float2half_rn(x); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
-
-// cos and sin of (pos * freq / 2^64) turns.  The nearest quarter turn is taken off in whole
-// numbers; what is left, within an eighth of a turn, goes to a 32-bit float with 24 good bits.
-__device__ __forceinline__ float2 turn(int32_t pos, uint64_t freq, float attn, bool backward) {
-  const uint32_t ph = (uint32_t)(((uint64_t)(int64_t)pos * freq) >> 32);
-  const uint32_t quarter = (ph + 0x20000000u) >> 30;
-  const int32_t rest = (int32_t)(ph - (quarter << 30));
-  float s, c;
-  sincospif((float)rest * 0x1p-31f, &s, &c);
-  if (quarter & 1) {
-    const float t = c;
-    c = -s;
-    s = t;
-  }
-  if (quarter & 2) {
-    c = -c;
-    s = -s;
-  }
-  if (backward) s = -s;
-  return make_float2(c * attn, s * attn);
-}
-
-// The sequence of token t: the last b in [0, n) with q_off[b] <= t, found by a warp 32 offsets at
-// a time (two rounds for 1,024 sequences; each round is one memory latency).  Bounded for
-// malformed offsets: the range shrinks in every round.
-__device__ __forceinline__ int find_sequence(const int32_t* q_off, int n, int t, int lane) {
-  int lo = 0, hi = n;  // the answer is in [lo, hi)
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32;
-    const int i = lo + lane * step;
-    const bool le = i < hi && (i == lo || __ldcg(q_off + i) <= t);
-    const unsigned m = __ballot_sync(0xffffffffu, le);
-    const int last = 31 - __clz(m);  // lane 0 always holds
-    lo += last * step;
-    hi = min(hi, lo + step);
-  }
-  return lo;
-}
-
-// VEC elements of T at p; VEC * sizeof(T) is 16 and p aligned to it, or VEC is 1.
-template <class T, int VEC>
-struct alignas(VEC * sizeof(T)) Vec {
-  T e[VEC];
 };
 
 template <class T, int VEC, bool HALF>

@@ -28,6 +28,9 @@ struct AttendArgs {
   float2* ws_ml; // [slots][128 rows]: m, l
   unsigned* ctr; // [2 x CTAs] arrivals of split items, zero between calls
   int32_t* err;
+  const uint32_t* bits;  // of a tree's nodes, [tokens][words]; nullptr: tokens in a row
+  const int32_t* depth;
+  int32_t words;
 };
 
 // ---- what there is to do ----
@@ -56,7 +59,8 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const AttendArgs& a, const Seq& s, int t0, int nt) {
   const int p0 = s.len - s.n + t0, to = max(p0 + nt, 0);
-  const int from = a.window > 0 && p0 >= a.window ? p0 - a.window + 1 : 0;
+  const int first = a.bits ? p0 - t0 : p0;  // the first position: any node of a tree may be a root
+  const int from = a.window > 0 && first >= a.window ? first - a.window + 1 : 0;
   const int jb = from / kKeys;
   return {from, to, jb, to > 0 ? (to + kKeys - 1) / kKeys - jb : 0};
 }

@@ -7,12 +7,14 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <sstream>
+#include <vector>
 
 #include "../../include/misat.h"
 
@@ -33,10 +35,26 @@ struct Pool {
   cudaStream_t last;  // of the last call outside a capture
   bool called;
 };
+// Tensors that a call made for later ones: these may run on another stream.
+struct Made {
+  cudaStream_t on;
+  std::vector<at::Tensor> tensors;
+};
 struct Batch {
   misat_kv_batch b;
   int64_t hq, hkv, d;
   c10::DeviceIndex device;
+  Made made{};
+};
+struct Tree {
+  misat_kv_draft d;
+  int64_t n_tokens, max_q;
+  c10::DeviceIndex device;
+  Made made;
+};
+struct Norm {
+  at::Tensor w;  // [head_dim] or [heads][head_dim]
+  float eps, offset;
 };
 
 template <class S>
@@ -98,6 +116,41 @@ at::Tensor fresh(at::IntArrayRef size, at::ScalarType dtype, c10::DeviceIndex de
 void written(const at::Tensor& t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
+// A contiguous tensor of whole numbers.
+template <class I = int32_t>
+I* ints(const at::Tensor& t, const char* name, c10::DeviceIndex device, std::initializer_list<int64_t> size) {
+  constexpr bool kWide = sizeof(I) == 8;
+  if (t.scalar_type() != (kWide ? at::kLong : at::kInt) || !t.is_cuda() || t.get_device() != device ||
+      !t.sizes().equals(size) || !t.is_contiguous()) {
+    std::ostringstream s;
+    s << "contiguous " << (kWide ? "int64 " : "int32 ") << at::IntArrayRef(size) << " on cuda:" << (int)device;
+    refuse(name, s.str(), t);
+  }
+  return t.data_ptr<I>();
+}
+// A block table [n][columns]: its columns.
+int64_t table_columns(const at::Tensor& t, c10::DeviceIndex device, int64_t n, int64_t& stride) {
+  const bool shaped = t.scalar_type() == at::kInt && t.is_cuda() && t.get_device() == device && t.dim() == 2 &&
+                      t.size(0) == n;
+  const int64_t columns = shaped ? t.size(1) : 0;
+  stride = shaped && n > 1 ? t.stride(0) : columns;
+  if (!shaped || (columns > 1 && t.stride(1) != 1) || stride < columns)
+    refuse("block_table",
+           "int32 [" + std::to_string(n) + ", blocks] on cuda:" + std::to_string((int)device) +
+               " with contiguous rows that do not overlap",
+           t);
+  return columns;
+}
+int32_t int32_of(PyObject* o, const char* name) {
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Raised{};
+  if (v < INT32_MIN || v > INT32_MAX) {
+    PyErr_Format(PyExc_ValueError, "%s: beyond 32 bits", name);
+    throw Raised{};
+  }
+  return (int32_t)v;
+}
+
 int code_of(at::ScalarType t) {
   return t == at::kBFloat16 ? MISAT_BF16 : t == at::kHalf ? MISAT_F16 : t == at::kFloat ? MISAT_F32 : -1;
 }
@@ -175,22 +228,11 @@ PyObject* batch_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const Pool* p = state<Pool>(a[0]);
   if (!p) return nullptr;
   const at::Tensor &off = tensor(a[1], "q_off"), &len = tensor(a[2], "kv_len"), &table = tensor(a[3], "block_table");
-  const int64_t seqs = len.dim() == 1 ? len.size(0) : -1;
-  auto ints = [&](const at::Tensor& t, const char* name, int64_t size) {
-    if (t.scalar_type() != at::kInt || !t.is_cuda() || t.get_device() != p->device || t.dim() != 1 || size < 0 ||
-        t.size(0) != size || !t.is_contiguous())
-      refuse(name, "contiguous int32 [" + std::to_string(size) + "] on cuda:" + std::to_string((int)p->device), t);
-  };
-  ints(len, "kv_len", seqs);
-  ints(off, "q_off", seqs + 1);
-  const bool shaped = table.scalar_type() == at::kInt && table.is_cuda() && table.get_device() == p->device &&
-                      table.dim() == 2 && table.size(0) == seqs;
-  const int64_t blocks = shaped ? table.size(1) : 0, stride = shaped && seqs > 1 ? table.stride(0) : blocks;
-  if (!shaped || (blocks > 1 && table.stride(1) != 1) || stride < blocks)
-    refuse("block_table",
-           "int32 [" + std::to_string(seqs) + ", blocks] on cuda:" + std::to_string((int)p->device) +
-               " with contiguous rows that do not overlap",
-           table);
+  const int64_t seqs = len.dim() == 1 ? len.size(0) : 0;
+  int64_t stride;
+  ints(len, "kv_len", p->device, {seqs});
+  ints(off, "q_off", p->device, {seqs + 1});
+  table_columns(table, p->device, seqs, stride);
   const long long tokens = PyLong_AsLongLong(a[4]), max_q = PyLong_AsLongLong(a[5]);
   if (PyErr_Occurred()) return nullptr;
   if (seqs > INT32_MAX || tokens < INT32_MIN || tokens > INT32_MAX || max_q < INT32_MIN || max_q > INT32_MAX)
@@ -200,6 +242,13 @@ PyObject* batch_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
           p->hq, p->hkv, p->d, p->device};
   return new_state(b);
   MISAT_END
+}
+
+// A later call on the tensors that an earlier one made: their memory is not used again before it is finished.
+void used(const Made& m, cudaStream_t st) {
+  if (m.tensors.empty() || m.on == st || capturing(st)) return;
+  for (const at::Tensor& t : m.tensors)
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), c10::cuda::getCurrentCUDAStream(t.get_device()));
 }
 
 // (rope, x, positions, out or None, backward) -> out
@@ -257,11 +306,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     out = given ? heads(a[5], "q_out", p->dtype, p->device, T, p->hq, p->d)
                 : fresh({T, p->hq, p->d}, p->dtype, p->device);
   }
+  const cudaStream_t st = ordered(p);
   const int rc = misat_kv_append(p->h, &b->b, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                                  v.stride(1), has_q ? q.data_ptr() : nullptr, has_q ? q.stride(0) : 0,
                                  has_q ? q.stride(1) : 0, has_q ? out.data_ptr() : nullptr, has_q ? out.stride(0) : 0,
-                                 has_q ? out.stride(1) : 0, ordered(p));
+                                 has_q ? out.stride(1) : 0, st);
   if (rc != MISAT_OK) return fail(rc, "misat_kv_append");
+  used(b->made, st);
   written(p->k_blocks);
   written(p->v_blocks);
   if (given) written(out);
@@ -288,12 +339,12 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       given ? heads(a[3], "out", p->dtype, p->device, T, p->hq, p->d) : fresh({T, p->hq, p->d}, p->dtype, p->device);
   at::Tensor lse;
   if (with_lse) lse = fresh({T, p->hq}, at::kFloat, p->device);
-  const int rc =
-      window < 0 || window > INT32_MAX
-          ? MISAT_ERR_INVALID_ARG
-          : misat_kv_attend(p->h, &b->b, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0),
-                            out.stride(1), with_lse ? lse.data_ptr<float>() : nullptr, (int32_t)window, ordered(p));
+  if (window < 0 || window > INT32_MAX) return fail(MISAT_ERR_INVALID_ARG, "misat_kv_attend");
+  const cudaStream_t st = ordered(p);
+  const int rc = misat_kv_attend(p->h, &b->b, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0),
+                                 out.stride(1), with_lse ? lse.data_ptr<float>() : nullptr, (int32_t)window, st);
   if (rc != MISAT_OK) return fail(rc, "misat_kv_attend");
+  used(b->made, st);
   if (given) written(out);
   PyObject* o = a[3];
   if (given) Py_INCREF(o);
@@ -304,6 +355,336 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_DECREF(o);
   Py_XDECREF(l);
   return both;
+  MISAT_END
+}
+
+// ---- normed heads ----
+
+// (weight, eps, offset)
+PyObject* norm_state(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 3)) return nullptr;
+  const double eps = PyFloat_AsDouble(a[1]), offset = PyFloat_AsDouble(a[2]);
+  if (PyErr_Occurred()) return nullptr;
+  const Norm norm{tensor(a[0], "weight"), (float)eps, (float)offset};
+  const at::Tensor& w = norm.w;
+  if (code_of(w.scalar_type()) < 0 || !w.is_cuda() || w.dim() < 1 || w.dim() > 2)
+    refuse("weight", "[head_dim] or [heads, head_dim] of bfloat16, float16 or float32 on a CUDA device", w);
+  return new_state(norm);
+  MISAT_END
+}
+// What the norm is now, for heads of d elements of a type: its weight may have been given other memory.
+misat_head_norm norm_of(const Norm* norm, const char* name, at::ScalarType dtype, c10::DeviceIndex device, int64_t heads,
+                        int64_t d) {
+  const at::Tensor& w = norm->w;
+  const bool each = w.dim() == 2;
+  if ((w.scalar_type() != dtype && w.scalar_type() != at::kFloat) || !w.is_cuda() || w.get_device() != device ||
+      w.dim() < 1 || w.dim() > 2 || w.size(-1) != d || (d > 1 && w.stride(-1) != 1) ||
+      (each && (w.size(0) != heads || (heads > 1 && w.stride(0) < d)))) {
+    std::ostringstream s;
+    s << "a weight [" << d << "] or [" << heads << ", " << d << "] of " << dtype << " or float32 on cuda:" << (int)device
+      << " with contiguous heads";
+    refuse(name, s.str(), w);
+  }
+  return {w.data_ptr(), each ? (heads > 1 ? w.stride(0) : d) : 0, code_of(w.scalar_type()), norm->eps, norm->offset};
+}
+
+struct Rotation {  // the checked arguments of a call on [tokens][heads][head_dim]
+  const Rope* r;
+  int64_t T, H, D;
+  int code;
+  const int32_t* positions;
+};
+Rotation rotation(PyObject* rope, PyObject* ox, PyObject* positions, const char* name) {
+  Rotation c{};
+  c.r = state<Rope>(rope);
+  if (!c.r) throw Raised{};
+  const at::Tensor& x = tensor(ox, "x");
+  c.code = code_of(x.scalar_type());
+  if (c.code < 0 || x.dim() != 3) refuse("x", "[tokens, heads, head_dim] of bfloat16, float16 or float32", x);
+  c.T = x.size(0), c.H = x.size(1), c.D = x.size(2);
+  heads(ox, "x", x.scalar_type(), c.r->device, c.T, c.H, c.D);
+  c.positions = ints(tensor(positions, "positions"), "positions", c.r->device, {c.T});
+  if (c.T > INT32_MAX || c.H > INT32_MAX || c.D > INT32_MAX) {
+    fail(MISAT_ERR_INVALID_ARG, name);
+    throw Raised{};
+  }
+  return c;
+}
+
+// (rope, x, positions, norm, out or None) -> out
+PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 5)) return nullptr;
+  const Rotation c = rotation(a[0], a[1], a[2], "misat_norm_rotary");
+  const Norm* norm = state<Norm>(a[3]);
+  if (!norm) return nullptr;
+  const at::Tensor& x = tensor(a[1], "x");
+  const misat_head_norm w = norm_of(norm, "norm", x.scalar_type(), c.r->device, c.H, c.D);
+  const bool given = a[4] != Py_None;
+  const at::Tensor out = given ? heads(a[4], "out", x.scalar_type(), c.r->device, c.T, c.H, c.D)
+                               : fresh({c.T, c.H, c.D}, x.scalar_type(), c.r->device);
+  const int rc = misat_norm_rotary(c.r->h, &w, c.code, (int32_t)c.T, (int32_t)c.H, (int32_t)c.D, x.data_ptr(),
+                                   x.stride(0), x.stride(1), c.positions, out.data_ptr(), out.stride(0), out.stride(1),
+                                   c10::cuda::getCurrentCUDAStream(c.r->device).stream());
+  if (rc != MISAT_OK) return fail(rc, "misat_norm_rotary");
+  if (given) {
+    written(out);
+    Py_INCREF(a[4]);
+    return a[4];
+  }
+  return THPVariable_Wrap(out);
+  MISAT_END
+}
+
+PyObject* pair(PyObject* first, const at::Tensor& second) {  // takes first over
+  PyObject* s = first ? THPVariable_Wrap(second) : nullptr;
+  PyObject* both = s ? PyTuple_Pack(2, first, s) : nullptr;
+  Py_XDECREF(first);
+  Py_XDECREF(s);
+  return both;
+}
+
+// (rope, x, grad, positions, norm, out or None) -> (dx, dweight)
+PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 6)) return nullptr;
+  const Rotation c = rotation(a[0], a[1], a[3], "misat_norm_rotary_backward");
+  const Norm* norm = state<Norm>(a[4]);
+  if (!norm) return nullptr;
+  const at::Tensor& x = tensor(a[1], "x");
+  const at::ScalarType dtype = x.scalar_type();
+  const at::Tensor& g = heads(a[2], "grad", dtype, c.r->device, c.T, c.H, c.D);
+  const misat_head_norm w = norm_of(norm, "norm", dtype, c.r->device, c.H, c.D);
+  const bool given = a[5] != Py_None;
+  const at::Tensor dx = given ? heads(a[5], "out", dtype, c.r->device, c.T, c.H, c.D)
+                              : fresh({c.T, c.H, c.D}, dtype, c.r->device);
+  int64_t bytes = 0;
+  int rc = misat_norm_rotary_work(c.r->h, &w, c.code, (int32_t)c.T, (int32_t)c.H, (int32_t)c.D, &bytes);
+  if (rc != MISAT_OK) return fail(rc, "misat_norm_rotary_backward");
+  const at::Tensor work = fresh({bytes / 4}, at::kFloat, c.r->device), dw = fresh(norm->w.sizes(), norm->w.scalar_type(), c.r->device);
+  rc = misat_norm_rotary_backward(c.r->h, &w, c.code, (int32_t)c.T, (int32_t)c.H, (int32_t)c.D, x.data_ptr(),
+                                  x.stride(0), x.stride(1), g.data_ptr(), g.stride(0), g.stride(1), c.positions,
+                                  dx.data_ptr(), dx.stride(0), dx.stride(1), dw.data_ptr(), c.D, work.data_ptr(), bytes,
+                                  c10::cuda::getCurrentCUDAStream(c.r->device).stream());
+  if (rc != MISAT_OK) return fail(rc, "misat_norm_rotary_backward");
+  PyObject* o = a[5];
+  if (given) {
+    written(dx);
+    Py_INCREF(o);
+  } else {
+    o = THPVariable_Wrap(dx);
+  }
+  return pair(o, dw);
+  MISAT_END
+}
+
+// ---- trees of drafted tokens ----
+
+// The tree was made for this batch's tokens.
+bool same_tokens(const Tree* t, const Batch* b) {
+  if (t->n_tokens == b->b.n_tokens && t->max_q == b->b.max_q && t->device == b->device) return true;
+  PyErr_SetString(PyExc_ValueError, "tree: made for a batch of other tokens or another device");
+  return false;
+}
+
+// (pool, batch, k, v, q or None, q_out or None, q_norm or None, k_norm or None, tree or None) -> q_out
+PyObject* append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 9)) return nullptr;
+  Pool* p = state<Pool>(a[0]);
+  const Batch* b = p ? state<Batch>(a[1]) : nullptr;
+  if (!b || !same_heads(p, b)) return nullptr;
+  const int64_t T = b->b.n_tokens;
+  const at::Tensor &k = heads(a[2], "k", p->dtype, p->device, T, p->hkv, p->d),
+                   &v = heads(a[3], "v", p->dtype, p->device, T, p->hkv, p->d);
+  const bool has_q = a[4] != Py_None, given = has_q && a[5] != Py_None;
+  at::Tensor q, out;
+  if (has_q) {
+    q = heads(a[4], "q", p->dtype, p->device, T, p->hq, p->d);
+    out = given ? heads(a[5], "q_out", p->dtype, p->device, T, p->hq, p->d)
+                : fresh({T, p->hq, p->d}, p->dtype, p->device);
+  }
+  misat_head_norm norms[2];
+  const misat_head_norm* norm[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i) {
+    if (a[6 + i] == Py_None) continue;
+    const Norm* w = state<Norm>(a[6 + i]);
+    if (!w) return nullptr;
+    norms[i] = norm_of(w, i ? "k_norm" : "q_norm", p->dtype, p->device, i ? p->hkv : p->hq, p->d);
+    norm[i] = norms + i;
+  }
+  const Tree* t = a[8] == Py_None ? nullptr : state<Tree>(a[8]);
+  if (a[8] != Py_None && (!t || !same_tokens(t, b))) return nullptr;
+  const cudaStream_t st = ordered(p);
+  const int rc = misat_kv_append_norm(
+      p->h, &b->b, norm[0], norm[1], t ? &t->d : nullptr, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+      v.stride(0), v.stride(1), has_q ? q.data_ptr() : nullptr, has_q ? q.stride(0) : 0, has_q ? q.stride(1) : 0,
+      has_q ? out.data_ptr() : nullptr, has_q ? out.stride(0) : 0, has_q ? out.stride(1) : 0, st);
+  if (rc != MISAT_OK) return fail(rc, "misat_kv_append_norm");
+  used(b->made, st);
+  if (t) used(t->made, st);
+  written(p->k_blocks);
+  written(p->v_blocks);
+  if (given) written(out);
+  if (has_q && !given) return THPVariable_Wrap(out);
+  PyObject* r = given ? a[5] : Py_None;
+  Py_INCREF(r);
+  return r;
+  MISAT_END
+}
+
+// (pool, batch, parents, window) -> (depth, bits, tree)
+PyObject* tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 4)) return nullptr;
+  Pool* p = state<Pool>(a[0]);
+  const Batch* b = p ? state<Batch>(a[1]) : nullptr;
+  if (!b || !same_heads(p, b)) return nullptr;
+  const int64_t T = b->b.n_tokens;
+  const int32_t* parents = ints(tensor(a[2], "parents"), "parents", p->device, {T});
+  const int32_t window = int32_of(a[3], "window");
+  if (window < 0 || b->b.max_q > MISAT_KV_TREE_NODES) return fail(MISAT_ERR_INVALID_ARG, "misat_kv_tree");
+  const int32_t words = (b->b.max_q + 31) / 32;
+  const at::Tensor depth = fresh({T}, at::kInt, p->device), bits = fresh({T, words}, at::kInt, p->device);
+  Tree t{{depth.data_ptr<int32_t>(), reinterpret_cast<uint32_t*>(bits.data_ptr<int32_t>()), words, window},
+         T, b->b.max_q, p->device, {nullptr, {depth, bits}}};
+  t.made.on = ordered(p);
+  const int rc = misat_kv_tree(p->h, &b->b, parents, window, const_cast<int32_t*>(t.d.depth),
+                               const_cast<uint32_t*>(t.d.bits), words, t.made.on);
+  if (rc != MISAT_OK) return fail(rc, "misat_kv_tree");
+  used(b->made, t.made.on);
+  PyObject* c = new_state(t);
+  if (!c) return nullptr;
+  PyObject *d = THPVariable_Wrap(depth), *w = d ? THPVariable_Wrap(bits) : nullptr;
+  PyObject* all = w ? PyTuple_Pack(3, d, w, c) : nullptr;
+  Py_DECREF(c);
+  Py_XDECREF(d);
+  Py_XDECREF(w);
+  return all;
+  MISAT_END
+}
+
+// (pool, batch, q, out or None, tree, return_lse) -> out or (out, lse)
+PyObject* attend_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 6)) return nullptr;
+  Pool* p = state<Pool>(a[0]);
+  const Batch* b = p ? state<Batch>(a[1]) : nullptr;
+  const Tree* t = b ? state<Tree>(a[4]) : nullptr;
+  if (!t || !same_heads(p, b) || !same_tokens(t, b)) return nullptr;
+  const int64_t T = b->b.n_tokens;
+  const at::Tensor& q = heads(a[2], "q", p->dtype, p->device, T, p->hq, p->d);
+  const bool given = a[3] != Py_None, with_lse = PyObject_IsTrue(a[5]) == 1;
+  const at::Tensor out =
+      given ? heads(a[3], "out", p->dtype, p->device, T, p->hq, p->d) : fresh({T, p->hq, p->d}, p->dtype, p->device);
+  at::Tensor lse;
+  if (with_lse) lse = fresh({T, p->hq}, at::kFloat, p->device);
+  const cudaStream_t st = ordered(p);
+  const int rc = misat_kv_attend_tree(p->h, &b->b, &t->d, q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(),
+                                      out.stride(0), out.stride(1), with_lse ? lse.data_ptr<float>() : nullptr, st);
+  if (rc != MISAT_OK) return fail(rc, "misat_kv_attend_tree");
+  used(b->made, st);
+  used(t->made, st);
+  PyObject* o = a[3];
+  if (given) {
+    written(out);
+    Py_INCREF(o);
+  } else {
+    o = THPVariable_Wrap(out);
+  }
+  return with_lse ? pair(o, lse) : o;
+  MISAT_END
+}
+
+// (pool, batch, path, n_keep, out or None) -> kv_len
+PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 5)) return nullptr;
+  Pool* p = state<Pool>(a[0]);
+  const Batch* b = p ? state<Batch>(a[1]) : nullptr;
+  if (!b || !same_heads(p, b)) return nullptr;
+  const int64_t seqs = b->b.n;
+  const at::Tensor& path = tensor(a[2], "path");
+  const int64_t width = path.dim() == 2 ? path.size(1) : 0;
+  const int32_t* nodes = ints(path, "path", p->device, {seqs, width});
+  const int32_t* many = ints(tensor(a[3], "n_keep"), "n_keep", p->device, {seqs});
+  const bool given = a[4] != Py_None;
+  const at::Tensor out = given ? tensor(a[4], "out") : fresh({seqs}, at::kInt, p->device);
+  int32_t* len = ints(out, "out", p->device, {seqs});
+  const cudaStream_t st = ordered(p);
+  const int rc = misat_kv_keep(p->h, &b->b, nodes, width, many, len, st);
+  if (rc != MISAT_OK) return fail(rc, "misat_kv_keep");
+  used(b->made, st);
+  written(p->k_blocks);
+  written(p->v_blocks);
+  if (!given) return THPVariable_Wrap(out);
+  written(out);
+  Py_INCREF(a[4]);
+  return a[4];
+  MISAT_END
+}
+
+// (pool, block_table, ring, state, new, kv_len, shared or None, n_tokens, max_q, out or None)
+//   -> (state, q_off, kv_len, positions, slots, batch)
+PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MISAT_TRY
+  if (!count(n, 10)) return nullptr;
+  Pool* p = state<Pool>(a[0]);
+  if (!p) return nullptr;
+  const at::Tensor &table = tensor(a[1], "block_table"), &ring = tensor(a[2], "ring"), &fresh_tokens = tensor(a[4], "new");
+  const int64_t seqs = fresh_tokens.dim() == 1 ? fresh_tokens.size(0) : 0;
+  misat_kv_step s{};
+  s.new_tokens = ints(fresh_tokens, "new", p->device, {seqs});
+  s.kv_len = ints(tensor(a[5], "kv_len"), "kv_len", p->device, {seqs});
+  if (a[6] != Py_None) s.shared = ints(tensor(a[6], "shared"), "shared", p->device, {seqs});
+  const at::Tensor& before = tensor(a[3], "state");
+  s.state = ints(before, "state", p->device, {seqs + 2});
+  const int64_t columns = table_columns(table, p->device, seqs, s.table_stride);
+  const int64_t places = ring.dim() == 1 ? ring.size(0) : 0;
+  s.ring = ints(ring, "ring", p->device, {places});
+  s.block_table = table.data_ptr<int32_t>();
+  s.n_tokens = int32_of(a[7], "n_tokens");
+  s.max_q = int32_of(a[8], "max_q");
+  if (seqs > INT32_MAX || columns > INT32_MAX || places > INT32_MAX || s.n_tokens < 0 || s.n_tokens == INT32_MAX)
+    return fail(MISAT_ERR_INVALID_ARG, "misat_kv_tables");
+  s.n = (int32_t)seqs;
+  s.columns = (int32_t)columns;
+  s.ring_size = (int32_t)places;
+  const bool given = a[9] != Py_None;
+  const at::Tensor after = given ? tensor(a[9], "out") : fresh({seqs + 2}, at::kInt, p->device);
+  s.state_out = ints(after, "out", p->device, {seqs + 2});
+  const int64_t bytes = MISAT_KV_TABLES_WORK(seqs);
+  const at::Tensor q_off = fresh({seqs + 1}, at::kInt, p->device), len = fresh({seqs}, at::kInt, p->device),
+                   positions = fresh({s.n_tokens}, at::kInt, p->device), slots = fresh({s.n_tokens}, at::kLong, p->device),
+                   work = fresh({bytes / 4}, at::kInt, p->device);
+  s.q_off = q_off.data_ptr<int32_t>();
+  s.kv_len_out = len.data_ptr<int32_t>();
+  s.positions = positions.data_ptr<int32_t>();
+  s.slots = slots.data_ptr<int64_t>();
+  const cudaStream_t st = ordered(p);
+  const int rc = misat_kv_tables(p->h, &s, work.data_ptr(), bytes, st);
+  if (rc != MISAT_OK) return fail(rc, "misat_kv_tables");
+  written(table);
+  written(ring);
+  if (given) written(after);
+  const Batch b{{s.n, s.n_tokens, s.max_q, s.q_off, s.kv_len_out, s.block_table, s.table_stride},
+                p->hq, p->hkv, p->d, p->device, {st, {q_off, len}}};
+  PyObject* all = PyTuple_New(6);
+  if (!all) return nullptr;
+  PyObject* first = a[9];
+  if (given) Py_INCREF(first);
+  else first = THPVariable_Wrap(after);
+  PyObject* items[6] = {first, THPVariable_Wrap(q_off), THPVariable_Wrap(len), THPVariable_Wrap(positions),
+                        THPVariable_Wrap(slots), new_state(b)};
+  bool ok = true;
+  for (int i = 0; i < 6; ++i) {
+    ok = ok && items[i];
+    PyTuple_SET_ITEM(all, i, items[i]);
+  }
+  if (ok) return all;
+  Py_DECREF(all);
+  return nullptr;
   MISAT_END
 }
 
@@ -331,6 +712,14 @@ PyMethodDef methods[] = {{"init", init, METH_O, nullptr},
                          MISAT_FAST(rotary),
                          MISAT_FAST(append),
                          MISAT_FAST(attend),
+                         MISAT_FAST(norm_state),
+                         MISAT_FAST(norm_rotate),
+                         MISAT_FAST(norm_backward),
+                         MISAT_FAST(append_norm),
+                         MISAT_FAST(tree),
+                         MISAT_FAST(attend_tree),
+                         MISAT_FAST(keep),
+                         MISAT_FAST(tables),
                          {"sync", sync, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

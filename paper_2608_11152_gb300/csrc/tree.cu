@@ -1,0 +1,194 @@
+// Trees of drafted tokens on a pool's blocks: the plan of a step's trees, and what is kept of them.
+//
+// Plan: node i of a sequence has a parent before it, or follows the tokens before the tree.  Depth and ancestors of a
+// node come from walking up, a thread per node, in shared memory: parents are smaller numbers, so the walk ends, and
+// its ancestors come in falling order, so the bits of a word are complete before the next lower word begins.
+//
+// Keep: the keys and values of the accepted nodes move from slot P + path[i] to P + i.  The path rises, so path[i] >= i,
+// and a thread that owns 16 bytes of a row's elements and goes through the path in order reads every row before it is
+// written, also where it has several rows in flight.
+//
+// Both are bound by latency: a few dependent reads a sequence, then one pass over the rows.
+#include <algorithm>
+
+#include "kv.h"
+
+using namespace misat;
+
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kRoot = -1, kAbsent = -2;
+
+struct TreeArgs {
+  KvBatch b;
+  const int32_t* parent;
+  int32_t* depth;
+  uint32_t* bits;
+  int32_t words, window;
+  int32_t* err;
+};
+
+// New tokens of sequence b and its place in the batch; n = 0 where it is malformed.
+struct Range {
+  int begin, n, len;
+};
+__device__ __forceinline__ Range load_range(const KvBatch& k, int b, int32_t* err) {
+  const int begin = __ldcg(k.q_off + b), end = __ldcg(k.q_off + b + 1), len = __ldcg(k.kv_len + b);
+  const bool ok = begin >= 0 && end >= begin && end <= k.n_tokens && end - begin <= k.max_q && len >= end - begin &&
+                  len <= kMaxLen && len <= k.stride * kBlockTokens;
+  if (!ok && threadIdx.x == 0) set_error(err, MISAT_ERR_INVALID_ARG);
+  return {begin, ok ? end - begin : 0, len};
+}
+
+__global__ void __launch_bounds__(kThreads) k_tree(const __grid_constant__ TreeArgs a) {
+  __shared__ int32_t up[MISAT_KV_TREE_NODES];
+  chain_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0 &&
+      (__ldcg(a.b.q_off) != 0 || __ldcg(a.b.q_off + a.b.n) != a.b.n_tokens))
+    set_error(a.err, MISAT_ERR_INVALID_ARG);
+  const Range s = load_range(a.b, blockIdx.x, a.err);
+  for (int i = threadIdx.x; i < s.n; i += kThreads) {
+    const int p = __ldcg(a.parent + s.begin + i);
+    up[i] = p < i && p >= kAbsent ? p : kAbsent - 1;  // (neither a parent nor one of the two marks)
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < s.n; i += kThreads) {
+    // Up once for the depth, and to see that the line ends at the tokens before the tree.
+    int depth = 0, at = i, p;
+    while ((p = up[at]) >= 0) {
+      at = p;
+      ++depth;
+    }
+    const bool there = p == kRoot;
+    if (!there && !(p == kAbsent && at == i)) set_error(a.err, MISAT_ERR_INVALID_ARG);
+    a.depth[s.begin + i] = there ? depth : 0;
+    uint32_t* row = a.bits + (int64_t)(s.begin + i) * a.words;
+    int left = !there ? 0 : a.window > 0 ? min(a.window, depth + 1) : depth + 1;
+    at = i;
+    for (int w = a.words - 1; w >= 0; --w) {
+      uint32_t word = 0;
+      for (; left > 0 && at >= w * 32; --left) {
+        word |= 1u << (at & 31);
+        at = up[at];
+      }
+      row[w] = word;
+    }
+  }
+}
+
+struct KeepArgs {
+  KvBatch b;
+  const int32_t* path;
+  int64_t path_stride;
+  const int32_t* n_keep;
+  int32_t* len_out;
+  uint4* kb;
+  uint4* vb;
+  int32_t hkv, vecs, n_blocks, split;  // vecs: of 16 bytes a row; split: CTAs of a sequence
+  int32_t* err;
+};
+
+__global__ void __launch_bounds__(kThreads) k_keep(const __grid_constant__ KeepArgs a) {
+  constexpr int kAhead = 8;
+  __shared__ int64_t from[MISAT_KV_TREE_NODES], to[MISAT_KV_TREE_NODES];  // rows of kv head 0, -1: stays
+  const int b = blockIdx.x, tid = threadIdx.x;
+  chain_wait();
+  const Range s = load_range(a.b, b, a.err);
+  const int m = __ldcg(a.n_keep + b);
+  const int32_t* path = a.path + (int64_t)b * a.path_stride;
+  bool ok = m >= 0 && m <= s.n && m <= a.path_stride && m <= MISAT_KV_TREE_NODES && s.len >= s.n;
+  const int before = s.len - s.n;
+  auto row_of = [&](int pos) {
+    const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
+    if (blk < 0 || blk >= a.n_blocks) return (int64_t)-1;
+    return ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.vecs;
+  };
+  if (ok) {
+    for (int i = tid; i < m; i += kThreads) {
+      const int p = __ldcg(path + i), last = i > 0 ? __ldcg(path + i - 1) : -1;
+      const bool fits = p > last && p < s.n && p >= i;
+      from[i] = to[i] = -1;
+      if (fits && p != i) {
+        from[i] = row_of(before + p);
+        to[i] = row_of(before + i);
+      }
+      ok = ok && fits && (p == i || (from[i] >= 0 && to[i] >= 0));
+    }
+  }
+  ok = __syncthreads_and(ok);
+  if (blockIdx.y == 0 && tid == 0) {
+    if (!ok) set_error(a.err, MISAT_ERR_INVALID_ARG);
+    a.len_out[b] = ok ? before + m : __ldcg(a.b.kv_len + b);
+  }
+  if (!ok) return;
+  // A column: 16 bytes of the rows of a kv head, of the keys or the values.
+  const int heads = a.hkv * a.vecs, cols = 2 * heads;
+  for (int c = blockIdx.y * kThreads + tid; c < cols; c += a.split * kThreads) {
+    uint4* p = c < heads ? a.kb : a.vb;
+    const int k = c < heads ? c : c - heads, head = k / a.vecs;
+    p += (int64_t)head * kBlockTokens * a.vecs + (k - head * a.vecs);
+#pragma unroll 1
+    for (int i = 0; i < m; i += kAhead) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < m && from[i + j] >= 0) v[j] = p[from[i + j]];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < m && from[i + j] >= 0) p[to[i + j]] = v[j];
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* parents, int32_t window, int32_t* depth,
+                  uint32_t* bits, int32_t words, void* cuda_stream) {
+  if (!batch_ok(kv, batch) || window < 0 || batch->max_q > MISAT_KV_TREE_NODES || words < 0 ||
+      words != (batch->max_q + 31) / 32)
+    return MISAT_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0) return MISAT_OK;
+  if (!parents || !depth || !bits || batch->max_q == 0 || !on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
+  const TreeArgs a{batch_view(batch), parents, depth, bits, words, window, kv->err};
+  launch_chained(k_tree, batch->n, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), a);
+  return launch_status();
+}
+
+int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path, int64_t path_stride,
+                  const int32_t* n_keep, int32_t* kv_len_out, void* cuda_stream) {
+  if (!batch_ok(kv, batch) || batch->max_q > MISAT_KV_TREE_NODES || path_stride < 0) return MISAT_ERR_INVALID_ARG;
+  if (batch->n == 0) return MISAT_OK;
+  if (!batch->q_off || !batch->kv_len || (!batch->block_table && batch->table_stride > 0) ||
+      (!path && path_stride > 0) || !n_keep || !kv_len_out || kv_len_out == batch->kv_len || !on_device(kv->device))
+    return MISAT_ERR_INVALID_ARG;
+  KeepArgs a{};
+  a.b = batch_view(batch);
+  a.path = path;
+  a.path_stride = path_stride;
+  a.n_keep = n_keep;
+  a.len_out = kv_len_out;
+  a.kb = static_cast<uint4*>(kv->kb);
+  a.vb = static_cast<uint4*>(kv->vb);
+  a.hkv = kv->hkv;
+  a.vecs = kv->d / 8;
+  a.n_blocks = kv->n_blocks;
+  a.err = kv->err;
+  const int cols = (2 * kv->hkv * a.vecs + kThreads - 1) / kThreads;
+  a.split = std::max(1, std::min(cols, kv->num_sms * 8 / batch->n));
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3(batch->n, a.split);
+  lc.blockDim = dim3(kThreads);
+  lc.stream = static_cast<cudaStream_t>(cuda_stream);
+  lc.attrs = &at;
+  lc.numAttrs = 1;
+  cudaLaunchKernelEx(&lc, k_keep, a);
+  return launch_status();
+}
+
+}  // extern "C"

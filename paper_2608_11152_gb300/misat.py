@@ -33,6 +33,7 @@ BF16, F16, F32 = 0, 1, 2
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BY_PARTS = 0, 1, 2
 BLOCK_TOKENS = 16
+KV_TREE_NODES, KV_ROOT, KV_ABSENT = 1024, -1, -2
 ADMIT_CONT, ADMIT_NEW, ADMIT_FOLLOW = 1, 2, 3
 HOLD_GLOBAL_CAP, HOLD_CLASS_CAP, HOLD_NO_ELIGIBLE, HOLD_PREFER_CACHE, HOLD_LEADER_HELD = 16, 17, 18, 19, 20
 
@@ -103,6 +104,22 @@ class misat_kv_batch(C.Structure):
                 ("block_table", _p), ("table_stride", C.c_int64)]
 
 
+class misat_kv_step(C.Structure):
+    _fields_ = [("n", C.c_int32), ("n_tokens", C.c_int32), ("max_q", C.c_int32), ("columns", C.c_int32),
+                ("table_stride", C.c_int64), ("ring_size", C.c_int32), ("new_tokens", _p), ("kv_len", _p),
+                ("shared", _p), ("state", _p), ("block_table", _p), ("ring", _p), ("state_out", _p), ("q_off", _p),
+                ("kv_len_out", _p), ("positions", _p), ("slots", _p)]
+
+
+class misat_head_norm(C.Structure):
+    _fields_ = [("weight", _p), ("head_stride", C.c_int64), ("dtype", C.c_int32), ("eps", C.c_float),
+                ("offset", C.c_float)]
+
+
+class misat_kv_draft(C.Structure):
+    _fields_ = [("depth", _p), ("bits", _p), ("words", C.c_int32), ("window", C.c_int32)]
+
+
 _SIG = {
     "misat_create": [C.POINTER(misat_config), _p, C.POINTER(_p)],
     "misat_destroy": [_p],
@@ -151,6 +168,19 @@ _SIG = {
                         C.c_int64, C.c_int64, _p],
     "misat_kv_attend": [_p, _p, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, C.c_int32, _p],
     "misat_kv_sync": [_p, _p],
+    "misat_kv_tables": [_p, C.POINTER(misat_kv_step), _p, C.c_int64, _p],
+    "misat_norm_rotary": [_p, C.POINTER(misat_head_norm), C.c_int32, C.c_int32, C.c_int32, C.c_int32, _p, C.c_int64,
+                          C.c_int64, _p, _p, C.c_int64, C.c_int64, _p],
+    "misat_norm_rotary_work": [_p, C.POINTER(misat_head_norm), C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                               C.POINTER(C.c_int64)],
+    "misat_norm_rotary_backward": [_p, C.POINTER(misat_head_norm), C.c_int32, C.c_int32, C.c_int32, C.c_int32, _p,
+                                   C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, _p, C.c_int64, C.c_int64, _p,
+                                   C.c_int64, _p, C.c_int64, _p],
+    "misat_kv_tree": [_p, _p, _p, C.c_int32, _p, _p, C.c_int32, _p],
+    "misat_kv_append_norm": [_p, _p, _p, _p, _p, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, C.c_int64,
+                             C.c_int64, _p, C.c_int64, C.c_int64, _p],
+    "misat_kv_attend_tree": [_p, _p, _p, _p, C.c_int64, C.c_int64, _p, C.c_int64, C.c_int64, _p, _p],
+    "misat_kv_keep": [_p, _p, _p, C.c_int64, _p, _p, _p],
 }
 NOALLOC_MAX_REQUESTS = 65536
 
@@ -585,7 +615,7 @@ class Rope:
         self._h = h
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._state = calls.rope_state(h.value, self.device.index)
-        self._rotary = calls.rotary
+        self._rotary, self._norm_rotate, self._norm_backward = calls.rotary, calls.norm_rotate, calls.norm_backward
 
     def close(self):
         """Frees the frequencies; MisatError (ERR_STATE) while an open KvPool applies them."""
@@ -610,6 +640,26 @@ class Rope:
         """Gradient of rotate()'s x, given the gradient of its result."""
         return self._rotary(self._state, grad, positions, out, True)
 
+    def norm_rotate(self, x, positions, norm, out=None):
+        """x [tokens, heads, head_dim] with `norm` (a HeadNorm) applied to each head, turned to `positions`; out may
+        be x."""
+        return self._norm_rotate(self._state, x, positions, norm._state, out)
+
+    def norm_backward(self, x, grad, positions, norm, out=None):
+        """Gradients (dx, dweight) of norm_rotate()'s x and norm's weight, given the gradient of its result; out, for
+        dx, may be x or grad."""
+        return self._norm_backward(self._state, x, grad, positions, norm._state, out)
+
+
+class HeadNorm:
+    """Root-mean-square norm of each head (misat_head_norm): x / sqrt(mean x^2 + eps) * (offset + weight), for
+    Rope.norm_rotate, Rope.norm_backward and KvPool.append.  weight: [head_dim] for all heads or [heads, head_dim], of the
+    heads' dtype or float32; the caller's tensor, read at every call."""
+
+    def __init__(self, weight, eps=1e-6, offset=0.0):
+        self.weight, self.eps, self.offset = weight, float(eps), float(offset)
+        self._state = _torch_calls().norm_state(weight, self.eps, self.offset)
+
 
 class KvBatch:
     """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer.  It serves
@@ -623,6 +673,59 @@ class KvBatch:
         self._c = misat_kv_batch(self.n, self.n_tokens, int(max_q), q_off.data_ptr(), kv_len.data_ptr(),
                                  block_table.data_ptr(), stride)
         self._ref = C.addressof(self._c)  # for calls of the C functions
+
+
+class KvStep(KvBatch):
+    """A KvBatch whose block table KvTables.step() brought to the step's lengths.  state: the tables' state after it;
+    q_off, kv_len, positions (int32) and slots (int64: 16 block + position % 16) of its tokens."""
+
+    def __init__(self, tables, made, n, n_tokens, max_q):
+        self.state, self.q_off, self.kv_len, self.positions, self.slots, self._state = made
+        self._keep = (self.q_off, self.kv_len, tables.block_table)
+        self.n, self.n_tokens, self.max_q = n, int(n_tokens), int(max_q)
+        self.block_table = tables.block_table
+
+
+class KvTables:
+    """Block tables of n sequences on the device (misat_kv_tables): each step() gives every row of `block_table` (int32
+    [n, blocks]) the blocks that its length takes and gives back those it does not need, from and to the ring `free`
+    (int32 [places], as many as the pool has blocks always suffice).  Both are the caller's tensors.
+
+    What changes from step to step is a tensor of its own, `state` (int32 [n + 2]): blocks in each row, then the ring's
+    front and how many free blocks follow it.  initial() makes the first one."""
+
+    def __init__(self, pool, block_table, free):
+        self.pool, self.block_table, self.free = pool, block_table, free
+        self._step = _torch_calls().tables
+
+    def initial(self, n_free, held=None):
+        """State of rows with `held` blocks (int32 [n]; none) and n_free free blocks in the ring's first places."""
+        import torch
+
+        n = self.block_table.shape[0]
+        s = torch.zeros(n + 2, dtype=torch.int32, device=self.block_table.device)
+        if held is not None:
+            s[:n] = held
+        s[n + 1] = int(n_free)
+        return s
+
+    def step(self, state, new, kv_len, *, n_tokens, max_q, shared=None, out=None):
+        """The step in which each sequence gets `new` tokens after its `kv_len` (int32 [n]; n_tokens is the sum of new,
+        max_q at least its largest): a KvStep.  shared: leading blocks of a row that are not given back (int32 [n]).
+        out: tensor for the state after the step; may be `state`.  Where it cannot be made (too few free blocks: ERR_OOM;
+        malformed numbers: ERR_INVALID_ARG), nothing changes and pool.sync() raises."""
+        made = self._step(self.pool._state, self.block_table, self.free, state, new, kv_len, shared, n_tokens, max_q, out)
+        return KvStep(self, made, new.shape[0], n_tokens, max_q)
+
+
+class KvTree:
+    """The trees of a step's drafted tokens (misat_kv_tree): made by KvPool.tree once for a step, used by every layer.
+    depth: int32 [n_tokens]; bits: int32 [n_tokens, words], bit j % 32 of word j // 32 where node j is the node itself or
+    an ancestor within the window."""
+
+    def __init__(self, made, window):
+        self.depth, self.bits, self._state = made
+        self.window = int(window)
 
 
 class KvPool:
@@ -664,6 +767,8 @@ class KvPool:
             rope._pools += 1
         self._state = calls.pool_state(h.value, self.device.index, k_blocks, v_blocks, self.n_q_heads)
         self._append, self._attend, self._sync = calls.append, calls.attend, calls.sync
+        self._append_norm, self._tree, self._attend_tree = calls.append_norm, calls.tree, calls.attend_tree
+        self._keep = calls.keep
 
     def close(self):
         if getattr(self, "_h", None):
@@ -684,16 +789,38 @@ class KvPool:
         tokens), kv_len [n] (tokens after the append), block_table [n, blocks]."""
         return KvBatch(self, q_off, kv_len, block_table, n_tokens, max_q)
 
-    def append(self, batch, k, v, q=None, q_out=None):
+    def append(self, batch, k, v, q=None, q_out=None, *, q_norm=None, k_norm=None, tree=None):
         """Put the new tokens' k (rotated) and v, [n_tokens, kv heads, head_dim], into their
-        blocks; returns the rotated q [n_tokens, q heads, head_dim] (None without q).  q_out may be q."""
-        return self._append(self._state, batch._state, k, v, q, q_out)
+        blocks; returns the rotated q [n_tokens, q heads, head_dim] (None without q).  q_out may be q.
+        q_norm, k_norm: HeadNorms applied before the rotation.  tree: a KvTree; its nodes are rotated to the
+        positions of their depths."""
+        if q_norm is None and k_norm is None and tree is None:
+            return self._append(self._state, batch._state, k, v, q, q_out)
+        return self._append_norm(self._state, batch._state, k, v, q, q_out, q_norm and q_norm._state,
+                                 k_norm and k_norm._state, tree and tree._state)
 
-    def attend(self, batch, q, out=None, window=0, return_lse=False):
+    def attend(self, batch, q, out=None, window=0, return_lse=False, *, tree=None):
         """Attention of the new tokens' q [n_tokens, q heads, head_dim] over the cached tokens up to
         and including each; window > 0: over the last `window` of them.  out may be q.  Returns out, or
-        (out, lse)."""
-        return self._attend(self._state, batch._state, q, out, window, return_lse)
+        (out, lse).  tree: a KvTree; a node sees the tokens before the tree and its ancestors, in the
+        tree's window."""
+        if tree is None:
+            return self._attend(self._state, batch._state, q, out, window, return_lse)
+        if window not in (0, tree.window):
+            raise ValueError(f"window: the tree was made for {tree.window}, got {window}")
+        return self._attend_tree(self._state, batch._state, q, out, tree._state, return_lse)
+
+    def tree(self, batch, parents, window=0):
+        """The trees of the batch's new tokens, at most KV_TREE_NODES a sequence: parents (int32 [n_tokens]) are numbers
+        of earlier nodes of the same sequence, KV_ROOT for a node that follows the tokens before the tree, or
+        KV_ABSENT for no node.  window > 0: a node sees the last `window` positions."""
+        return KvTree(self._tree(self._state, batch._state, parents, window), window)
+
+    def keep(self, batch, path, n_keep, out=None):
+        """Move the keys and values of the accepted nodes of each tree, path[b, :n_keep[b]] (int32, rising), to the
+        slots behind the tokens before the tree; returns the lengths after it (int32 [n]; out must not be the
+        batch's kv_len)."""
+        return self._keep(self._state, batch._state, path, n_keep, out)
 
     def sync(self):
         """Wait for the current stream and raise the pool's sticky device error, if there is one."""
