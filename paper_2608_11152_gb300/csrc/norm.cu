@@ -21,10 +21,13 @@ using namespace misat;
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kMaxTile = 32;   // tokens of a CTA at a time: their places are found by one warp
 constexpr int kMaxHead = 256;  // elements
-constexpr int kBackward = 2;   // CTAs of the gradient on an SM
+constexpr int kForward = 4, kBackward = 2;  // CTAs on an SM
+constexpr int kShared = 47 * 1024;          // dynamic bytes of a CTA, at most 48 KiB with the places of its tokens
+// Threads of a CTA, and copies in flight of a thread: bytes.  (A head of more than 32 units has two a lane.)
+constexpr int threads_of(int upl) { return upl == 2 ? 128 : 256; }
+constexpr int in_flight(bool backward) { return backward ? 128 : 96; }
 
 struct HeadWeight {
   const void* p;  // nullptr: no norm
@@ -36,7 +39,8 @@ struct HeadWeight {
 struct NormArgs {
   int32_t n_tokens, hq, hkv, d, rot;  // hkv = 0: plain rotation of hq heads
   int32_t heads, first;               // rows of a token, and the first of them (queries, keys, values)
-  int32_t units, lane_bits, chunk, side, tile;  // lanes of a head; heads of a CTA, its tokens side by side and in all
+  int32_t units, lane_bits, chunk, side;  // lanes of a head; heads of a CTA, tokens side by side
+  int32_t per, tile;                  // tokens of a CTA, and of those at a time
   int32_t turns;                      // 32-bit numbers of a token's cosines
   FastDiv by_chunk;
   const uint64_t* freq;
@@ -53,6 +57,14 @@ struct NormArgs {
   float* parts;
 };
 
+// Two elements rounded in one instruction.
+__device__ __forceinline__ void narrow2(float a, float b, __nv_bfloat16* out) {
+  *reinterpret_cast<__nv_bfloat162*>(out) = __floats2bfloat162_rn(a, b);
+}
+__device__ __forceinline__ void narrow2(float a, float b, __half* out) {
+  *reinterpret_cast<__half2*>(out) = __floats2half2_rn(a, b);
+}
+
 // A lane's part of a head: UPL units of up to two vectors.
 template <class T, int VEC, bool HALF, int UPL>
 struct Part {
@@ -62,6 +74,8 @@ struct Part {
   static constexpr int kStep = kPair ? 2 : VEC;              // elements a unit steps over
   static constexpr int kPairs = HALF ? VEC : kPair ? 1 : VEC / 2;  // pairs of a unit
   static constexpr int kElems = kTwo ? 2 * VEC : VEC;        // elements of a unit
+  static constexpr int kBytes = UPL * kElems * (int)sizeof(T);
+  static constexpr int kThreads = threads_of(UPL);
 
   int half, paired, units, d, lane, lanes;
   __device__ __forceinline__ Part(const NormArgs& a, int lane)
@@ -84,7 +98,17 @@ struct Part {
 
   struct Raw {
     V lo[UPL], hi[kTwo ? UPL : 1];
+    __device__ __forceinline__ V& vec(int v) { return kTwo && v % 2 ? hi[v / 2] : lo[kTwo ? v / 2 : v]; }
   };
+  // Each vector with its number, its first element, and whether it is there.
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < UPL; ++j) {
+      f(kTwo ? 2 * j : j, first(j), has(j));
+      if constexpr (kTwo) f(2 * j + 1, second(j), has(j) && has_second(j));
+    }
+  }
   __device__ __forceinline__ void fetch(const T* p, Raw& r) const {
 #pragma unroll
     for (int j = 0; j < UPL; ++j) {
@@ -101,22 +125,33 @@ struct Part {
         if (has(j) && has_second(j)) *reinterpret_cast<V*>(p + second(j)) = r.hi[j];
     }
   }
-  // In 32 bits; elements that are not there are zeros.
-  __device__ __forceinline__ void widen(const Raw& r, bool ok, float (&x)[UPL][kElems]) const {
+  // Vectors that are not there become zeros, whatever the copy left: they add nothing to the sums.
+  __device__ __forceinline__ void clear_absent(Raw& r) const {
+    each([&](int v, int, bool there) {
+      if (!there) r.vec(v) = V{};
+    });
+  }
+  // In 32 bits, and back.
+  __device__ __forceinline__ void widen(const Raw& r, float (&x)[UPL][kElems]) const {
 #pragma unroll
     for (int j = 0; j < UPL; ++j)
 #pragma unroll
       for (int i = 0; i < kElems; ++i)
-        x[j][i] = ok && has_element(j, i) ? to_f(i < VEC ? r.lo[j].e[i] : r.hi[kTwo ? j : 0].e[i < VEC ? 0 : i - VEC])
-                                          : 0.f;
+        x[j][i] = to_f(i < VEC ? r.lo[j].e[i] : r.hi[kTwo ? j : 0].e[i < VEC ? 0 : i - VEC]);
   }
   __device__ __forceinline__ void narrow(const float (&x)[UPL][kElems], Raw& r) const {
 #pragma unroll
     for (int j = 0; j < UPL; ++j)
 #pragma unroll
-      for (int i = 0; i < kElems; ++i) {
-        if (i < VEC) r.lo[j].e[i] = from_f<T>(x[j][i]);
-        else r.hi[kTwo ? j : 0].e[i - VEC] = from_f<T>(x[j][i]);
+      for (int i = 0; i < kElems; i += VEC) {
+        V& v = i < VEC ? r.lo[j] : r.hi[kTwo ? j : 0];
+        if constexpr (VEC > 1 && sizeof(T) == 2) {
+#pragma unroll
+          for (int e = 0; e < VEC; e += 2) narrow2(x[j][i + e], x[j][i + e + 1], v.e + e);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v.e[e] = from_f<T>(x[j][i + e]);
+        }
       }
   }
 
@@ -146,17 +181,21 @@ struct Part {
           s[k] = sines[unit(j) * kPairs + k];
         }
       }
+      auto pairs = [&](bool ends) {
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) {
-        // The rotated part may end inside a vector: what is behind stays as it is (a product with zero would make
-        // NaN of an infinity).
-        if (!HALF && unit(j) * kPairs + k >= half) continue;
-        float& u = x[j][kTwo ? k : 2 * k];
-        float& w = x[j][kTwo ? VEC + k : 2 * k + 1];
-        const float a = u, b = w, sn = BACK ? -s[k] : s[k];
-        u = a * c[k] - b * sn;
-        w = a * sn + b * c[k];
-      }
+        for (int k = 0; k < kPairs; ++k) {
+          if (ends && unit(j) * kPairs + k >= half) continue;
+          float& u = x[j][kTwo ? k : 2 * k];
+          float& w = x[j][kTwo ? VEC + k : 2 * k + 1];
+          const float a = u, b = w, sn = BACK ? -s[k] : s[k];
+          u = a * c[k] - b * sn;
+          w = a * sn + b * c[k];
+        }
+      };
+      // The rotated part may end inside a vector: what is behind stays as it is (a product with zero would make NaN of
+      // an infinity).
+      if (HALF || kPairs == 1 || half % kPairs == 0) pairs(false);
+      else pairs(true);
     }
   }
   __device__ __forceinline__ void load_weight(const HeadWeight& w, int head, float (&out)[UPL][kElems]) const {
@@ -171,8 +210,11 @@ struct Part {
                                          : to_f(static_cast<const T*>(w.p)[at + element(j, i)]));
       }
   }
+  // The sum over the head's lanes.
   __device__ __forceinline__ float sum(float v) const {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (lanes > o) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
 };
@@ -190,113 +232,200 @@ __device__ __forceinline__ void fill_turns(const NormArgs& a, int nt, int paired
   }
 }
 
+// A lane's parts of the next tokens on their way: asynchronous copies into shared memory that no other lane reads, so
+// that many are in flight without registers; where a part is no whole vectors, the next one in registers.
+template <class P, class T, bool WHOLE, int TENSORS>
+struct Stages {
+  static constexpr int kDepth = WHOLE ? (in_flight(TENSORS == 2) / (P::kBytes * TENSORS) > 2
+                                             ? in_flight(TENSORS == 2) / (P::kBytes * TENSORS)
+                                             : 2)
+                                      : 1;
+  static constexpr int kSize = WHOLE ? kDepth * TENSORS * P::kBytes * P::kThreads : 0;  // shared memory
+  const P& part;
+  uint32_t base;  // this thread's first vector
+  typename P::Raw next[WHOLE ? 1 : TENSORS];
+
+  __device__ __forceinline__ Stages(const P& part, void* smem)
+      : part(part), base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16) {}
+  __device__ __forceinline__ uint32_t at(int stage, int tensor, int vec) const {
+    return base + ((stage * TENSORS + tensor) * (P::kBytes / 16) + vec) * P::kThreads * 16;
+  }
+  __device__ __forceinline__ void issue(int stage, int tensor, const T* p, bool ok) {
+    if constexpr (WHOLE) {
+      part.each([&](int v, int e, bool there) {
+        if (ok && there)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at(stage, tensor, v)), "l"(p + e) : "memory");
+      });
+      if (tensor + 1 == TENSORS) asm volatile("cp.async.commit_group;" ::: "memory");
+    } else {
+      if (ok) part.fetch(p, next[tensor]);
+    }
+  }
+  __device__ __forceinline__ void wait() const {
+    if constexpr (WHOLE) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+  }
+  __device__ __forceinline__ void take(int stage, int tensor, typename P::Raw& r) const {
+    if constexpr (WHOLE) {
+      part.each([&](int v, int e, bool) {
+        uint4 x;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                     : "r"(at(stage, tensor, v))
+                     : "memory");
+        r.vec(v) = *reinterpret_cast<typename P::V*>(&x);
+      });
+    } else {
+      r = next[tensor];
+    }
+  }
+};
+
 template <class T, int VEC, bool HALF, int UPL>
-__global__ void __launch_bounds__(kThreads, 3) k_norm_rotate(const __grid_constant__ NormArgs a) {
-  extern __shared__ __align__(16) float s_turn[];
+__global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 2 : kForward)
+    k_norm_rotate(const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) float s_mem[];
   __shared__ int32_t s_pos[kMaxTile];
   __shared__ int64_t s_slot[kMaxTile];  // element offset of the token's row of kv head 0, -1: skip
   using P = Part<T, VEC, HALF, UPL>;
+  using S = Stages<P, T, VEC != 1, 1>;
+  float* s_turn = s_mem + S::kSize / 4;
   const int tid = threadIdx.x, group = tid >> a.lane_bits, side = a.by_chunk.div(group);
   const P part(a, tid & ((1 << a.lane_bits) - 1));
-  const int t0 = blockIdx.x * a.tile, nt = min(a.tile, a.n_tokens - t0);
+  S stages(part, s_mem);
   const int h = a.first + blockIdx.y * a.chunk + group - side * a.chunk;
   const bool mine = side < a.side && h < a.first + a.heads;
   const bool q = h < a.hq, k = h < a.hq + a.hkv;
   const Heads& src = q ? a.x : k ? a.k : a.v;
   const int hh = q ? h : k ? h - a.hq : h - a.hq - a.hkv;
-  const T* in = static_cast<const T*>(src.p) + (int64_t)t0 * src.ts + (int64_t)hh * src.hs;
+  const int begin = blockIdx.x * a.per, end = min(begin + a.per, a.n_tokens);
+  const T* in = static_cast<const T*>(src.p) + (int64_t)hh * src.hs + (int64_t)(begin + side) * src.ts;
+  const int64_t step = (int64_t)a.side * src.ts;
+  // A token's row is at its number's place in the queries' result, or at its slot of the blocks.
+  T* const base_out = q ? static_cast<T*>(a.out.p) + (int64_t)h * a.out.hs
+                        : static_cast<T*>(k ? a.kb : a.vb) + (int64_t)hh * kBlockTokens * a.d;
   chain_wait();
-  typename P::Raw next;
-  if (mine && side < nt) part.fetch(in + side * src.ts, next);
+  int ahead = mine ? begin + side : end;  // the next token to copy
+  int put_at = 0, take_at = 0;            // its stage, and that of the next one to work on
+  auto issue = [&]() {
+    stages.issue(put_at, 0, in, ahead < end);
+    ahead += a.side;
+    in += step;
+    put_at = put_at + 1 == S::kDepth ? 0 : put_at + 1;
+  };
+#pragma unroll
+  for (int i = 0; i < (S::kDepth > 1 ? S::kDepth - 1 : 1); ++i) issue();
   const HeadWeight& hw = q ? a.wq : a.wk;
   const bool normed = k && hw.p;
   float w[UPL][P::kElems];
   if (normed && mine) part.load_weight(hw, hh, w);
-  if (a.hkv == 0) {
-    if (tid < nt) {
-      s_pos[tid] = __ldcg(a.positions + t0 + tid);
-      s_slot[tid] = 0;
-    }
-  } else if (tid < 32) {
-    const int t = t0 + min(tid, nt - 1);
-    OffsetFinder find(a.b.q_off, a.b.n, t0);
-    const int b = find(t);
-    const int from = __ldcg(a.b.q_off + b), end = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
-    const int64_t pos = (int64_t)len - end + t;
-    const bool ok = from <= t && t < end && end - from <= a.b.max_q && len >= end - from && pos >= 0 &&
-                    len <= kMaxLen && pos < a.b.stride * kBlockTokens;
-    int64_t at = -1;
-    if (ok) {
-      const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
-      if (blk >= 0 && blk < a.n_blocks) at = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
-    }
-    if (tid < nt) {
-      if (at < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
-      s_pos[tid] = a.depth ? len - (end - from) + __ldcg(a.depth + t) : (int32_t)pos;
-      s_slot[tid] = at;
-    }
-  }
-  __syncthreads();
-  fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
-  __syncthreads();
-  for (int base = 0; base < nt; base += a.side) {
-    const int t = base + side;
-    const bool ok = mine && t < nt;
-    typename P::Raw raw = next;
-    if (mine && t + a.side < nt) part.fetch(in + (int64_t)(t + a.side) * src.ts, next);
-    float x[UPL][P::kElems];
-    part.widen(raw, ok, x);
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < UPL; ++j)
-#pragma unroll
-      for (int i = 0; i < P::kElems; ++i) sum = fmaf(x[j][i], x[j][i], sum);
-    sum = part.sum(sum);
-    if (!ok || s_slot[t] < 0) continue;
-    if (k) {
-      if (normed) {
-        const float r = rsqrtf(fmaf(sum, a.inv_d, hw.eps));
-#pragma unroll
-        for (int j = 0; j < UPL; ++j)
-#pragma unroll
-          for (int i = 0; i < P::kElems; ++i) x[j][i] = x[j][i] * r * w[j][i];
+  for (int t0 = begin; t0 < end; t0 += a.tile) {
+    const int nt = min(a.tile, end - t0);
+    if (t0 > begin) __syncthreads();  // the last tile's turns have been read
+    if (a.hkv == 0) {
+      if (tid < nt) {
+        s_pos[tid] = __ldcg(a.positions + t0 + tid);
+        s_slot[tid] = 0;
       }
-      const float* cs = s_turn + t * 2 * a.turns;
-      part.template turn_all<false>(cs, cs + a.turns, x);
-      part.narrow(x, raw);
+    } else if (tid < 32) {
+      const int t = t0 + min(tid, nt - 1);
+      OffsetFinder find(a.b.q_off, a.b.n, t0);
+      const int b = find(t);
+      const int from = __ldcg(a.b.q_off + b), to = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
+      const int64_t pos = (int64_t)len - to + t;
+      const bool ok = from <= t && t < to && to - from <= a.b.max_q && len >= to - from && pos >= 0 &&
+                      len <= kMaxLen && pos < a.b.stride * kBlockTokens;
+      int64_t at = -1;
+      if (ok) {
+        const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
+        if (blk >= 0 && blk < a.n_blocks) at = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
+      }
+      if (tid < nt) {
+        if (at < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
+        s_pos[tid] = a.depth ? len - (to - from) + __ldcg(a.depth + t) : (int32_t)pos;
+        s_slot[tid] = at;
+      }
     }
-    T* o = q ? static_cast<T*>(a.out.p) + (int64_t)(t0 + t) * a.out.ts + (int64_t)h * a.out.hs
-             : static_cast<T*>(k ? a.kb : a.vb) + s_slot[t] + (int64_t)hh * kBlockTokens * a.d;
-    part.put(o, raw);
+    __syncthreads();
+    fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
+    __syncthreads();
+    for (int base = 0; base < nt; base += a.side) {
+      const int t = base + side;
+      const bool ok = mine && t < nt;
+      typename P::Raw raw;
+      if constexpr (S::kDepth > 1) {
+        issue();
+        stages.wait();
+        stages.take(take_at, 0, raw);
+        take_at = take_at + 1 == S::kDepth ? 0 : take_at + 1;
+      } else {
+        stages.take(0, 0, raw);
+        issue();
+      }
+      part.clear_absent(raw);
+      float x[UPL][P::kElems];
+      part.widen(raw, x);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < UPL; ++j)
+#pragma unroll
+        for (int i = 0; i < P::kElems; ++i) sum = fmaf(x[j][i], x[j][i], sum);
+      sum = part.sum(sum);
+      if (!ok || s_slot[t] < 0) continue;
+      if (k) {
+        if (normed) {
+          const float r = rsqrtf(fmaf(sum, a.inv_d, hw.eps));
+#pragma unroll
+          for (int j = 0; j < UPL; ++j)
+#pragma unroll
+            for (int i = 0; i < P::kElems; ++i) x[j][i] = x[j][i] * r * w[j][i];
+        }
+        const float* cs = s_turn + t * 2 * a.turns;
+        part.template turn_all<false>(cs, cs + a.turns, x);
+        part.narrow(x, raw);
+      }
+      part.put(base_out + (q ? (int64_t)(t0 + t) * a.out.ts : s_slot[t]), raw);
+    }
   }
 }
 
 template <class T, int VEC, bool HALF, int UPL>
-__global__ void __launch_bounds__(kThreads, kBackward) k_norm_backward(const __grid_constant__ NormArgs a) {
-  extern __shared__ __align__(16) float s_turn[];
+__global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 1 : kBackward)
+    k_norm_backward(const __grid_constant__ NormArgs a) {
+  extern __shared__ __align__(16) float s_mem[];
   __shared__ int32_t s_pos[kMaxTile];
   using P = Part<T, VEC, HALF, UPL>;
+  using S = Stages<P, T, VEC != 1, 2>;
+  float* s_turn = s_mem + S::kSize / 4;
   const int tid = threadIdx.x, group = tid >> a.lane_bits, side = a.by_chunk.div(group);
   const P part(a, tid & ((1 << a.lane_bits) - 1));
+  S stages(part, s_mem);
   const int h = blockIdx.y * a.chunk + group - side * a.chunk;
   const bool mine = side < a.side && h < a.heads;
-  const int tiles = (a.n_tokens + a.tile - 1) / a.tile;
+  const int begin = blockIdx.x * a.per, end = min(begin + a.per, a.n_tokens);
+  const T* x_in = static_cast<const T*>(a.x.p) + (int64_t)h * a.x.hs + (int64_t)(begin + side) * a.x.ts;
+  const T* g_in = static_cast<const T*>(a.dy.p) + (int64_t)h * a.dy.hs + (int64_t)(begin + side) * a.dy.ts;
+  T* out = static_cast<T*>(a.out.p) + (int64_t)h * a.out.hs + (int64_t)(begin + side) * a.out.ts;
+  const int64_t x_step = (int64_t)a.side * a.x.ts, g_step = (int64_t)a.side * a.dy.ts, step = (int64_t)a.side * a.out.ts;
   chain_wait();
+  int ahead = mine ? begin + side : end, put_at = 0, take_at = 0;
+  auto issue = [&]() {
+    stages.issue(put_at, 0, x_in, ahead < end);
+    stages.issue(put_at, 1, g_in, ahead < end);
+    ahead += a.side;
+    x_in += x_step;
+    g_in += g_step;
+    put_at = put_at + 1 == S::kDepth ? 0 : put_at + 1;
+  };
+#pragma unroll
+  for (int i = 0; i < (S::kDepth > 1 ? S::kDepth - 1 : 1); ++i) issue();
   float w[UPL][P::kElems], dw[UPL][P::kElems];
 #pragma unroll
   for (int j = 0; j < UPL; ++j)
 #pragma unroll
     for (int i = 0; i < P::kElems; ++i) dw[j][i] = 0.f;
   if (mine) part.load_weight(a.wq, h, w);
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int t0 = tile * a.tile, nt = min(a.tile, a.n_tokens - t0);
-    const T* x_in = static_cast<const T*>(a.x.p) + (int64_t)t0 * a.x.ts + (int64_t)h * a.x.hs;
-    const T* g_in = static_cast<const T*>(a.dy.p) + (int64_t)t0 * a.dy.ts + (int64_t)h * a.dy.hs;
-    typename P::Raw next_x, next_g;
-    if (mine && side < nt) {
-      part.fetch(x_in + side * a.x.ts, next_x);
-      part.fetch(g_in + side * a.dy.ts, next_g);
-    }
+  for (int t0 = begin; t0 < end; t0 += a.tile) {
+    const int nt = min(a.tile, end - t0);
     if (tid < nt) s_pos[tid] = __ldcg(a.positions + t0 + tid);
     __syncthreads();
     fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
@@ -304,14 +433,23 @@ __global__ void __launch_bounds__(kThreads, kBackward) k_norm_backward(const __g
     for (int base = 0; base < nt; base += a.side) {
       const int t = base + side;
       const bool ok = mine && t < nt;
-      typename P::Raw raw_x = next_x, raw_g = next_g;
-      if (mine && t + a.side < nt) {
-        part.fetch(x_in + (int64_t)(t + a.side) * a.x.ts, next_x);
-        part.fetch(g_in + (int64_t)(t + a.side) * a.dy.ts, next_g);
+      typename P::Raw raw_x, raw_g;
+      if constexpr (S::kDepth > 1) {
+        issue();
+        stages.wait();
+        stages.take(take_at, 0, raw_x);
+        stages.take(take_at, 1, raw_g);
+        take_at = take_at + 1 == S::kDepth ? 0 : take_at + 1;
+      } else {
+        stages.take(0, 0, raw_x);
+        stages.take(0, 1, raw_g);
+        issue();
       }
       float x[UPL][P::kElems], g[UPL][P::kElems];
-      part.widen(raw_x, ok, x);
-      part.widen(raw_g, ok, g);
+      part.clear_absent(raw_x);
+      part.clear_absent(raw_g);
+      part.widen(raw_x, x);
+      part.widen(raw_g, g);
       const float* cs = s_turn + (ok ? t : 0) * 2 * a.turns;
       part.template turn_all<true>(cs, cs + a.turns, g);
       float squares = 0.f, dot = 0.f;
@@ -320,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, kBackward) k_norm_backward(const __g
 #pragma unroll
         for (int i = 0; i < P::kElems; ++i) {
           squares = fmaf(x[j][i], x[j][i], squares);
-          if (part.has_element(j, i)) dot = fmaf(g[j][i] * w[j][i], x[j][i], dot);
+          dot = fmaf(g[j][i] * w[j][i], x[j][i], dot);
         }
       squares = part.sum(squares);
       dot = part.sum(dot);
@@ -335,12 +473,15 @@ __global__ void __launch_bounds__(kThreads, kBackward) k_norm_backward(const __g
           x[j][i] = r * fmaf(-u, m, g[j][i] * w[j][i]);
         }
       part.narrow(x, raw_x);
-      part.put(static_cast<T*>(a.out.p) + (int64_t)(t0 + t) * a.out.ts + (int64_t)h * a.out.hs, raw_x);
+      part.put(out, raw_x);
+      out += step;
     }
     __syncthreads();  // the next tile's turns come where these were read
   }
   // The CTA's sum: over its tokens side by side, and over its heads where they share the weight.
-  float* red = s_turn;  // [groups][d]
+  if constexpr (S::kDepth > 1) asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  float* red = s_mem;  // [groups][d]
   if (mine) {
 #pragma unroll
     for (int j = 0; j < UPL; ++j)
@@ -411,22 +552,26 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   g.upl = vec ? (a.units > 32 ? 2 : 1) : 8;
   a.lane_bits = 0;
   while ((g.upl << a.lane_bits) < a.units) ++a.lane_bits;
-  // All heads of a token in one CTA where they fit, else equal parts of them; the rest of the CTA takes other tokens.
-  const int slots = kThreads >> a.lane_bits, chunks = (a.heads + slots - 1) / slots;
-  a.chunk = (a.heads + chunks - 1) / chunks;
-  a.side = std::min(slots / a.chunk, kMaxTile);
-  a.by_chunk.set(a.chunk);
-  g.y = (a.heads + a.chunk - 1) / a.chunk;
-  g.threads = ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
-  // As many tokens a CTA as leave several CTAs for each SM.
-  a.tile = a.side;
-  while (a.tile * 2 <= kMaxTile && (int64_t)((a.n_tokens - 1) / (a.tile * 2) + 1) * g.y >= (int64_t)num_sms * 8)
-    a.tile *= 2;
-  g.x = (a.n_tokens - 1) / a.tile + 1;
-  if (backward) g.x = std::min(g.x, std::max(1, num_sms * kBackward / g.y));
   const int pairs = vec ? (half_layout ? n : n / 2) : 1;
   a.turns = (a.rot / 2 + pairs - 1) / pairs * pairs;
-  g.smem = sizeof(float) * 2 * a.turns * a.tile;
+  // What the copies in flight leave of the shared memory holds the turns of a tile's tokens.
+  const int threads = threads_of(g.upl), bytes = g.upl * (half_layout ? 32 : 16) * (backward ? 2 : 1);
+  const int ring = vec ? std::max(2, in_flight(backward) / bytes) * bytes * threads : 0, turn = 8 * a.turns;
+  const int room = turn ? std::min(kMaxTile, (kShared - ring) / turn) : kMaxTile;
+  // All heads of a token in one CTA where they fit, else equal parts of them; the rest of the CTA takes other tokens.
+  const int slots = threads >> a.lane_bits, chunks = (a.heads + slots - 1) / slots;
+  a.chunk = (a.heads + chunks - 1) / chunks;
+  a.side = std::min(slots / a.chunk, room);
+  a.by_chunk.set(a.chunk);
+  g.y = (a.heads + a.chunk - 1) / a.chunk;
+  g.threads = vec ? threads : ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
+  // As many CTAs as the GPU holds at a time, with equally many tokens each.
+  const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * (backward ? kBackward : kForward) / g.y);
+  a.per = (rounds - 1) / std::min(rounds, most) + 1;
+  g.x = (rounds - 1) / a.per + 1;
+  a.per *= a.side;
+  a.tile = std::min(a.per, room / a.side * a.side);
+  g.smem = ring + turn * a.tile;
   if (backward) g.smem = std::max(g.smem, sizeof(float) * a.side * a.chunk * a.d);
   return g;
 }
