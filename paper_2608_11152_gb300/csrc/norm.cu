@@ -16,6 +16,7 @@
 
 #include "kv.h"
 #include "rotary.cuh"
+#include "tensor.cuh"
 
 using namespace misat;
 
@@ -23,17 +24,29 @@ namespace {
 
 constexpr int kMaxTile = 32;   // tokens of a CTA at a time: their places are found by one warp
 constexpr int kMaxHead = 256;  // elements
-constexpr int kForward = 4, kBackward = 2;  // CTAs on an SM
-constexpr int kShared = 47 * 1024;          // dynamic bytes of a CTA, at most 48 KiB with the places of its tokens
-// Threads of a CTA, and copies in flight of a thread: bytes.  (A head of more than 32 units has two a lane.)
-constexpr int threads_of(int upl) { return upl == 2 ? 128 : 256; }
-constexpr int in_flight(bool backward) { return backward ? 128 : 96; }
+constexpr int kShared = 47 * 1024;  // dynamic bytes of a CTA, at most 48 KiB with the places of its tokens
+
+// By the elements of a lane and the bytes of its part of a token: threads of a CTA, CTAs on an SM, copies in flight.
+struct Shape {
+  int threads, ctas, depth;
+};
+constexpr Shape shape_of(int elements, int bytes, bool backward) {
+  if (backward) {
+    if (elements > 16) return {128, 3, 3};
+    if (bytes > 64) return {128, 3, 2};
+    return {256, 2, 128 / bytes};
+  }
+  if (elements > 16) return {256, 3, 3};
+  if (bytes > 48) return {128, 6, 2};
+  return {256, 4, 96 / bytes};
+}
 
 struct HeadWeight {
   const void* p;  // nullptr: no norm
   int64_t hs;
   float eps, offset;
-  bool wide;  // 32 bits, else the tensor's type
+  bool wide;   // 32 bits, else the tensor's type
+  bool whole;  // heads at 16-byte boundaries
 };
 
 struct NormArgs {
@@ -75,7 +88,9 @@ struct Part {
   static constexpr int kPairs = HALF ? VEC : kPair ? 1 : VEC / 2;  // pairs of a unit
   static constexpr int kElems = kTwo ? 2 * VEC : VEC;        // elements of a unit
   static constexpr int kBytes = UPL * kElems * (int)sizeof(T);
-  static constexpr int kThreads = threads_of(UPL);
+  static constexpr Shape shape(bool backward) {
+    return VEC == 1 ? Shape{256, backward ? 1 : 2, 1} : shape_of(UPL * kElems, kBytes * (backward ? 2 : 1), backward);
+  }
 
   int half, paired, units, d, lane, lanes;
   __device__ __forceinline__ Part(const NormArgs& a, int lane)
@@ -181,6 +196,18 @@ struct Part {
           s[k] = sines[unit(j) * kPairs + k];
         }
       }
+      if constexpr (kTwo && kPairs > 1) {  // two pairs at a time
+#pragma unroll
+        for (int k = 0; k < kPairs; k += 2) {
+          const uint64_t u = pack2(x[j][k], x[j][k + 1]), w = pack2(x[j][VEC + k], x[j][VEC + k + 1]);
+          const uint64_t cc = pack2(c[k], c[k + 1]), ss = pack2(s[k], s[k + 1]);
+          const uint64_t first = BACK ? fma2(w, ss, mul2(u, cc)) : sub2(mul2(u, cc), mul2(w, ss));
+          const uint64_t second = BACK ? sub2(mul2(w, cc), mul2(u, ss)) : fma2(u, ss, mul2(w, cc));
+          unpack2(first, x[j][k], x[j][k + 1]);
+          unpack2(second, x[j][VEC + k], x[j][VEC + k + 1]);
+        }
+        continue;
+      }
       auto pairs = [&](bool ends) {
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) {
@@ -198,17 +225,29 @@ struct Part {
       else pairs(true);
     }
   }
-  __device__ __forceinline__ void load_weight(const HeadWeight& w, int head, float (&out)[UPL][kElems]) const {
-    const int64_t at = (int64_t)head * w.hs;
+  template <class W>
+  __device__ __forceinline__ void load_weight(const W* w, bool whole, float offset, float (&out)[UPL][kElems]) const {
+    constexpr int N = VEC > 1 ? 16 / (int)sizeof(W) : 1;  // of a vector
 #pragma unroll
     for (int j = 0; j < UPL; ++j)
 #pragma unroll
-      for (int i = 0; i < kElems; ++i) {
-        out[j][i] = 1.f;
-        if (w.p && has_element(j, i))
-          out[j][i] = w.offset + (w.wide ? static_cast<const float*>(w.p)[at + element(j, i)]
-                                         : to_f(static_cast<const T*>(w.p)[at + element(j, i)]));
+      for (int i = 0; i < kElems; i += N) {
+        Vec<W, N> v{};
+        if (N > 1 && whole) {
+          if (has_element(j, i)) v = *reinterpret_cast<const Vec<W, N>*>(w + element(j, i));
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (has_element(j, i + e)) v.e[e] = w[element(j, i + e)];
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[j][i + e] = offset + to_f(v.e[e]);
       }
+  }
+  __device__ __forceinline__ void load_weight(const HeadWeight& w, int head, float (&out)[UPL][kElems]) const {
+    const int64_t at = (int64_t)head * w.hs;
+    if (w.wide) load_weight(static_cast<const float*>(w.p) + at, w.whole, w.offset, out);
+    else load_weight(static_cast<const T*>(w.p) + at, w.whole, w.offset, out);
   }
   // The sum over the head's lanes.
   __device__ __forceinline__ float sum(float v) const {
@@ -218,6 +257,20 @@ struct Part {
     return v;
   }
 };
+
+// Sum of products of a lane's elements.
+template <int U, int E>
+__device__ __forceinline__ float dot(const float (&x)[U][E], const float (&y)[U][E]) {
+  uint64_t sum = 0;
+#pragma unroll
+  for (int j = 0; j < U; ++j)
+#pragma unroll
+    for (int i = 0; i < E; i += 2)
+      sum = fma2(pack2(x[j][i], x[j][i + 1]), pack2(y[j][i], y[j][i + 1]), sum);
+  float a, b;
+  unpack2(sum, a, b);
+  return a + b;
+}
 
 // The tile's cosines and sines: [tokens][2][turns].
 template <class P>
@@ -236,11 +289,9 @@ __device__ __forceinline__ void fill_turns(const NormArgs& a, int nt, int paired
 // that many are in flight without registers; where a part is no whole vectors, the next one in registers.
 template <class P, class T, bool WHOLE, int TENSORS>
 struct Stages {
-  static constexpr int kDepth = WHOLE ? (in_flight(TENSORS == 2) / (P::kBytes * TENSORS) > 2
-                                             ? in_flight(TENSORS == 2) / (P::kBytes * TENSORS)
-                                             : 2)
-                                      : 1;
-  static constexpr int kSize = WHOLE ? kDepth * TENSORS * P::kBytes * P::kThreads : 0;  // shared memory
+  static constexpr int kThreads = P::shape(TENSORS == 2).threads;
+  static constexpr int kDepth = P::shape(TENSORS == 2).depth;
+  static constexpr int kSize = WHOLE ? kDepth * TENSORS * P::kBytes * kThreads : 0;  // shared memory
   const P& part;
   uint32_t base;  // this thread's first vector
   typename P::Raw next[WHOLE ? 1 : TENSORS];
@@ -248,7 +299,7 @@ struct Stages {
   __device__ __forceinline__ Stages(const P& part, void* smem)
       : part(part), base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16) {}
   __device__ __forceinline__ uint32_t at(int stage, int tensor, int vec) const {
-    return base + ((stage * TENSORS + tensor) * (P::kBytes / 16) + vec) * P::kThreads * 16;
+    return base + ((stage * TENSORS + tensor) * (P::kBytes / 16) + vec) * kThreads * 16;
   }
   __device__ __forceinline__ void issue(int stage, int tensor, const T* p, bool ok) {
     if constexpr (WHOLE) {
@@ -281,7 +332,8 @@ struct Stages {
 };
 
 template <class T, int VEC, bool HALF, int UPL>
-__global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 2 : kForward)
+__global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
+                                  Part<T, VEC, HALF, UPL>::shape(false).ctas)
     k_norm_rotate(const __grid_constant__ NormArgs a) {
   extern __shared__ __align__(16) float s_mem[];
   __shared__ int32_t s_pos[kMaxTile];
@@ -321,32 +373,31 @@ __global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 2 : kForward)
   for (int t0 = begin; t0 < end; t0 += a.tile) {
     const int nt = min(a.tile, end - t0);
     if (t0 > begin) __syncthreads();  // the last tile's turns have been read
+    int64_t pos = 0;
+    int blk = -1;
     if (a.hkv == 0) {
       if (tid < nt) {
         s_pos[tid] = __ldcg(a.positions + t0 + tid);
         s_slot[tid] = 0;
       }
     } else if (tid < 32) {
-      const int t = t0 + min(tid, nt - 1);
+      const int t = t0 + min(tid, nt - 1), depth = a.depth ? __ldcg(a.depth + t) : 0;
       OffsetFinder find(a.b.q_off, a.b.n, t0);
-      const int b = find(t);
-      const int from = __ldcg(a.b.q_off + b), to = __ldcg(a.b.q_off + b + 1), len = __ldcg(a.b.kv_len + b);
-      const int64_t pos = (int64_t)len - to + t;
+      int from, to;
+      const int b = find(t, from, to), len = __ldcg(a.b.kv_len + b);
+      pos = (int64_t)len - to + t;
       const bool ok = from <= t && t < to && to - from <= a.b.max_q && len >= to - from && pos >= 0 &&
                       len <= kMaxLen && pos < a.b.stride * kBlockTokens;
-      int64_t at = -1;
-      if (ok) {
-        const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
-        if (blk >= 0 && blk < a.n_blocks) at = ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d;
-      }
-      if (tid < nt) {
-        if (at < 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
-        s_pos[tid] = a.depth ? len - (to - from) + __ldcg(a.depth + t) : (int32_t)pos;
-        s_slot[tid] = at;
-      }
+      if (ok) blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
+      if (tid < nt) s_pos[tid] = a.depth ? len - (to - from) + depth : (int32_t)pos;
     }
     __syncthreads();
     fill_turns<P>(a, nt, part.paired, s_pos, s_turn);
+    if (a.hkv > 0 && tid < nt) {  // (the block's number arrives meanwhile)
+      const bool ok = blk >= 0 && blk < a.n_blocks;
+      if (!ok) set_error(a.err, MISAT_ERR_INVALID_ARG);
+      s_slot[tid] = ok ? ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d : -1;
+    }
     __syncthreads();
     for (int base = 0; base < nt; base += a.side) {
       const int t = base + side;
@@ -364,20 +415,17 @@ __global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 2 : kForward)
       part.clear_absent(raw);
       float x[UPL][P::kElems];
       part.widen(raw, x);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < UPL; ++j)
-#pragma unroll
-        for (int i = 0; i < P::kElems; ++i) sum = fmaf(x[j][i], x[j][i], sum);
-      sum = part.sum(sum);
+      const float sum = part.sum(dot(x, x));
       if (!ok || s_slot[t] < 0) continue;
       if (k) {
         if (normed) {
           const float r = rsqrtf(fmaf(sum, a.inv_d, hw.eps));
+          const uint64_t r2 = pack2(r, r);
 #pragma unroll
           for (int j = 0; j < UPL; ++j)
 #pragma unroll
-            for (int i = 0; i < P::kElems; ++i) x[j][i] = x[j][i] * r * w[j][i];
+            for (int i = 0; i < P::kElems; i += 2)
+              unpack2(mul2(mul2(pack2(x[j][i], x[j][i + 1]), r2), pack2(w[j][i], w[j][i + 1])), x[j][i], x[j][i + 1]);
         }
         const float* cs = s_turn + t * 2 * a.turns;
         part.template turn_all<false>(cs, cs + a.turns, x);
@@ -389,7 +437,8 @@ __global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 2 : kForward)
 }
 
 template <class T, int VEC, bool HALF, int UPL>
-__global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 1 : kBackward)
+__global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(true).threads,
+                                  Part<T, VEC, HALF, UPL>::shape(true).ctas)
     k_norm_backward(const __grid_constant__ NormArgs a) {
   extern __shared__ __align__(16) float s_mem[];
   __shared__ int32_t s_pos[kMaxTile];
@@ -452,25 +501,24 @@ __global__ void __launch_bounds__(threads_of(UPL), VEC == 1 ? 1 : kBackward)
       part.widen(raw_g, g);
       const float* cs = s_turn + (ok ? t : 0) * 2 * a.turns;
       part.template turn_all<true>(cs, cs + a.turns, g);
-      float squares = 0.f, dot = 0.f;
+      const float squares = part.sum(dot(x, x));
+      float aw[UPL][P::kElems];  // g w
 #pragma unroll
       for (int j = 0; j < UPL; ++j)
 #pragma unroll
-        for (int i = 0; i < P::kElems; ++i) {
-          squares = fmaf(x[j][i], x[j][i], squares);
-          dot = fmaf(g[j][i] * w[j][i], x[j][i], dot);
-        }
-      squares = part.sum(squares);
-      dot = part.sum(dot);
+        for (int i = 0; i < P::kElems; i += 2)
+          unpack2(mul2(pack2(g[j][i], g[j][i + 1]), pack2(w[j][i], w[j][i + 1])), aw[j][i], aw[j][i + 1]);
+      const float along = part.sum(dot(aw, x));
       if (!ok) continue;
-      const float r = rsqrtf(fmaf(squares, a.inv_d, a.wq.eps)), m = r * dot * a.inv_d;
+      const float r = rsqrtf(fmaf(squares, a.inv_d, a.wq.eps)), m = r * along * a.inv_d;
+      const uint64_t r2 = pack2(r, r), m2 = pack2(-m, -m);
 #pragma unroll
       for (int j = 0; j < UPL; ++j)
 #pragma unroll
-        for (int i = 0; i < P::kElems; ++i) {
-          const float u = x[j][i] * r;
-          dw[j][i] = fmaf(g[j][i], u, dw[j][i]);
-          x[j][i] = r * fmaf(-u, m, g[j][i] * w[j][i]);
+        for (int i = 0; i < P::kElems; i += 2) {
+          const uint64_t u = mul2(pack2(x[j][i], x[j][i + 1]), r2);
+          unpack2(fma2(pack2(g[j][i], g[j][i + 1]), u, pack2(dw[j][i], dw[j][i + 1])), dw[j][i], dw[j][i + 1]);
+          unpack2(mul2(r2, fma2(u, m2, pack2(aw[j][i], aw[j][i + 1]))), x[j][i], x[j][i + 1]);
         }
       part.narrow(x, raw_x);
       part.put(out, raw_x);
@@ -549,14 +597,24 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   g.vec = vec;
   if (vec) a.units = half_layout ? a.rot / 2 / n + (a.d - a.rot) / n : a.d / n;
   else a.units = half_layout ? a.d - a.rot / 2 : (a.d + 1) / 2;
-  g.upl = vec ? (a.units > 32 ? 2 : 1) : 8;
-  a.lane_bits = 0;
-  while ((g.upl << a.lane_bits) < a.units) ++a.lane_bits;
+  const auto lanes_for = [&](int upl) {
+    int bits = 0;
+    while ((upl << bits) < a.units) ++bits;
+    return bits;
+  };
+  // Units of a lane: one of the half layout's, as they are 16 elements (in 32 bits 8: two where a warp is too small);
+  // else two or three, whichever leaves fewer places of the lanes empty.
+  if (!vec) g.upl = 8;
+  else if (half_layout) g.upl = a.units > 32 ? 2 : 1;
+  else g.upl = 3 << lanes_for(3) < 2 << lanes_for(2) ? 3 : 2;
+  a.lane_bits = lanes_for(g.upl);
   const int pairs = vec ? (half_layout ? n : n / 2) : 1;
   a.turns = (a.rot / 2 + pairs - 1) / pairs * pairs;
   // What the copies in flight leave of the shared memory holds the turns of a tile's tokens.
-  const int threads = threads_of(g.upl), bytes = g.upl * (half_layout ? 32 : 16) * (backward ? 2 : 1);
-  const int ring = vec ? std::max(2, in_flight(backward) / bytes) * bytes * threads : 0, turn = 8 * a.turns;
+  const int elements = vec ? g.upl * n * (half_layout ? 2 : 1) : 0, bytes = elements * elem * (backward ? 2 : 1);
+  const Shape shape = vec ? shape_of(elements, bytes, backward) : Shape{256, backward ? 1 : 2, 1};
+  const int threads = shape.threads, turn = 8 * a.turns;
+  const int ring = vec ? shape.depth * bytes * threads : 0;
   const int room = turn ? std::min(kMaxTile, (kShared - ring) / turn) : kMaxTile;
   // All heads of a token in one CTA where they fit, else equal parts of them; the rest of the CTA takes other tokens.
   const int slots = threads >> a.lane_bits, chunks = (a.heads + slots - 1) / slots;
@@ -566,7 +624,7 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   g.y = (a.heads + a.chunk - 1) / a.chunk;
   g.threads = vec ? threads : ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
   // As many CTAs as the GPU holds at a time, with equally many tokens each.
-  const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * (backward ? kBackward : kForward) / g.y);
+  const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * shape.ctas / g.y);
   a.per = (rounds - 1) / std::min(rounds, most) + 1;
   g.x = (rounds - 1) / a.per + 1;
   a.per *= a.side;
@@ -599,23 +657,21 @@ void launch(void (*kernel)(P...), const Grid& g, cudaStream_t st, A&&... args) {
   cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
 }
 
-template <class T, int VEC, int UPL>
-void launch_part(const NormArgs& a, const Grid& g, bool half_layout, bool backward, cudaStream_t st) {
-  if (backward) {
-    if (half_layout) launch(k_norm_backward<T, VEC, true, UPL>, g, st, a);
-    else launch(k_norm_backward<T, VEC, false, UPL>, g, st, a);
-  } else {
-    if (half_layout) launch(k_norm_rotate<T, VEC, true, UPL>, g, st, a);
-    else launch(k_norm_rotate<T, VEC, false, UPL>, g, st, a);
-  }
+template <class T, int VEC, bool HALF, int UPL>
+void launch_part(const NormArgs& a, const Grid& g, bool backward, cudaStream_t st) {
+  if (backward) launch(k_norm_backward<T, VEC, HALF, UPL>, g, st, a);
+  else launch(k_norm_rotate<T, VEC, HALF, UPL>, g, st, a);
 }
 template <class T>
 void launch_t(const NormArgs& a, const Grid& g, bool half_layout, bool backward, cudaStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
-  if (!g.vec) return launch_part<T, 1, 8>(a, g, half_layout, backward, st);
+  if (!g.vec) return half_layout ? launch_part<T, 1, true, 8>(a, g, backward, st)
+                                 : launch_part<T, 1, false, 8>(a, g, backward, st);
+  if (!half_layout) return g.upl == 3 ? launch_part<T, VEC, false, 3>(a, g, backward, st)
+                                      : launch_part<T, VEC, false, 2>(a, g, backward, st);
   if constexpr (sizeof(T) == 4)
-    if (g.upl == 2) return launch_part<T, VEC, 2>(a, g, half_layout, backward, st);
-  launch_part<T, VEC, 1>(a, g, half_layout, backward, st);
+    if (g.upl == 2) return launch_part<T, VEC, true, 2>(a, g, backward, st);
+  launch_part<T, VEC, true, 1>(a, g, backward, st);
 }
 void launch_norm(const NormArgs& a, const Grid& g, int dtype, bool half_layout, bool backward, cudaStream_t st) {
   if (dtype == MISAT_BF16) launch_t<__nv_bfloat16>(a, g, half_layout, backward, st);
@@ -632,7 +688,9 @@ bool norm_ok(const misat_head_norm* n, int dtype, int heads, int d) {
 }
 HeadWeight weight_of(const misat_head_norm* n) {
   if (!n) return {};
-  return {n->weight, n->head_stride, n->eps, n->offset, n->dtype == MISAT_F32};
+  const int elem = n->dtype == MISAT_F32 ? 4 : 2;
+  return {n->weight, n->head_stride, n->eps, n->offset, elem == 4,
+          ((reinterpret_cast<uintptr_t>(n->weight) | (uintptr_t)(n->head_stride * elem)) & 15) == 0};
 }
 
 bool sizes_ok(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens, int32_t n_heads,

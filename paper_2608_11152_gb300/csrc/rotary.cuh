@@ -55,10 +55,10 @@ __device__ __forceinline__ float2 turn(int32_t pos, uint64_t freq, float attn, b
 
 // The sequence of token t: the last b in [0, n) with q_off[b] <= t, found by a warp 32 offsets at
 // a time (two rounds for 1,024 sequences; each round is one memory latency).  Bounded for
-// malformed offsets: the range shrinks in every round.
-__device__ __forceinline__ int find_sequence(const int32_t* q_off, int n, int t, int lane) {
+// malformed offsets: the range shrinks in every round.  many: stops where that many are left, and returns the first.
+__device__ __forceinline__ int find_sequence(const int32_t* q_off, int n, int t, int lane, int many = 1) {
   int lo = 0, hi = n;  // the answer is in [lo, hi)
-  while (hi - lo > 1) {
+  while (hi - lo > many) {
     const int step = (hi - lo + 31) / 32;
     const int i = lo + lane * step;
     const bool le = i < hi && (i == lo || __ldcg(q_off + i) <= t);
@@ -79,11 +79,17 @@ struct OffsetFinder {
     mine = base + lane <= n ? __ldcg(off + base + lane) : 0x7fffffff;
   }
   __device__ __forceinline__ OffsetFinder(const int32_t* off, int n, int t) : off(off), n(n), lane(threadIdx.x & 31) {
-    load(find_sequence(off, n, t, lane));
+    load(find_sequence(off, n, t, lane, 32));
   }
-  // All lanes call it, each with its item, in rising order over the calls; items of a call lie 32 apart at most.
+  // All lanes call it, each with its item, in rising order over the calls; items of a call lie 32 apart at most.  from, to:
+  // off[b] and off[b + 1].
   __device__ __forceinline__ int operator()(int t) {
+    int from, to;
+    return operator()(t, from, to);
+  }
+  __device__ __forceinline__ int operator()(int t, int& from, int& to) {
     int b = -1;
+    from = to = 0;
 #pragma unroll 1
     while (true) {
       int lo = 0;  // the last of the 32 offsets that is at most t
@@ -93,7 +99,12 @@ struct OffsetFinder {
         if (v <= t) lo += o;
       }
       const bool beyond = lo == 31 && base + 31 < n;  // the next offsets may be at most t too
-      if (b < 0 && !beyond) b = base + lo;
+      const int first = __shfl_sync(0xffffffffu, mine, lo), second = __shfl_sync(0xffffffffu, mine, min(lo + 1, 31));
+      if (b < 0 && !beyond) {
+        b = base + lo;
+        from = first;
+        to = lo < 31 ? second : __ldcg(off + b + 1);
+      }
       if (!__any_sync(0xffffffffu, b < 0)) return min(b, n - 1);
       load(base + 31);
     }
