@@ -81,7 +81,7 @@ struct OffsetFinder {
   __device__ __forceinline__ OffsetFinder(const int32_t* off, int n, int t) : off(off), n(n), lane(threadIdx.x & 31) {
     load(find_sequence(off, n, t, lane, 32));
   }
-  // All lanes call it, each with its item, in rising order over the calls; items of a call lie 32 apart at most.  from, to:
+  // All lanes call it, each with its item, in rising order over the lanes and the calls.  from, to:
   // off[b] and off[b + 1].
   __device__ __forceinline__ int operator()(int t) {
     int from, to;
