@@ -626,10 +626,10 @@ typedef struct misat_kv_step {
   int32_t* positions;        /* [n_tokens] position of each new token */
   int64_t* slots;            /* [n_tokens] its slot: 16 block + position % 16 */
 } misat_kv_step;
-/* work: device scratch of MISAT_KV_TABLES_WORK(n) bytes, 4-byte aligned, the call's own until it
+/* work: device scratch of MISAT_KV_TABLES_WORK(n) bytes, 16-byte aligned, the call's own until it
  * is finished.  Writes what a misat_kv_batch of this step takes.  [async]
  * Errors: INVALID_ARG, CUDA; OOM and INVALID_ARG later. */
-#define MISAT_KV_TABLES_WORK(n) (16 * (int64_t)(n) + 32)
+#define MISAT_KV_TABLES_WORK(n) (24 * (int64_t)(n) + 64)
 int misat_kv_tables(misat_kv* kv, const misat_kv_step* step, void* work, int64_t work_bytes, void* cuda_stream);
 
 /* Norm of each head, and the rotation behind it:

@@ -11,6 +11,7 @@
 //
 // Bound by latency in a step of single tokens, by the 12 bytes a token in a round of prompts.
 #include <algorithm>
+#include <initializer_list>
 
 #include "kv.h"
 #include "rotary.cuh"
@@ -22,7 +23,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kThreads = 256;
 constexpr int kEach = 4;                   // tokens of a lane side by side
-constexpr int kAhead = 4;                  // times that many tokens of a warp on their way together
+constexpr int kAhead = 2;                  // times that many tokens of a warp on their way together
 constexpr int kRun = 32 * kEach * kAhead;  // tokens of a warp at a time
 constexpr int kGiveRun = 128;              // blocks given back
 constexpr int kFillTokens = 4096;          // most tokens of a step that one CTA makes
@@ -42,11 +43,18 @@ struct TableArgs {
   int32_t* positions;
   int64_t* slots;
   int32_t* err;
-  // What the second kernel needs of the first: per sequence blocks held before, blocks taken and given before it, first
-  // block given; then Head.
-  int32_t *held, *take_off, *give_off, *give_from, *head;
-  bool whole;  // positions and slots at 16-byte boundaries
+  // What the second kernel needs of the first: Head, a Mark of each sequence and of the end, blocks given before each,
+  // first block given of each.
+  int32_t* head;
+  int4* marks;
+  int32_t *give_off, *give_from;
+  bool vec_rows, vec_tokens;  // what is read and written of each sequence, and of each token, at 16-byte boundaries
 };
+// Of a sequence: first new token, length after the step, blocks held before it, blocks taken before it.
+struct Mark {
+  int off, len, held, take;
+};
+__device__ __forceinline__ Mark as_mark(int4 v) { return {v.x, v.y, v.z, v.w}; }
 enum Head { kOk, kRingHead, kGiveBase, kGiven, kHeadWords };
 
 // Sums that stay at the largest number where they would pass it: malformed counts cannot wrap around.
@@ -68,10 +76,7 @@ struct Row {
     return {(uint32_t)fresh, (uint32_t)max(need() - held, 0), (uint32_t)max(held - from, 0)};
   }
 };
-__device__ __forceinline__ Row load_row(const TableArgs& a, int b) {
-  if (b >= a.n) return {0, 0, 0, 0, true};
-  const int fresh = __ldcg(a.fresh + b), before = __ldcg(a.kv_len + b), held = __ldcg(a.state + b);
-  const int shared = a.shared ? __ldcg(a.shared + b) : 0;
+__device__ __forceinline__ Row row_of(const TableArgs& a, int fresh, int before, int held, int shared) {
   // A row holds blocks for the tokens that are there, and has room for those to come.
   const bool ok = fresh >= 0 && fresh <= a.max_q && before >= 0 && before <= kMaxLen && fresh <= kMaxLen - before &&
                   held >= 0 && held <= a.columns && (int64_t)before <= (int64_t)held * kBlockTokens && shared >= 0 &&
@@ -81,12 +86,40 @@ __device__ __forceinline__ Row load_row(const TableArgs& a, int b) {
   r.from = max(r.need(), shared);
   return r;
 }
-
-// What the tokens' places follow from, in memory between two kernels or in shared memory.
-struct Plan {
-  const int32_t *q_off, *len, *held, *take_off, *give_off, *give_from;
-  int ring_head, give_base, given;
-};
+// EACH sequences from b on; those past the last are empty.
+template <int EACH>
+__device__ __forceinline__ void load_rows(const TableArgs& a, int b, Row (&r)[EACH]) {
+  if constexpr (EACH == 4) {
+    if (a.vec_rows && b + EACH <= a.n) {
+      const auto four = [&](const int32_t* p) { return __ldcg(reinterpret_cast<const int4*>(p + b)); };
+      const int4 f = four(a.fresh), l = four(a.kv_len), h = four(a.state), s = a.shared ? four(a.shared) : int4{};
+      r[0] = row_of(a, f.x, l.x, h.x, s.x);
+      r[1] = row_of(a, f.y, l.y, h.y, s.y);
+      r[2] = row_of(a, f.z, l.z, h.z, s.z);
+      r[3] = row_of(a, f.w, l.w, h.w, s.w);
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    r[i] = Row{0, 0, 0, 0, true};
+    if (b + i < a.n)
+      r[i] = row_of(a, __ldcg(a.fresh + b + i), __ldcg(a.kv_len + b + i), __ldcg(a.state + b + i),
+                    a.shared ? __ldcg(a.shared + b + i) : 0);
+  }
+}
+template <int EACH>
+__device__ __forceinline__ void store_rows(const TableArgs& a, int32_t* p, int b, const int (&v)[EACH]) {
+  if constexpr (EACH == 4) {
+    if (a.vec_rows && b + EACH <= a.n) {
+      *reinterpret_cast<int4*>(p + b) = make_int4(v[0], v[1], v[2], v[3]);
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (b + i < a.n) p[b + i] = v[i];
+}
 
 __device__ __forceinline__ int ring_place(const TableArgs& a, int first, int i) {
   const int64_t p = (int64_t)first + i;
@@ -106,10 +139,9 @@ __device__ __forceinline__ Place place_of(const TableArgs& a, int b, int col, in
   return {a.ring + ring_place(a, ring_head, k), row};
 }
 // One block given back: the j-th of all.
-__device__ __forceinline__ void give(const TableArgs& a, const Plan& p, int b, int j, int from, int off) {
+__device__ __forceinline__ void give(const TableArgs& a, int base, int b, int j, int from, int off) {
   const int col = from + j - off;
-  if (col >= 0 && col < a.columns)
-    a.ring[ring_place(a, p.give_base, j)] = __ldcg(a.table + (int64_t)b * a.stride + col);
+  if (col >= 0 && col < a.columns) a.ring[ring_place(a, base, j)] = __ldcg(a.table + (int64_t)b * a.stride + col);
 }
 
 // The last i with off[i] <= t, off in shared memory with off[n] > t.
@@ -161,8 +193,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
   Row r[EACH];
   auto load = [&](int b0) {
     Sums mine{0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) r[i] = load_row(a, b0 + tid * EACH + i);
+    load_rows(a, b0 + tid * EACH, r);
 #pragma unroll
     for (int i = 0; i < EACH; ++i) mine.add(r[i].sums());
     return mine;
@@ -188,37 +219,41 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
       at.add(base);
       base.add(all);
     }
+    const int b = b0 + tid * EACH;
+    int off[EACH], len[EACH], need[EACH], given[EACH], from[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int b = b0 + tid * EACH + i;
-      if (b >= a.n) break;
-      if (go) {
+      off[i] = go ? (int)at.fresh : 0;
+      len[i] = r[i].len;
+      need[i] = r[i].need();
+      given[i] = (int)at.give;
+      from[i] = r[i].from;
+      if (go && b + i < a.n) {
         if constexpr (FILL) {
-          s_q[b] = (int)at.fresh;
-          s_len[b] = r[i].len;
+          s_q[b] = off[i];
+          s_len[b] = len[i];
           s_held[b] = r[i].held;
           s_take[b] = (int)at.take;
-          s_give[b] = (int)at.give;
-          s_from[b] = r[i].from;
+          s_give[b] = given[i];
+          s_from[b] = from[i];
         } else {
-          a.held[b] = r[i].held;
-          a.take_off[b] = (int)at.take;
-          a.give_off[b] = (int)at.give;
-          a.give_from[b] = r[i].from;
+          a.marks[b + i] = make_int4(off[i], len[i], r[i].held, (int)at.take);
         }
-        a.q_off[b] = (int)at.fresh;
-        a.kv_len_out[b] = r[i].len;
-        a.state_out[b] = r[i].need();
-      } else {
-        a.q_off[b] = 0;
-        if (a.kv_len_out != a.kv_len) a.kv_len_out[b] = __ldcg(a.kv_len + b);
-        if (a.state_out != a.state) a.state_out[b] = __ldcg(a.state + b);
+      } else if (b + i < a.n) {
+        len[i] = __ldcg(a.kv_len + b + i);
+        need[i] = __ldcg(a.state + b + i);
       }
       at.add(r[i].sums());
     }
+    store_rows(a, a.q_off, b, off);
+    store_rows(a, a.kv_len_out, b, len);
+    store_rows(a, a.state_out, b, need);
+    if constexpr (!FILL) {
+      store_rows(a, a.give_off, b, given);
+      store_rows(a, a.give_from, b, from);
+    }
   }
-  Plan p{s_q, s_len, s_held, s_take, s_give, s_from, head, 0, (int)total.give};
-  if (go) p.give_base = ring_place(a, head, count);
+  const int give_base = go ? ring_place(a, head, count) : 0, given = (int)total.give;
   if (tid == 0) {
     a.q_off[a.n] = go ? a.n_tokens : 0;
     if (!go) set_error(a.err, sound ? MISAT_ERR_OOM : MISAT_ERR_INVALID_ARG);
@@ -226,13 +261,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
     a.state_out[a.n + 1] = go ? count - (int)total.take + (int)total.give : count;
     if constexpr (FILL) {
       s_q[a.n] = a.n_tokens;
-      s_give[a.n] = (int)total.give;
+      s_give[a.n] = given;
     } else {
-      a.give_off[a.n] = (int)total.give;
+      a.marks[a.n] = make_int4(a.n_tokens, 0, 0, 0);
+      a.give_off[a.n] = given;
       a.head[kOk] = go;
-      a.head[kRingHead] = p.ring_head;
-      a.head[kGiveBase] = p.give_base;
-      a.head[kGiven] = p.given;
+      a.head[kRingHead] = head;
+      a.head[kGiveBase] = give_base;
+      a.head[kGiven] = given;
     }
   }
   if constexpr (FILL) {
@@ -243,7 +279,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
       if (go) {
         const int b = search(s_q, a.n, t);
         pos = s_len[b] - s_q[b + 1] + t;
-        const Place at = place_of(a, b, pos / kBlockTokens, s_held[b], s_take[b], p.ring_head);
+        const Place at = place_of(a, b, pos / kBlockTokens, s_held[b], s_take[b], head);
         const int blk = at.from ? __ldcg(at.from) : -1;
         if (at.row && pos % kBlockTokens == 0) *at.row = blk;
         slot = (int64_t)blk * kBlockTokens + pos % kBlockTokens;
@@ -252,12 +288,52 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
       a.slots[t] = slot;
     }
     if (go)
-      for (int j = tid; j < p.given; j += kPlanThreads) {
+      for (int j = tid; j < given; j += kPlanThreads) {
         const int b = search(s_give, a.n, j);
-        give(a, p, b, j, s_from[b], s_give[b]);
+        give(a, give_base, b, j, s_from[b], s_give[b]);
       }
   }
 }
+
+// The marks of 32 sequences, one a lane, and the one that a token belongs to (as OffsetFinder finds it).
+struct MarkFinder {
+  const int4* marks;
+  int n, lane, base;
+  int4 mine;  // marks[base + lane]
+  __device__ __forceinline__ void load(int b) {
+    base = b;
+    mine = base + lane <= n ? __ldcg(marks + base + lane) : make_int4(0x7fffffff, 0, 0, 0);
+  }
+  __device__ __forceinline__ MarkFinder(const TableArgs& a, int t) : marks(a.marks), n(a.n), lane(threadIdx.x & 31) {
+    load(find_sequence(a.q_off, a.n, t, lane, 32));
+  }
+  // to: the first token of the next sequence.
+  __device__ __forceinline__ int operator()(int t, Mark& m, int& to) {
+    int b = -1;
+    m = Mark{0, 0, 0, 0};
+    to = 0;
+#pragma unroll 1
+    while (true) {
+      int lo = 0;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const int v = __shfl_sync(0xffffffffu, mine.x, lo + o);
+        if (v <= t) lo += o;
+      }
+      const bool beyond = lo == 31 && base + 31 < n;
+      const Mark own{__shfl_sync(0xffffffffu, mine.x, lo), __shfl_sync(0xffffffffu, mine.y, lo),
+                     __shfl_sync(0xffffffffu, mine.z, lo), __shfl_sync(0xffffffffu, mine.w, lo)};
+      const int next = __shfl_sync(0xffffffffu, mine.x, min(lo + 1, 31));
+      if (b < 0 && !beyond) {
+        b = base + lo;
+        m = own;
+        to = lo < 31 ? next : __ldcg(&marks[b + 1].x);
+      }
+      if (!__any_sync(0xffffffffu, b < 0)) return min(b, n - 1);
+      load(base + 31);
+    }
+  }
+};
 
 __global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__ TableArgs a) {
   const int lane = threadIdx.x & 31;
@@ -272,29 +348,21 @@ __global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__
     }
     return;
   }
-  const Plan p{a.q_off,     a.kv_len_out, a.held, a.take_off, a.give_off, a.give_from, __ldcg(a.head + kRingHead),
-               __ldcg(a.head + kGiveBase), __ldcg(a.head + kGiven)};
+  const int head = __ldcg(a.head + kRingHead), base = __ldcg(a.head + kGiveBase), given = __ldcg(a.head + kGiven);
   for (int64_t t0 = (int64_t)warp * kRun; t0 < n; t0 += (int64_t)warps * kRun) {
-    // A lane's first token of each part of the run, then the sequence's numbers, then the blocks: each step's loads are
-    // on their way together.
-    OffsetFinder find(p.q_off, a.n, (int)t0);
-    int b[kAhead], to[kAhead], pos[kAhead], held[kAhead], take[kAhead], blk[kAhead];
-    Place at[kAhead];
+    // A lane's first token of each part of the run, then the blocks: each step's loads are on their way together.
+    MarkFinder find(a, (int)t0);
+    Mark mark[kAhead];
+    int seq[kAhead], end[kAhead], blk[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      seq[i] = find((int)min(t0 + (i * 32 + lane) * kEach, n - 1), mark[i], end[i]);
+    auto at = [&](int b, const Mark& m, int pos) { return place_of(a, b, pos / kBlockTokens, m.held, m.take, head); };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      int from;
-      b[i] = find((int)min(t0 + (i * 32 + lane) * kEach, n - 1), from, to[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      pos[i] = __ldcg(p.len + b[i]) - to[i] + (int)min(t0 + (i * 32 + lane) * kEach, n - 1);
-      held[i] = __ldcg(p.held + b[i]);
-      take[i] = __ldcg(p.take_off + b[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      at[i] = place_of(a, b[i], pos[i] / kBlockTokens, held[i], take[i], p.ring_head);
-      blk[i] = at[i].from ? __ldcg(at[i].from) : -1;
+      const int t = (int)min(t0 + (i * 32 + lane) * kEach, n - 1);
+      const Place p = at(seq[i], mark[i], mark[i].len - end[i] + t);
+      blk[i] = p.from ? __ldcg(p.from) : -1;
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -302,32 +370,34 @@ __global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__
       if (first >= n) continue;
       int32_t x[kEach];
       int64_t y[kEach];
-      int s = b[i], q = pos[i], end = to[i], h = held[i], k = take[i], block = blk[i];
-      Place place = at[i];
+      Mark m = mark[i];
+      int s = seq[i], to = end[i], block = blk[i], q = m.len - to + (int)first;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
+        const int t = (int)first + e;
+        if (e > 0 && t < n) {
+          ++q;
+          const bool next = t >= to;
+          if (next) {  // the next sequence with tokens
+            do {
+              m = as_mark(__ldcg(a.marks + ++s));
+              to = __ldcg(&a.marks[min(s + 1, a.n)].x);
+            } while (t >= to && s < a.n - 1);
+            q = m.len - to + t;
+          }
+          if (next || q % kBlockTokens == 0) {
+            const Place p = at(s, m, q);
+            block = p.from ? __ldcg(p.from) : -1;
+          }
+        }
+        if (q % kBlockTokens == 0 && t < n) {
+          const Place p = at(s, m, q);
+          if (p.row) *p.row = block;
+        }
         x[e] = q;
         y[e] = (int64_t)block * kBlockTokens + q % kBlockTokens;
-        if (place.row && q % kBlockTokens == 0) *place.row = block;
-        ++q;
-        if (e + 1 == kEach || first + e + 1 >= n) continue;
-        const bool next = first + e + 1 >= end;
-        if (next) {  // the next sequence with tokens
-          do {
-            ++s;
-            end = __ldcg(p.q_off + min(s, a.n - 1) + 1);
-          } while (first + e + 1 >= end && s + 1 < a.n);
-          s = min(s, a.n - 1);
-          q = __ldcg(p.len + s) - end + (int)first + e + 1;
-          h = __ldcg(p.held + s);
-          k = __ldcg(p.take_off + s);
-        }
-        if (next || q % kBlockTokens == 0) {
-          place = place_of(a, s, q / kBlockTokens, h, k, p.ring_head);
-          block = place.from ? __ldcg(place.from) : -1;
-        }
       }
-      if (a.whole && first + kEach <= n) {
+      if (a.vec_tokens && first + kEach <= n) {
         *reinterpret_cast<int4*>(a.positions + first) = make_int4(x[0], x[1], x[2], x[3]);
         *reinterpret_cast<longlong2*>(a.slots + first) = make_longlong2(y[0], y[1]);
         *reinterpret_cast<longlong2*>(a.slots + first + 2) = make_longlong2(y[2], y[3]);
@@ -341,14 +411,14 @@ __global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__
       }
     }
   }
-  for (int64_t j0 = (int64_t)warp * kGiveRun; j0 < p.given; j0 += (int64_t)warps * kGiveRun) {
-    OffsetFinder find(p.give_off, a.n, (int)j0);
+  for (int64_t j0 = (int64_t)warp * kGiveRun; j0 < given; j0 += (int64_t)warps * kGiveRun) {
+    OffsetFinder find(a.give_off, a.n, (int)j0);
 #pragma unroll 1
-    for (int i = 0; i < kGiveRun && j0 + i < p.given; i += 32) {
-      const int j = (int)min(j0 + i + lane, (int64_t)p.given - 1);
+    for (int i = 0; i < kGiveRun && j0 + i < given; i += 32) {
+      const int j = (int)min(j0 + i + lane, (int64_t)given - 1);
       int off, end;
       const int b = find(j, off, end);
-      if (j0 + i + lane < p.given) give(a, p, b, j, __ldcg(p.give_from + b), off);
+      if (j0 + i + lane < given) give(a, base, b, j, __ldcg(a.give_from + b), off);
     }
   }
 }
@@ -363,7 +433,7 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
     return MISAT_ERR_INVALID_ARG;
   if (!s->q_off || !s->state || !s->state_out || !s->ring ||
       (s->n > 0 && (!s->new_tokens || !s->kv_len || !s->kv_len_out || (!s->block_table && s->columns > 0))) ||
-      (s->n_tokens > 0 && (!s->positions || !s->slots)) || !work || (reinterpret_cast<uintptr_t>(work) & 3) ||
+      (s->n_tokens > 0 && (!s->positions || !s->slots)) || !work || (reinterpret_cast<uintptr_t>(work) & 15) ||
       work_bytes < MISAT_KV_TABLES_WORK(s->n) || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
   TableArgs a{};
@@ -385,14 +455,18 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
   a.positions = s->positions;
   a.slots = s->slots;
   a.err = kv->err;
-  int32_t* w = static_cast<int32_t*>(work);
-  a.head = w;
-  a.held = w + 4;
-  a.take_off = a.held + s->n;
-  a.give_from = a.take_off + s->n;
-  a.give_off = a.give_from + s->n;
+  a.head = static_cast<int32_t*>(work);
+  a.marks = static_cast<int4*>(work) + 1;
+  a.give_from = reinterpret_cast<int32_t*>(a.marks + s->n + 1);
+  a.give_off = a.give_from + (s->n + 3) / 4 * 4;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  a.whole = ((reinterpret_cast<uintptr_t>(s->positions) | reinterpret_cast<uintptr_t>(s->slots)) & 15) == 0;
+  const auto whole = [](std::initializer_list<const void*> list) {
+    uintptr_t all = 0;
+    for (const void* p : list) all |= reinterpret_cast<uintptr_t>(p);
+    return (all & 15) == 0;
+  };
+  a.vec_rows = whole({a.fresh, a.kv_len, a.shared, a.state, a.state_out, a.q_off, a.kv_len_out});
+  a.vec_tokens = whole({a.positions, a.slots});
   // A small step is one CTA's.
   if (s->n <= kPlanThreads && s->n_tokens <= kFillTokens) {
     launch_chained(k_table_plan<1, true>, 1, kPlanThreads, 0, st, a);

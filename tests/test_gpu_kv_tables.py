@@ -248,5 +248,5 @@ def test_refused_arguments():
     s = ctypes.byref(m.misat_kv_step(**fields))
     assert f(None, s, p, 1000, None) == m.ERR_INVALID_ARG
     assert f(t.pool._h, None, p, 1000, None) == m.ERR_INVALID_ARG
-    for args in ((None, 1000), (p, 63), (p + 2, 900)):
+    for args in ((None, 1000), (p, 111), (p + 4, 900)):
         assert f(t.pool._h, s, *args, None) == m.ERR_INVALID_ARG
