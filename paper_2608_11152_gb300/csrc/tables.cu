@@ -22,10 +22,8 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kThreads = 256;
-constexpr int kEach = 4;                   // tokens of a lane side by side
-constexpr int kAhead = 2;                  // times that many tokens of a warp on their way together
-constexpr int kRun = 32 * kEach * kAhead;  // tokens of a warp at a time
-constexpr int kGiveRun = 128;              // blocks given back
+constexpr int kFillCtas = 4;               // on an SM
+constexpr int kRun = 480;                  // tokens of a warp at a time: at most 31 blocks, one a lane
 constexpr int kFillTokens = 4096;          // most tokens of a step that one CTA makes
 
 struct TableArgs {
@@ -48,13 +46,12 @@ struct TableArgs {
   int32_t* head;
   int4* marks;
   int32_t *give_off, *give_from;
-  bool vec_rows, vec_tokens;  // what is read and written of each sequence, and of each token, at 16-byte boundaries
+  bool vec_rows;  // what is read and written of each sequence, at 16-byte boundaries
 };
 // Of a sequence: first new token, length after the step, blocks held before it, blocks taken before it.
 struct Mark {
   int off, len, held, take;
 };
-__device__ __forceinline__ Mark as_mark(int4 v) { return {v.x, v.y, v.z, v.w}; }
 enum Head { kOk, kRingHead, kGiveBase, kGiven, kHeadWords };
 
 // Sums that stay at the largest number where they would pass it: malformed counts cannot wrap around.
@@ -335,7 +332,7 @@ struct MarkFinder {
   }
 };
 
-__global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__ TableArgs a) {
+__global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid_constant__ TableArgs a) {
   const int lane = threadIdx.x & 31;
   const int warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
   chain_wait();
@@ -349,76 +346,66 @@ __global__ void __launch_bounds__(kThreads) k_table_fill(const __grid_constant__
     return;
   }
   const int head = __ldcg(a.head + kRingHead), base = __ldcg(a.head + kGiveBase), given = __ldcg(a.head + kGiven);
-  for (int64_t t0 = (int64_t)warp * kRun; t0 < n; t0 += (int64_t)warps * kRun) {
-    // A lane's first token of each part of the run, then the blocks: each step's loads are on their way together.
-    MarkFinder find(a, (int)t0);
-    Mark mark[kAhead];
-    int seq[kAhead], end[kAhead], blk[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      seq[i] = find((int)min(t0 + (i * 32 + lane) * kEach, n - 1), mark[i], end[i]);
-    auto at = [&](int b, const Mark& m, int pos) { return place_of(a, b, pos / kBlockTokens, m.held, m.take, head); };
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int t = (int)min(t0 + (i * 32 + lane) * kEach, n - 1);
-      const Place p = at(seq[i], mark[i], mark[i].len - end[i] + t);
-      blk[i] = p.from ? __ldcg(p.from) : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t first = t0 + (i * 32 + lane) * kEach;
-      if (first >= n) continue;
-      int32_t x[kEach];
-      int64_t y[kEach];
-      Mark m = mark[i];
-      int s = seq[i], to = end[i], block = blk[i], q = m.len - to + (int)first;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int t = (int)first + e;
-        if (e > 0 && t < n) {
-          ++q;
-          const bool next = t >= to;
-          if (next) {  // the next sequence with tokens
-            do {
-              m = as_mark(__ldcg(a.marks + ++s));
-              to = __ldcg(&a.marks[min(s + 1, a.n)].x);
-            } while (t >= to && s < a.n - 1);
-            q = m.len - to + t;
-          }
-          if (next || q % kBlockTokens == 0) {
-            const Place p = at(s, m, q);
-            block = p.from ? __ldcg(p.from) : -1;
+  // A warp's tokens are next to each other: only its first one is searched for.
+  const int share = (int)((n + warps - 1) / warps);
+  const int stop = (int)min((int64_t)(warp + 1) * share, n);
+  int t = (int)min((int64_t)warp * share, n);
+  if (t < stop) {
+    MarkFinder find(a, t);
+    Mark m;
+    int to, b = find(t, m, to);
+    while (true) {
+      const int left = min(to, stop) - t;
+      if (left >= 32 || to >= stop) {
+        // Up to kRun tokens of one sequence: a lane looks up one of their blocks, and puts it into the row if it is new.
+        const int some = min(left, kRun), first = m.len - to + t, col = first / kBlockTokens;
+        const int last = (first + some - 1) / kBlockTokens;
+        int blk = -1;
+        if (col + lane <= last) {
+          const Place p = place_of(a, b, col + lane, m.held, m.take, head);
+          if (p.from) blk = __ldcg(p.from);
+          if (p.row && (col + lane) * kBlockTokens >= first) *p.row = blk;
+        }
+#pragma unroll 5
+        for (int i = 0; i < some; i += 32) {
+          const int pos = first + i + lane;
+          const int64_t base = (int64_t)__shfl_sync(0xffffffffu, blk, (pos / kBlockTokens - col) & 31) * kBlockTokens;
+          if (i + lane < some) {
+            a.positions[t + i + lane] = pos;
+            a.slots[t + i + lane] = base + pos % kBlockTokens;
           }
         }
-        if (q % kBlockTokens == 0 && t < n) {
-          const Place p = at(s, m, q);
-          if (p.row) *p.row = block;
-        }
-        x[e] = q;
-        y[e] = (int64_t)block * kBlockTokens + q % kBlockTokens;
-      }
-      if (a.vec_tokens && first + kEach <= n) {
-        *reinterpret_cast<int4*>(a.positions + first) = make_int4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<longlong2*>(a.slots + first) = make_longlong2(y[0], y[1]);
-        *reinterpret_cast<longlong2*>(a.slots + first + 2) = make_longlong2(y[2], y[3]);
+        t += some;
       } else {
-#pragma unroll
-        for (int e = 0; e < kEach; ++e)
-          if (first + e < n) {
-            a.positions[first + e] = x[e];
-            a.slots[first + e] = y[e];
-          }
+        // Short sequences: a token a lane.
+        const int mine = t + lane;
+        Mark own;
+        int end;
+        const int s = find(min(mine, stop - 1), own, end);
+        if (mine < stop) {
+          const int pos = own.len - end + mine;
+          const Place p = place_of(a, s, pos / kBlockTokens, own.held, own.take, head);
+          const int blk = p.from ? __ldcg(p.from) : -1;
+          if (p.row && pos % kBlockTokens == 0) *p.row = blk;
+          a.positions[mine] = pos;
+          a.slots[mine] = (int64_t)blk * kBlockTokens + pos % kBlockTokens;
+        }
+        t += 32;
       }
+      if (t >= stop) break;
+      if (t >= to) b = find(t, m, to);
     }
   }
-  for (int64_t j0 = (int64_t)warp * kGiveRun; j0 < given; j0 += (int64_t)warps * kGiveRun) {
+  const int64_t gives = ((int64_t)given + warps - 1) / warps, last = min((warp + 1) * gives, (int64_t)given);
+  int64_t j0 = warp * gives;
+  if (j0 < last) {
     OffsetFinder find(a.give_off, a.n, (int)j0);
-#pragma unroll 1
-    for (int i = 0; i < kGiveRun && j0 + i < given; i += 32) {
-      const int j = (int)min(j0 + i + lane, (int64_t)given - 1);
+#pragma unroll 2
+    for (; j0 < last; j0 += 32) {
+      const int j = (int)min(j0 + lane, last - 1);
       int off, end;
       const int b = find(j, off, end);
-      if (j0 + i + lane < given) give(a, base, b, j, __ldcg(a.give_from + b), off);
+      if (j0 + lane < last) give(a, base, b, j, __ldcg(a.give_from + b), off);
     }
   }
 }
@@ -466,7 +453,6 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
     return (all & 15) == 0;
   };
   a.vec_rows = whole({a.fresh, a.kv_len, a.shared, a.state, a.state_out, a.q_off, a.kv_len_out});
-  a.vec_tokens = whole({a.positions, a.slots});
   // A small step is one CTA's.
   if (s->n <= kPlanThreads && s->n_tokens <= kFillTokens) {
     launch_chained(k_table_plan<1, true>, 1, kPlanThreads, 0, st, a);
@@ -474,10 +460,10 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
   }
   if (s->n <= kPlanThreads) launch_chained(k_table_plan<1, false>, 1, kPlanThreads, 0, st, a);
   else launch_chained(k_table_plan<4, false>, 1, kPlanThreads, 0, st, a);
-  // Warps for the tokens, and for blocks given back.
-  const int64_t warps = std::max<int64_t>((s->n_tokens - 1) / kRun + 1, s->n / 2);
-  const int64_t most = (int64_t)kv->num_sms * 8;
-  launch_chained(k_table_fill, (int)std::min((warps - 1) / (kThreads / 32) + 1, most), kThreads, 0, st, a);
+  // Warps for the tokens, and for blocks given back: at most as many as the GPU holds at a time.
+  const int64_t warps = std::max<int64_t>((s->n_tokens - 1) / 128 + 1, s->n / 4);
+  launch_chained(k_table_fill, (int)std::min<int64_t>((warps - 1) / (kThreads / 32) + 1, kv->num_sms * kFillCtas), kThreads,
+                 0, st, a);
   return launch_status();
 }
 
