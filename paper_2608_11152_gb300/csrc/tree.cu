@@ -85,35 +85,37 @@ struct KeepArgs {
   int32_t* len_out;
   uint4* kb;
   uint4* vb;
-  int32_t hkv, vecs, n_blocks, split;  // vecs: of 16 bytes a row; split: CTAs of a sequence
+  int32_t hkv, vecs, n_blocks, split, width;  // vecs: of 16 bytes a row; split: CTAs of a sequence; width: longest path
   int32_t* err;
 };
 
 __global__ void __launch_bounds__(kThreads) k_keep(const __grid_constant__ KeepArgs a) {
-  constexpr int kAhead = 8;
-  __shared__ int64_t from[MISAT_KV_TREE_NODES], to[MISAT_KV_TREE_NODES];  // rows of kv head 0, -1: stays
+  constexpr int kAhead = 16;
+  extern __shared__ __align__(16) longlong2 moves[];  // rows of kv head 0: from and to, from = -1: stays
   const int b = blockIdx.x, tid = threadIdx.x;
   chain_wait();
-  const Range s = load_range(a.b, b, a.err);
-  const int m = __ldcg(a.n_keep + b);
   const int32_t* path = a.path + (int64_t)b * a.path_stride;
-  bool ok = m >= 0 && m <= s.n && m <= a.path_stride && m <= MISAT_KV_TREE_NODES && s.len >= s.n;
+  // The path is read beside the lengths that say how much of it counts.
+  int p = tid < a.width ? __ldcg(path + tid) : 0, last = tid > 0 && tid < a.width ? __ldcg(path + tid - 1) : -1;
+  const int m = __ldcg(a.n_keep + b);
+  const Range s = load_range(a.b, b, a.err);
+  bool ok = m >= 0 && m <= s.n && m <= a.width && s.len >= s.n;
   const int before = s.len - s.n;
   auto row_of = [&](int pos) {
     const int blk = __ldcg(a.b.table + (int64_t)b * a.b.stride + pos / kBlockTokens);
-    if (blk < 0 || blk >= a.n_blocks) return (int64_t)-1;
-    return ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.vecs;
+    return blk >= 0 && blk < a.n_blocks ? ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.vecs : -1;
   };
   if (ok) {
     for (int i = tid; i < m; i += kThreads) {
-      const int p = __ldcg(path + i), last = i > 0 ? __ldcg(path + i - 1) : -1;
-      const bool fits = p > last && p < s.n && p >= i;
-      from[i] = to[i] = -1;
-      if (fits && p != i) {
-        from[i] = row_of(before + p);
-        to[i] = row_of(before + i);
+      if (i != tid) {
+        p = __ldcg(path + i);
+        last = __ldcg(path + i - 1);
       }
-      ok = ok && fits && (p == i || (from[i] >= 0 && to[i] >= 0));
+      const bool fits = p > last && p < s.n && p >= i;
+      longlong2 move = make_longlong2(-1, -1);
+      if (fits && p != i) move = make_longlong2(row_of(before + p), row_of(before + i));
+      moves[i] = move;
+      ok = ok && fits && (p == i || (move.x >= 0 && move.y >= 0));
     }
   }
   ok = __syncthreads_and(ok);
@@ -125,18 +127,18 @@ __global__ void __launch_bounds__(kThreads) k_keep(const __grid_constant__ KeepA
   // A column: 16 bytes of the rows of a kv head, of the keys or the values.
   const int heads = a.hkv * a.vecs, cols = 2 * heads;
   for (int c = blockIdx.y * kThreads + tid; c < cols; c += a.split * kThreads) {
-    uint4* p = c < heads ? a.kb : a.vb;
+    uint4* rows = c < heads ? a.kb : a.vb;
     const int k = c < heads ? c : c - heads, head = k / a.vecs;
-    p += (int64_t)head * kBlockTokens * a.vecs + (k - head * a.vecs);
+    rows += (int64_t)head * kBlockTokens * a.vecs + (k - head * a.vecs);
 #pragma unroll 1
     for (int i = 0; i < m; i += kAhead) {
       uint4 v[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        if (i + j < m && from[i + j] >= 0) v[j] = p[from[i + j]];
+        if (i + j < m && moves[i + j].x >= 0) v[j] = rows[moves[i + j].x];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        if (i + j < m && from[i + j] >= 0) p[to[i + j]] = v[j];
+        if (i + j < m && moves[i + j].x >= 0) rows[moves[i + j].y] = v[j];
     }
   }
 }
@@ -175,6 +177,7 @@ int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path
   a.hkv = kv->hkv;
   a.vecs = kv->d / 8;
   a.n_blocks = kv->n_blocks;
+  a.width = (int)std::min<int64_t>(path_stride, MISAT_KV_TREE_NODES);
   a.err = kv->err;
   const int cols = (2 * kv->hkv * a.vecs + kThreads - 1) / kThreads;
   a.split = std::max(1, std::min(cols, kv->num_sms * 8 / batch->n));
@@ -184,6 +187,7 @@ int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3(batch->n, a.split);
   lc.blockDim = dim3(kThreads);
+  lc.dynamicSmemBytes = sizeof(longlong2) * a.width;
   lc.stream = static_cast<cudaStream_t>(cuda_stream);
   lc.attrs = &at;
   lc.numAttrs = 1;
