@@ -227,7 +227,7 @@ struct Part {
   }
   template <class W>
   __device__ __forceinline__ void load_weight(const W* w, bool whole, float offset, float (&out)[UPL][kElems]) const {
-    constexpr int N = VEC > 1 ? 16 / (int)sizeof(W) : 1;  // of a vector
+    constexpr int N = VEC * (int)sizeof(W) > 16 ? 16 / (int)sizeof(W) : VEC;  // of a vector
 #pragma unroll
     for (int j = 0; j < UPL; ++j)
 #pragma unroll
@@ -292,20 +292,27 @@ struct Stages {
   static constexpr int kThreads = P::shape(TENSORS == 2).threads;
   static constexpr int kDepth = P::shape(TENSORS == 2).depth;
   static constexpr int kSize = WHOLE ? kDepth * TENSORS * P::kBytes * kThreads : 0;  // shared memory
+  static constexpr int kVec = sizeof(typename P::V);  // bytes
   const P& part;
-  uint32_t base;  // this thread's first vector
+  const char* smem;  // this thread's first vector
+  uint32_t base;
   typename P::Raw next[WHOLE ? 1 : TENSORS];
 
   __device__ __forceinline__ Stages(const P& part, void* smem)
-      : part(part), base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16) {}
+      : part(part), smem(static_cast<const char*>(smem) + threadIdx.x * kVec),
+        base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * kVec) {}
   __device__ __forceinline__ uint32_t at(int stage, int tensor, int vec) const {
-    return base + ((stage * TENSORS + tensor) * (P::kBytes / 16) + vec) * kThreads * 16;
+    return base + ((stage * TENSORS + tensor) * (P::kBytes / kVec) + vec) * kThreads * kVec;
   }
   __device__ __forceinline__ void issue(int stage, int tensor, const T* p, bool ok) {
     if constexpr (WHOLE) {
       part.each([&](int v, int e, bool there) {
-        if (ok && there)
+        if (!ok || !there) return;
+        if constexpr (kVec == 16)
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at(stage, tensor, v)), "l"(p + e) : "memory");
+        else
+          asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at(stage, tensor, v)), "l"(p + e), "n"(kVec)
+                       : "memory");
       });
       if (tensor + 1 == TENSORS) asm volatile("cp.async.commit_group;" ::: "memory");
     } else {
@@ -318,12 +325,7 @@ struct Stages {
   __device__ __forceinline__ void take(int stage, int tensor, typename P::Raw& r) const {
     if constexpr (WHOLE) {
       part.each([&](int v, int e, bool) {
-        uint4 x;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
-                     : "r"(at(stage, tensor, v))
-                     : "memory");
-        r.vec(v) = *reinterpret_cast<typename P::V*>(&x);
+        r.vec(v) = *reinterpret_cast<const typename P::V*>(smem + (at(stage, tensor, v) - at(0, 0, 0)));
       });
     } else {
       r = next[tensor];
@@ -586,16 +588,16 @@ __global__ void __launch_bounds__(kSumCols * kSumRows) k_norm_weight(const __gri
 struct Grid {
   int x, y, threads;
   size_t smem;
-  bool vec;
+  int vec;  // elements of a vector, 1: one by one
   int upl;
 };
 
 // How heads and tokens are laid over lanes and CTAs.
-Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int num_sms) {
-  const int n = 16 / elem;
+Grid plan(NormArgs& a, int elem, bool half_layout, int vec, bool backward, int num_sms) {
+  const int n = vec > 1 ? vec : 1;
   Grid g{};
   g.vec = vec;
-  if (vec) a.units = half_layout ? a.rot / 2 / n + (a.d - a.rot) / n : a.d / n;
+  if (vec > 1) a.units = half_layout ? a.rot / 2 / n + (a.d - a.rot) / n : a.d / n;
   else a.units = half_layout ? a.d - a.rot / 2 : (a.d + 1) / 2;
   const auto lanes_for = [&](int upl) {
     int bits = 0;
@@ -604,17 +606,17 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   };
   // Units of a lane: one of the half layout's, as they are 16 elements (in 32 bits 8: two where a warp is too small);
   // else two or three, whichever leaves fewer places of the lanes empty.
-  if (!vec) g.upl = 8;
+  if (vec <= 2) g.upl = vec == 2 && half_layout ? 4 : 8;
   else if (half_layout) g.upl = a.units > 32 ? 2 : 1;
   else g.upl = 3 << lanes_for(3) < 2 << lanes_for(2) ? 3 : 2;
   a.lane_bits = lanes_for(g.upl);
-  const int pairs = vec ? (half_layout ? n : n / 2) : 1;
+  const int pairs = vec > 1 ? (half_layout ? n : n / 2) : 1;
   a.turns = (a.rot / 2 + pairs - 1) / pairs * pairs;
   // What the copies in flight leave of the shared memory holds the turns of a tile's tokens.
-  const int elements = vec ? g.upl * n * (half_layout ? 2 : 1) : 0, bytes = elements * elem * (backward ? 2 : 1);
-  const Shape shape = vec ? shape_of(elements, bytes, backward) : Shape{256, backward ? 1 : 2, 1};
+  const int elements = vec > 1 ? g.upl * n * (half_layout ? 2 : 1) : 0, bytes = elements * elem * (backward ? 2 : 1);
+  const Shape shape = vec > 1 ? shape_of(elements, bytes, backward) : Shape{256, backward ? 1 : 2, 1};
   const int threads = shape.threads, turn = 8 * a.turns;
-  const int ring = vec ? shape.depth * bytes * threads : 0;
+  const int ring = shape.depth * bytes * threads;
   const int room = turn ? std::min(kMaxTile, (kShared - ring) / turn) : kMaxTile;
   // All heads of a token in one CTA where they fit, else equal parts of them; the rest of the CTA takes other tokens.
   const int slots = threads >> a.lane_bits, chunks = (a.heads + slots - 1) / slots;
@@ -622,7 +624,7 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   a.side = std::min(slots / a.chunk, room);
   a.by_chunk.set(a.chunk);
   g.y = (a.heads + a.chunk - 1) / a.chunk;
-  g.threads = vec ? threads : ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
+  g.threads = vec > 1 ? threads : ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
   // As many CTAs as the GPU holds at a time, with equally many tokens each.
   const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * shape.ctas / g.y);
   a.per = (rounds - 1) / std::min(rounds, most) + 1;
@@ -634,12 +636,15 @@ Grid plan(NormArgs& a, int elem, bool half_layout, bool vec, bool backward, int 
   return g;
 }
 
-// Whole 16-byte vectors wherever every row starts on such a boundary and no vector straddles the end of a head or
-// (half layout) of the rotated halves.
-bool whole_vectors(const NormArgs& a, int elem, bool half_layout) {
-  const int n = 16 / elem;
-  return aligned16(a.x, elem) && aligned16(a.out, elem) && aligned16(a.k, elem) && aligned16(a.v, elem) &&
-         aligned16(a.dy, elem) && a.d % n == 0 && (!half_layout || a.rot / 2 % n == 0);
+// Elements of the vectors that every row is made of: 16 bytes, or two elements, where every row starts on such a
+// boundary and no vector straddles the end of a head or (half layout) of the rotated halves; else one by one.
+int vector_of(const NormArgs& a, int elem, bool half_layout) {
+  uintptr_t at = 0;
+  for (const Heads* h : {&a.x, &a.out, &a.k, &a.v, &a.dy})
+    if (h->p) at |= reinterpret_cast<uintptr_t>(h->p) | (uintptr_t)(h->ts * elem) | (uintptr_t)(h->hs * elem);
+  for (const int n : {16 / elem, 2})
+    if (at % (n * elem) == 0 && a.d % n == 0 && (!half_layout || a.rot / 2 % n == 0)) return n;
+  return 1;
 }
 
 template <class... P, class... A>
@@ -665,8 +670,10 @@ void launch_part(const NormArgs& a, const Grid& g, bool backward, cudaStream_t s
 template <class T>
 void launch_t(const NormArgs& a, const Grid& g, bool half_layout, bool backward, cudaStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
-  if (!g.vec) return half_layout ? launch_part<T, 1, true, 8>(a, g, backward, st)
-                                 : launch_part<T, 1, false, 8>(a, g, backward, st);
+  if (g.vec == 1) return half_layout ? launch_part<T, 1, true, 8>(a, g, backward, st)
+                                     : launch_part<T, 1, false, 8>(a, g, backward, st);
+  if (g.vec == 2) return half_layout ? launch_part<T, 2, true, 4>(a, g, backward, st)
+                                     : launch_part<T, 2, false, 8>(a, g, backward, st);
   if (!half_layout) return g.upl == 3 ? launch_part<T, VEC, false, 3>(a, g, backward, st)
                                       : launch_part<T, VEC, false, 2>(a, g, backward, st);
   if constexpr (sizeof(T) == 4)
@@ -733,7 +740,7 @@ int misat_norm_rotary(const misat_rope* r, const misat_head_norm* norm, int32_t 
   a.out = {out, o_ts, o_hs};
   a.positions = positions;
   const bool half = r->layout == MISAT_ROPE_HALF;
-  const Grid g = plan(a, elem, half, whole_vectors(a, elem, half), false, r->num_sms);
+  const Grid g = plan(a, elem, half, vector_of(a, elem, half), false, r->num_sms);
   launch_norm(a, g, dtype, half, false, static_cast<cudaStream_t>(cuda_stream));
   return launch_status();
 }
@@ -743,12 +750,12 @@ int misat_norm_rotary_work(const misat_rope* r, const misat_head_norm* norm, int
   if (!sizes_ok(r, norm, dtype, n_tokens, n_heads, head_dim) || !bytes) return MISAT_ERR_INVALID_ARG;
   *bytes = 0;
   if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
-  // The larger of the two layouts: which one it will be depends on the tensors' addresses.
-  for (const bool vec : {false, true}) {
+  // The largest of what they may be: it depends on the tensors' addresses.
+  const int elem = dtype == MISAT_F32 ? 4 : 2;
+  for (const int vec : {1, 2, 16 / elem}) {
     NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
     const bool half = r->layout == MISAT_ROPE_HALF;
-    const int elem = dtype == MISAT_F32 ? 4 : 2;
-    if (vec && !whole_vectors(a, elem, half)) continue;
+    if (vec > vector_of(a, elem, half)) continue;
     const Grid g = plan(a, elem, half, vec, true, r->num_sms);
     *bytes = std::max(*bytes, parts_of(a, g) * part_size(a) * (int64_t)sizeof(float));
   }
@@ -782,7 +789,7 @@ int misat_norm_rotary_backward(const misat_rope* r, const misat_head_norm* norm,
     a.positions = positions;
     a.parts = static_cast<float*>(work);
     const bool half = r->layout == MISAT_ROPE_HALF;
-    const Grid g = plan(a, elem, half, whole_vectors(a, elem, half), true, r->num_sms);
+    const Grid g = plan(a, elem, half, vector_of(a, elem, half), true, r->num_sms);
     s.n_parts = (int32_t)parts_of(a, g);
     if (!work || work_bytes < parts_of(a, g) * part_size(a) * (int64_t)sizeof(float)) return MISAT_ERR_INVALID_ARG;
     launch_norm(a, g, dtype, half, true, st);
@@ -833,7 +840,7 @@ int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_
   a.vb = kv->vb;
   a.n_blocks = kv->n_blocks;
   a.err = kv->err;
-  const Grid g = plan(a, 2, half, whole_vectors(a, 2, half), false, kv->num_sms);
+  const Grid g = plan(a, 2, half, vector_of(a, 2, half), false, kv->num_sms);
   launch_norm(a, g, kv->dtype, half, false, static_cast<cudaStream_t>(cuda_stream));
   return launch_status();
 }
