@@ -609,7 +609,7 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
  * all sticky, from misat_kv_sync). */
 typedef struct misat_kv_step {
   int32_t n;                 /* sequences, 0..max_batch of the pool */
-  int32_t n_tokens;          /* sum of new_tokens, below 2^31 - 1 */
+  int32_t n_tokens;          /* sum of new_tokens, below 2^31 - 4096 */
   int32_t max_q;             /* at least the new tokens of any sequence */
   int32_t columns;           /* blocks that a row of the table has room for */
   int64_t table_stride;      /* >= columns */
@@ -644,8 +644,8 @@ typedef struct misat_head_norm {
   float eps;           /* finite, > 0 */
   float offset;        /* finite */
 } misat_head_norm;
-/* Like misat_rotary with the norm before the rotation; head_dim at most 256.  Values are rounded
- * once.  Errors: INVALID_ARG, CUDA.  [async] */
+/* Like misat_rotary with the norm before the rotation; head_dim at most 256, n_tokens below
+ * 2^31 - 4096.  Values are rounded once.  Errors: INVALID_ARG, CUDA.  [async] */
 int misat_norm_rotary(const misat_rope* rope, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
                       int32_t n_heads, int32_t head_dim, const void* x, int64_t x_token_stride, int64_t x_head_stride,
                       const int32_t* positions, void* out, int64_t out_token_stride, int64_t out_head_stride,

@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kMaxTile = 32;   // tokens of a CTA at a time: their places are found by one warp
 constexpr int kMaxHead = 256;  // elements
+constexpr int kMaxTokens = INT32_MAX - 4096;  // numbers of tokens run past the last one by a few rounds
 constexpr int kShared = 47 * 1024;  // dynamic bytes of a CTA, at most 48 KiB with the places of its tokens
 
 // By the elements of a lane and the bytes of its part of a token: threads of a CTA, CTAs on an SM, copies in flight.
@@ -387,7 +388,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
   const bool q = h < a.hq, k = h < a.hq + a.hkv;
   const Heads& src = q ? a.x : k ? a.k : a.v;
   const int hh = q ? h : k ? h - a.hq : h - a.hq - a.hkv;
-  const int begin = blockIdx.x * a.per, end = min(begin + a.per, a.n_tokens);
+  const int begin = blockIdx.x * a.per, end = (int)min((int64_t)begin + a.per, (int64_t)a.n_tokens);
   const T* in = static_cast<const T*>(src.p) + (int64_t)hh * src.hs + (int64_t)(begin + side) * src.ts;
   const int64_t step = (int64_t)a.side * src.ts;
   // A token's row is at its number's place in the queries' result, or at its slot of the blocks.
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(true).threads,
   S stages(part, s_mem);
   const int h = blockIdx.y * a.chunk + group - side * a.chunk;
   const bool mine = side < a.side && h < a.heads;
-  const int begin = blockIdx.x * a.per, end = min(begin + a.per, a.n_tokens);
+  const int begin = blockIdx.x * a.per, end = (int)min((int64_t)begin + a.per, (int64_t)a.n_tokens);
   const T* x_in = static_cast<const T*>(a.x.p) + (int64_t)h * a.x.hs + (int64_t)(begin + side) * a.x.ts;
   const T* g_in = static_cast<const T*>(a.dy.p) + (int64_t)h * a.dy.hs + (int64_t)(begin + side) * a.dy.ts;
   T* out = static_cast<T*>(a.out.p) + (int64_t)h * a.out.hs + (int64_t)(begin + side) * a.out.ts;
@@ -744,7 +745,7 @@ HeadWeight weight_of(const misat_head_norm* n) {
 
 bool sizes_ok(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens, int32_t n_heads,
               int32_t head_dim) {
-  return r && dtype >= MISAT_BF16 && dtype <= MISAT_F32 && n_tokens >= 0 && n_heads >= 0 && n_heads <= 65535 &&
+  return r && dtype >= MISAT_BF16 && dtype <= MISAT_F32 && n_tokens >= 0 && n_tokens <= kMaxTokens && n_heads >= 0 && n_heads <= 65535 &&
          head_dim >= r->rot && head_dim <= kMaxHead && norm_ok(norm, dtype, n_heads, head_dim);
 }
 NormArgs rotary_args(const misat_rope* r, const misat_head_norm* norm, int32_t n_tokens, int32_t n_heads,
@@ -844,7 +845,7 @@ int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_
                          const misat_head_norm* k_norm, const misat_kv_draft* draft, const void* k, int64_t k_ts,
                          int64_t k_hs, const void* v, int64_t v_ts, int64_t v_hs, const void* q, int64_t q_ts,
                          int64_t q_hs, void* q_out, int64_t qo_ts, int64_t qo_hs, void* cuda_stream) {
-  if (!batch_ok(kv, batch) || (q_norm && !norm_ok(q_norm, kv->dtype, kv->hq, kv->d)) ||
+  if (!batch_ok(kv, batch) || batch->n_tokens > kMaxTokens || (q_norm && !norm_ok(q_norm, kv->dtype, kv->hq, kv->d)) ||
       (k_norm && !norm_ok(k_norm, kv->dtype, kv->hkv, kv->d)))
     return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;

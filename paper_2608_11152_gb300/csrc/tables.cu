@@ -20,6 +20,7 @@ using namespace misat;
 
 namespace {
 
+constexpr int kMaxTokens = INT32_MAX - 4096;  // numbers of tokens run past the last one by a few
 constexpr int kPlanThreads = 1024;
 constexpr int kThreads = 256;
 constexpr int kFillCtas = 4;               // on an SM
@@ -415,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid
 extern "C" {
 
 int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t work_bytes, void* cuda_stream) {
-  if (!kv || !s || s->n < 0 || s->n > kv->max_batch || s->n_tokens < 0 || s->n_tokens == INT32_MAX || s->max_q < 0 ||
+  if (!kv || !s || s->n < 0 || s->n > kv->max_batch || s->n_tokens < 0 || s->n_tokens > kMaxTokens || s->max_q < 0 ||
       s->columns < 0 || s->table_stride < s->columns || s->ring_size < 1 || (s->n == 0 && s->n_tokens > 0))
     return MISAT_ERR_INVALID_ARG;
   if (!s->q_off || !s->state || !s->state_out || !s->ring ||

@@ -23,10 +23,12 @@ namespace {
 PyObject* g_error = nullptr;  // MisatError
 
 struct Rope {
+  static constexpr const char* kName = "Rope";
   misat_rope* h;
   c10::DeviceIndex device;
 };
 struct Pool {
+  static constexpr const char* kName = "KvPool";
   misat_kv* h;
   c10::DeviceIndex device;
   at::Tensor k_blocks, v_blocks;
@@ -41,36 +43,40 @@ struct Made {
   std::vector<at::Tensor> tensors;
 };
 struct Batch {
+  static constexpr const char* kName = "KvBatch";
   misat_kv_batch b;
   int64_t hq, hkv, d;
   c10::DeviceIndex device;
   Made made{};
 };
 struct Tree {
+  static constexpr const char* kName = "KvTree";
   misat_kv_draft d;
   int64_t n_tokens, max_q;
   c10::DeviceIndex device;
   Made made;
 };
 struct Norm {
+  static constexpr const char* kName = "HeadNorm";
   at::Tensor w;  // [head_dim] or [heads][head_dim]
   float eps, offset;
 };
 
 template <class S>
 void free_state(PyObject* c) {
-  delete static_cast<S*>(PyCapsule_GetPointer(c, nullptr));
+  delete static_cast<S*>(PyCapsule_GetPointer(c, S::kName));
 }
 template <class S>
 PyObject* new_state(const S& s) {
   S* p = new S(s);
-  PyObject* c = PyCapsule_New(p, nullptr, free_state<S>);
+  PyObject* c = PyCapsule_New(p, S::kName, free_state<S>);
   if (!c) delete p;
   return c;
 }
+// The state behind an object of the binding; nullptr with an error set for another kind's.
 template <class S>
 S* state(PyObject* c) {
-  return static_cast<S*>(PyCapsule_GetPointer(c, nullptr));
+  return static_cast<S*>(PyCapsule_GetPointer(c, S::kName));
 }
 
 struct Raised {};  // a Python error is set
@@ -653,7 +659,7 @@ PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   s.block_table = table.data_ptr<int32_t>();
   s.n_tokens = int32_of(a[7], "n_tokens");
   s.max_q = int32_of(a[8], "max_q");
-  if (seqs > INT32_MAX || columns > INT32_MAX || places > INT32_MAX || s.n_tokens < 0 || s.n_tokens == INT32_MAX)
+  if (seqs > INT32_MAX || columns > INT32_MAX || places > INT32_MAX || s.n_tokens < 0 || s.n_tokens > INT32_MAX - 4096)
     return fail(MISAT_ERR_INVALID_ARG, "misat_kv_tables");
   s.n = (int32_t)seqs;
   s.columns = (int32_t)columns;

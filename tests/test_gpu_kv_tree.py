@@ -493,3 +493,21 @@ def test_written_tensors_have_a_new_version():
         call()
         assert all(t._version > v for t, v in zip(tensors, before))
     pool.sync()
+
+
+def test_objects_of_another_kind_are_refused():
+    m = misat()
+    s = Step([(3, 20)], 2, 32, BF16)
+    rope = m.Rope(32)
+    pool = s.pool(4, rope=rope)
+    batch = s.batch(pool)
+    tree = pool.tree(batch, ints([-1, 0, 0]))
+    norm = m.HeadNorm(torch.ones(32, device="cuda"))
+    q, k, pos = rand((3, 4, 32), BF16, 1), rand((3, 2, 32), BF16, 2), ints([0, 1, 2])
+    for call in (lambda: pool.attend(tree, q), lambda: pool.attend(batch, q, tree=batch), lambda: pool.attend(pool, q),
+                 lambda: pool.append(batch, k, k, k_norm=rope), lambda: pool.append(batch, k, k, tree=norm),
+                 lambda: rope.norm_rotate(q, pos, rope), lambda: pool.keep(tree, pos[:, None], pos),
+                 lambda: pool.tree(norm, pos)):
+        with pytest.raises((ValueError, AttributeError)):
+            call()
+    pool.sync()
