@@ -668,13 +668,16 @@ Grid plan(NormArgs& a, int elem, bool half_layout, int vec, bool backward, int n
   a.by_chunk.set(a.chunk);
   g.y = (a.heads + a.chunk - 1) / a.chunk;
   g.threads = vec > 1 ? threads : ((a.side * a.chunk << a.lane_bits) + 31) / 32 * 32;
-  // As many CTAs as the GPU holds at a time, with equally many tokens each; forward, more CTAs where that would be many
-  // tokens: they then work on neighbouring rows at any time (65,536 x 32 heads of 128 in bf16: 192 us with one wave, 173
-  // with 32 tokens a CTA, 166 with 24, 163 with 16; the append of 70,000 tokens, which looks up their places: 280, 258,
-  // 256, 262).  Element by element a CTA's first steps cost more than that (10,000 x 32 heads of 154: 100 us, 126 with 32).
+  // As many CTAs as the GPU holds at a time, with equally many rounds of tokens each; forward, several times as many where
+  // that would be many rounds: they then work on neighbouring rows at any time (65,536 x 32 heads of 128 in bf16: 192 us
+  // with one wave of CTAs, 173 with 32 rounds a CTA, 166 with 24, 163 with 16; the append of 70,000 tokens, which looks up
+  // their places: 280, 258, 256, 262).  A little more than one wave would be two (40,000 x 8 heads: 33.5 us with 17
+  // rounds, 38.3 with 16).  Element by element a CTA's first steps cost more than that gains (10,000 x 32 heads of 154:
+  // 100 us, 126 with 32 rounds).
   const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * shape.ctas / g.y);
   a.per = (rounds - 1) / std::min(rounds, most) + 1;
-  if (!backward && vec > 1) a.per = std::min(a.per, std::max((a.hkv ? 24 : 16) / a.side, 1));
+  const int most_rounds = a.hkv ? 24 : 16;
+  if (!backward && vec > 1 && a.per > 3 * most_rounds) a.per = most_rounds;
   g.x = (rounds - 1) / a.per + 1;
   a.per *= a.side;
   a.tile = std::min(a.per, room / a.side * a.side);
