@@ -75,8 +75,12 @@ struct Weights<__half> {
 __device__ __forceinline__ uint32_t col_s(int st) { return st * 128; }
 template <int DP>
 __device__ __forceinline__ uint32_t col_o(int st) { return 256 + st * DP; }
+// APART: the weights have columns of their own, which heads up to 64 leave free.  The next scores then form as soon as
+// the last ones are read, under the exponentials, and the chain of a stream is its softmax alone.
+template <bool APART>
+__device__ __forceinline__ uint32_t col_p(int st) { return APART ? 384 + st * 64 : col_s(st); }
 
-template <class T, int DP>
+template <class T, int DP, bool APART>
 struct Issuer {
   using L = Layout<DP>;
   static constexpr bool kBf16 = std::is_same_v<T, __nv_bfloat16>;
@@ -87,6 +91,7 @@ struct Issuer {
   Ring ring;
   int k_stage = 0, v_stage = 0;
   uint32_t p_phases = 0;  // bit per stream
+  uint32_t free_phases = 0, v_phase = 0;  // (APART)
 
   // Address of a barrier of the control block.
   __device__ __forceinline__ uint32_t bar(size_t offset, int i = 0) const { return ctl + (uint32_t)offset + i * 8; }
@@ -104,7 +109,7 @@ struct Issuer {
   // O of the stream (+)= weights times values, over the pages of the block that hold visible keys.
   __device__ __forceinline__ void product(const Segment& g, int st, int stage, int j, bool fresh) const {
     const uint32_t v = desc_lo(base + L::kKv + stage * L::kStage, L::kHalf);
-    const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_s(st);
+    const uint32_t d = tmem + col_o<DP>(st), p = tmem + col_p<APART>(st);
     constexpr uint32_t id = mma_desc(kBf16, 128, DP, true);
     if (j * kKeys >= g.k.from && (j + 1) * kKeys <= g.k.to) {
 #pragma unroll
@@ -172,6 +177,48 @@ struct Issuer {
     }
     return true;
   }
+  // The same where weights and scores are apart: the scores of step x + 2 come before the product of step x, as soon as
+  // the scores of step x are read.
+  __device__ __forceinline__ bool step_apart(const Segment& g, int x, int n, int slot0, int slot1) {
+    const int st = x & 1, slot = st ? slot1 : slot0;
+    const bool has_v = x >= 0, has_k = x + 2 < n;
+    const bool first_use = !g.pair || st == 0, last_use = !g.pair || st == 1;
+    if (has_v && first_use) {
+      v_stage = ring.at;
+      v_phase = ring.phase;
+      ring.step(L::kStages);
+    }
+    if (has_k) {
+      if (first_use) {
+        k_stage = ring.at;
+        if (!mbar_wait_one(MISAT_BAR(kv_full, k_stage), ring.phase, &c->abort)) return false;
+        ring.step(L::kStages);
+      }
+      if (has_v) {
+        if (!mbar_wait_one(MISAT_BAR(s_free, st), free_phases >> st & 1, &c->abort)) return false;
+        tc_fence_after();
+      }
+      scores(st, slot, k_stage);
+      mma_commit(MISAT_BAR(s_full, st));
+      if (last_use) mma_commit(MISAT_BAR(kv_empty, k_stage));
+      if (x + 3 == n) {  // the last scores: the queries have been read
+        mma_commit(MISAT_BAR(q_empty, slot0));
+        if (g.both()) mma_commit(MISAT_BAR(q_empty, 1));
+      }
+    }
+    if (has_v) {
+      free_phases ^= 1 << st;  // (of an item's last scores too: read when their weights are there)
+      if (first_use && !mbar_wait_one(MISAT_BAR(kv_full, v_stage), v_phase, &c->abort)) return false;
+      if (!mbar_wait_one(MISAT_BAR(p_full, st), p_phases >> st & 1, &c->abort)) return false;
+      p_phases ^= 1 << st;
+      tc_fence_after();
+      product(g, st, v_stage, g.block(x), x < 2);
+      if (last_use) mma_commit(MISAT_BAR(kv_empty, v_stage));
+      mma_commit(MISAT_BAR(pv_done, st));
+      if (!has_k) mma_commit(MISAT_BAR(o_full, st));
+    }
+    return true;
+  }
   __device__ __forceinline__ void run() {
     QuerySlots qs;
     Feed feed{c};
@@ -202,13 +249,14 @@ struct Issuer {
           bool ok = true;
 #pragma unroll 1
           for (int y = x; y < min(end, n) && ok; ++y)
-            ok = step(g, y, n, slot0, slot1);
-          state = ring.at | (int)ring.phase << 8 | (int)p_phases << 9 | (int)ok << 11;
+            ok = APART ? step_apart(g, y, n, slot0, slot1) : step(g, y, n, slot0, slot1);
+          state = ring.at | (int)ring.phase << 8 | (int)p_phases << 9 | (int)ok << 11 | (int)free_phases << 12;
         }
         state = __shfl_sync(0xffffffffu, state, lead);
         ring.at = state & 0xff;
         ring.phase = state >> 8 & 1;
         p_phases = state >> 9 & 3;
+        free_phases = state >> 12 & 3;
         if (!(state >> 11 & 1)) return;
         x = end;
       }
@@ -248,6 +296,8 @@ struct Softmax {
   uint32_t tmem;  // with the warp's lanes
   int st;         // stream
   int row;        // row of the tile = lane of tensor memory
+  static constexpr bool kApart = TREE && DP == 64;
+  uint32_t pv_phase = 0;  // (kApart)
   uint32_t s_phase = 0, o_phase = 0, o1_phase = 0, wg_phase = 0, ml_phase = 0;  // o1: of stream 1, kept by stream 0
   bool joined = false;  // stream 1: its last item was joined by stream 0
 
@@ -313,8 +363,8 @@ struct Softmax {
   }
 
   // One block: scores to weights, with the running reference m and sum l.
-  // words: of a tree's node, where the block needs a mask (hi is then the shift).
-  __device__ __forceinline__ void block(int lo, int hi, bool mask, uint32_t (&words)[5], bool fresh, float& m,
+  // words: of a tree's node, where the block needs a mask (hi is then the shift).  False: gave up waiting.
+  __device__ __forceinline__ bool block(int lo, int hi, bool mask, uint32_t (&words)[5], bool fresh, float& m,
                                         float& l) {
     if (mask) {
       if constexpr (TREE) hide_tree(words, hi, lo);
@@ -340,7 +390,10 @@ struct Softmax {
     // Where c m has few bits behind the point, the weights' exponents do not come out of c s - c m: m is taken off the
     // scores first, which is exact near it.  (The rounding of c m would pass float16's largest weight.)
     const bool far = fabsf(ref) >= 0x1p20f;
-    if (__any_sync(0xffffffffu, need || far)) {
+    const bool rescale = __any_sync(0xffffffffu, need || far);
+    // Where the scores came before the last product: it is done before its sums and its weights are written over.
+    if (kApart && rescale && !fresh && !last_product()) return false;
+    if (rescale) {
       if (!fresh) {
         const float f = need ? exp2_approx((from - top) * a.c) : 1.f;
         const uint64_t f2 = pack2(f, f);
@@ -378,6 +431,7 @@ struct Softmax {
 #pragma unroll
       for (int q = 0; q < 4; ++q) tmem_tie(r[q]);
     }
+    if (kApart) scores_read();
     const uint64_t c2 = pack2(a.c, a.c), ref2 = pack2(ref, ref);
     uint64_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -393,12 +447,26 @@ struct Softmax {
         sum[i & 3] = add2(sum[i & 3], pack2(x, y));
         p[i] = pack16<T>(x, y);
       }
-      // Over the first scores, which have been read.
-      tmem_st16(tmem + col_s(st) + q * 16, p);
+      if (kApart && q == 0 && !rescale && !fresh && !last_product()) return false;
+      // Where they are not apart, over the first scores, which have been read.
+      tmem_st16(tmem + col_p<kApart>(st) + q * 16, p);
     }
     float x, y;
     unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), x, y);
     l += x + y;
+    return true;
+  }
+  // kApart: the product of the stream's block before is complete.
+  __device__ __forceinline__ bool last_product() {
+    const bool ok = mbar_wait(smem_u32(&c->pv_done[st]), pv_phase, &c->abort);
+    tc_fence_after();
+    return ok;
+  }
+  // kApart: this warp has its scores in registers.
+  __device__ __forceinline__ void scores_read() {
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&c->s_free[st]));
   }
 
   __device__ __forceinline__ bool wg_sync() {
@@ -623,10 +691,14 @@ struct Softmax {
             hi = (k0 - before) & 31;
             lo = reach - k0;
           }
-          block(lo, hi, mask, words, i == 0, m, l);
+          if (!block(lo, hi, mask, words, i == 0, m, l)) return;
           tc_wait_st();
           tc_fence_before();
+        } else if (kApart) {  // (a warp without rows keeps step with the others, whose next scores may be there already)
+          scores_read();
+          if (i > 0 && !last_product()) return;
         }
+        if (kApart && i > 0) pv_phase ^= 1;
         // the join of the item before has to have read this stream's O before it is overwritten
         if (joined) {
           if (!mbar_wait(smem_u32(&c->ml_free), ml_phase ^ 1, &c->abort)) return;
@@ -641,6 +713,10 @@ struct Softmax {
       if (nb > 0) {
         if (!mbar_wait(smem_u32(&c->o_full[st]), o_phase, &c->abort)) return;
         o_phase ^= 1;
+        if (kApart) {  // of the last block, as of the others
+          if (!mbar_wait(smem_u32(&c->pv_done[st]), pv_phase, &c->abort)) return;
+          pv_phase ^= 1;
+        }
       }
       if (join && st == 1) {
         c->ml[row] = make_float2(m, l);
@@ -693,6 +769,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&c->s_full[i]), 1);
       mbar_init(smem_u32(&c->p_full[i]), 4);
       mbar_init(smem_u32(&c->o_full[i]), 1);
+      mbar_init(smem_u32(&c->s_free[i]), 4);
+      mbar_init(smem_u32(&c->pv_done[i]), 1);
       mbar_init(smem_u32(&c->wg[i]), 4);
     }
     mbar_init(smem_u32(&c->ml_full), 4);
@@ -729,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ld.run();
         if (*(volatile int*)&c->abort) ld.drain();
       } else if (warp == 9) {
-        Issuer<T, DP> is{a, c, smem, smem_u32(smem), smem_u32(smem) + L::kCtl, tmem};
+        Issuer<T, DP, TREE && DP == 64> is{a, c, smem, smem_u32(smem), smem_u32(smem) + L::kCtl, tmem};
         is.run();
         is.drain();
       } else if (warp == 8) {

@@ -240,6 +240,7 @@ struct Control {
   uint64_t kv_full[10], kv_empty[10];
   uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
   uint64_t ml_full, ml_free, wg[2], drain;
+  uint64_t s_free[2], pv_done[2];  // where weights and scores are apart
   float2 ml[kTile];  // m and l of stream 1 for the join
   int before[kMaxSeqs];  // items before each sequence, where they are taken in columns
   Cost sum[kThreads / 32];
