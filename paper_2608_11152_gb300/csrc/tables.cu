@@ -25,6 +25,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kThreads = 256;
 constexpr int kFillCtas = 4;               // on an SM
 constexpr int kRun = 480;                  // tokens of a warp at a time: at most 31 blocks, one a lane
+constexpr int kGives = 4;                  // blocks given back of a lane at a time
 constexpr int kFillTokens = 4096;          // most tokens of a step that one CTA makes
 
 struct TableArgs {
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid
   }
   const int head = __ldcg(a.head + kRingHead), base = __ldcg(a.head + kGiveBase), given = __ldcg(a.head + kGiven);
   // A warp's tokens are next to each other: only its first one is searched for.
-  const int share = (int)((n + warps - 1) / warps);
+  const int share = (int)max((n + warps - 1) / warps, (int64_t)32);
   const int stop = (int)min((int64_t)(warp + 1) * share, n);
   int t = (int)min((int64_t)warp * share, n);
   if (t < stop) {
@@ -397,16 +398,28 @@ __global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid
       if (t >= to) b = find(t, m, to);
     }
   }
-  const int64_t gives = ((int64_t)given + warps - 1) / warps, last = min((warp + 1) * gives, (int64_t)given);
+  const int64_t gives = max(((int64_t)given + warps - 1) / warps, (int64_t)32), last = min((warp + 1) * gives, (int64_t)given);
   int64_t j0 = warp * gives;
   if (j0 < last) {
     OffsetFinder find(a.give_off, a.n, (int)j0);
-#pragma unroll 2
-    for (; j0 < last; j0 += 32) {
-      const int j = (int)min(j0 + lane, last - 1);
-      int off, end;
-      const int b = find(j, off, end);
-      if (j0 + lane < last) give(a, base, b, j, __ldcg(a.give_from + b), off);
+    for (; j0 < last; j0 += 32 * kGives) {  // each step's loads on their way together
+      int64_t at[kGives];
+      int blk[kGives];
+#pragma unroll
+      for (int i = 0; i < kGives; ++i) {
+        const int j = (int)min(j0 + i * 32 + lane, last - 1);
+        int off, end;
+        const int b = find(j, off, end);
+        at[i] = (int64_t)b * a.stride + (j - off);
+        blk[i] = b;
+      }
+#pragma unroll
+      for (int i = 0; i < kGives; ++i) at[i] += __ldcg(a.give_from + blk[i]);
+#pragma unroll
+      for (int i = 0; i < kGives; ++i) blk[i] = __ldcg(a.table + at[i]);
+#pragma unroll
+      for (int i = 0; i < kGives; ++i)
+        if (j0 + i * 32 + lane < last) a.ring[ring_place(a, base, (int)(j0 + i * 32 + lane))] = blk[i];
     }
   }
 }
@@ -462,7 +475,7 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
   if (s->n <= kPlanThreads) launch_chained(k_table_plan<1, false>, 1, kPlanThreads, 0, st, a);
   else launch_chained(k_table_plan<4, false>, 1, kPlanThreads, 0, st, a);
   // Warps for the tokens, and for blocks given back: at most as many as the GPU holds at a time.
-  const int64_t warps = std::max<int64_t>((s->n_tokens - 1) / 128 + 1, s->n / 4);
+  const int64_t warps = std::max<int64_t>((s->n_tokens - 1) / 128 + 1, s->n / 2);
   launch_chained(k_table_fill, (int)std::min<int64_t>((warps - 1) / (kThreads / 32) + 1, kv->num_sms * kFillCtas), kThreads,
                  0, st, a);
   return launch_status();
