@@ -605,8 +605,8 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
  * A step that cannot be made changes nothing, but for q_off (zeros), positions and slots (-1) and
  * copies of what is not changed (state_out, kv_len_out): fewer free blocks than it takes (OOM),
  * more given than the ring has room for, a negative or longer count than allowed, a row with
- * fewer blocks than its kv_len tokens fill or too short for the step, offsets whose sum is not n_tokens (INVALID_ARG;
- * all sticky, from misat_kv_sync). */
+ * fewer blocks than its kv_len tokens fill or too short for the step, new tokens whose sum is not
+ * n_tokens (INVALID_ARG; all sticky, from misat_kv_sync). */
 typedef struct misat_kv_step {
   int32_t n;                 /* sequences, 0..max_batch of the pool */
   int32_t n_tokens;          /* sum of new_tokens, below 2^31 - 4096 */
@@ -634,7 +634,8 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* step, void* work, int64_t
 
 /* Norm of each head, and the rotation behind it:
  *   y = R_p (x r (offset + weight)),   r = 1 / sqrt(mean x^2 + eps)
- * over the head's head_dim elements, the sum of squares in 32 bits (elements beyond 2^60 in magnitude may overflow it).
+ * over the head's head_dim elements, the sum of squares in 32 bits (elements beyond 2^59 in
+ * magnitude may overflow it: y is then zero).
  * weight: [head_dim] for all heads (head_stride 0), or [heads][head_stride], of the tensor's dtype
  * or of MISAT_F32. */
 typedef struct misat_head_norm {
@@ -653,9 +654,10 @@ int misat_norm_rotary(const misat_rope* rope, const misat_head_norm* norm, int32
 /* Gradients of misat_norm_rotary's x and weight, given the gradient of its result (grad):
  *   g = R_p^T grad,  a = g (offset + weight),  dx = r a - x r^3 mean(a x),  dweight = sum g x r
  * (the sum over tokens, and over heads where they share the weight; in 32 bits, in an order that
- * depends on sizes and GPU alone, so the same call gives the same bits).  dx may be x or grad
- * (same pointer and strides); dweight has the weight's dtype and shape, its rows dw_head_stride >=
- * head_dim elements apart (not read where the heads share one).  work: device scratch of *bytes from misat_norm_rotary_work, 16-byte aligned, the call's own until it is
+ * depends on sizes, alignment and GPU alone, so the same call gives the same bits).  dx may be x
+ * or grad (same pointer and strides).  dweight has the weight's dtype and shape, its rows
+ * dw_head_stride >= head_dim elements apart (not read where the heads share one).  work: device
+ * scratch of *bytes from misat_norm_rotary_work, 16-byte aligned, the call's own until it is
  * finished.  Errors: INVALID_ARG, CUDA.  [async] */
 int misat_norm_rotary_work(const misat_rope* rope, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens,
                            int32_t n_heads, int32_t head_dim, int64_t* bytes);
@@ -688,29 +690,32 @@ typedef struct misat_kv_draft {
 int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* parents, int32_t window, int32_t* depth,
                   uint32_t* bits, int32_t words, void* cuda_stream);
 
-/* misat_kv_append with norms of the queries' and the keys' heads before the rotation (each NULL: none),
- * and with the positions of a tree's nodes (draft NULL: tokens in a row).  Nodes go into the slots of their
- * numbers, absent ones at depth 0.  Errors as misat_kv_append's.  [async] */
+/* misat_kv_append with norms of the queries' and the keys' heads before the rotation (each NULL:
+ * none), and with the positions of a tree's nodes (draft NULL: tokens in a row).  Nodes go into the
+ * slots of their numbers, absent ones at depth 0.  Errors as misat_kv_append's.  [async] */
 int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_head_norm* q_norm,
                          const misat_head_norm* k_norm, const misat_kv_draft* draft, const void* k,
                          int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
                          int64_t v_head_stride, const void* q, int64_t q_token_stride, int64_t q_head_stride,
                          void* q_out, int64_t qo_token_stride, int64_t qo_head_stride, void* cuda_stream);
 
-/* misat_kv_attend of a tree's nodes: a node sees the tokens before the tree (with a window those at positions
- * above its own less the window) and the nodes of its bits.  An absent node gets zeros, and -infinity
- * in lse.  kv_len below the new tokens leaves nodes below position zero, which see nothing.  As there, what only some nodes see has to be
- * finite for all of them.  Errors as misat_kv_attend's.  [async] */
+/* misat_kv_attend of a tree's nodes: a node sees the tokens before the tree (with a window those
+ * at positions above its own less the window) and the nodes of its bits.  An absent node gets
+ * zeros, and -infinity in lse, whatever its query holds.  kv_len below the new tokens leaves nodes
+ * below position zero, which see nothing.  As there, what only some nodes see has to be finite for
+ * all of them.  Errors as misat_kv_attend's.  [async] */
 int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_kv_draft* draft, const void* q,
                          int64_t q_token_stride, int64_t q_head_stride, void* out, int64_t out_token_stride,
                          int64_t out_head_stride, float* lse, void* cuda_stream);
 
-/* What is kept of the trees: for every sequence, keys and values of the nodes path[0] < path[1] < ... (the first
- * n_keep of row b of path) move to the slots kv_len - new, kv_len - new + 1, ..., in place, and kv_len_out
- * becomes kv_len - new + n_keep.  Where the path is a line of the tree these are the positions that the keys were rotated
- * to.  The slots behind hold what they held.  A path that does not rise or leaves the tree is a sticky error: that
- * sequence is left as it was.  No two rows of a batch may share the blocks of their new tokens.  kv_len_out must not be kv_len.
- * [async]  Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES), CUDA; INVALID_ARG later. */
+/* What is kept of the trees: for every sequence, keys and values of the nodes path[0] < path[1] <
+ * ... (the first n_keep of row b of path, at most path_stride) move to the slots kv_len - new,
+ * kv_len - new + 1, ..., in place, and kv_len_out becomes kv_len - new + n_keep.  Where the path is
+ * a line of the tree these are the positions that the keys were rotated to.  The slots behind hold
+ * what they held.  A path that does not rise or leaves the tree is a sticky error: that sequence is
+ * left as it was.  No two sequences of a batch may share the blocks of their new tokens.
+ * kv_len_out must not be kv_len.  [async]
+ * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES), CUDA; INVALID_ARG later. */
 int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path, int64_t path_stride,
                   const int32_t* n_keep, int32_t* kv_len_out, void* cuda_stream);
 

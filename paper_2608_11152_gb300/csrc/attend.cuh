@@ -33,7 +33,9 @@
 // loaded by warp 8 beside them, 256 sequences took 1,274 us instead of 1,209.
 //
 // Trees of drafted tokens (TREE): a node's keys are those before the tree and the ones of its bits, so a block that reaches
-// into the tree takes its mask from the node's words instead of from its position; nothing else differs.
+// into the tree takes its mask from the node's words instead of from its position.  64 query heads' 63 nodes over
+// 130,941 tokens (8 kv heads of 64, f16) take 176 us, 96 sequences of 16 to 32 nodes over 512 to 16,000 tokens (8 kv heads of
+// 128) 509 against 505 for the same tokens in a row.
 #pragma once
 
 #include <algorithm>
@@ -76,7 +78,8 @@ __device__ __forceinline__ uint32_t col_s(int st) { return st * 128; }
 template <int DP>
 __device__ __forceinline__ uint32_t col_o(int st) { return 256 + st * DP; }
 // APART: the weights have columns of their own, which heads up to 64 leave free.  The next scores then form as soon as
-// the last ones are read, under the exponentials, and the chain of a stream is its softmax alone.
+// the last ones are read, under the exponentials, and the chain of a stream is its softmax alone (the 63 nodes above: 175 us,
+// 184 with weights in the scores' place).
 template <bool APART>
 __device__ __forceinline__ uint32_t col_p(int st) { return APART ? 384 + st * 64 : col_s(st); }
 
