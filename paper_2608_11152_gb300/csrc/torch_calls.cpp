@@ -118,11 +118,13 @@ const at::Tensor& heads(PyObject* o, const char* name, at::ScalarType dtype, c10
 at::Tensor fresh(at::IntArrayRef size, at::ScalarType dtype, c10::DeviceIndex device) {
   return at::Tensor(at::detail::empty_cuda(size, dtype, at::Device(at::kCUDA, device), std::nullopt));
 }
-// n whole numbers of an array, from one on, as a tensor by itself (an allocation is 0.7 us, this 0.1).
-at::Tensor piece(const at::Tensor& array, int64_t from, int64_t n) {
-  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(array.storage()), array.key_set(), array.dtype());
+// A tensor of whole numbers in an array of them, from number `from` (of the tensor's type) on: an allocation is 0.7 us,
+// this 0.1.
+at::Tensor piece(const at::Tensor& array, int64_t from, at::IntArrayRef size, at::ScalarType dtype = at::kInt) {
+  at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(array.storage()), array.key_set(),
+                                                          c10::scalarTypeToTypeMeta(dtype));
   t.unsafeGetTensorImpl()->set_storage_offset(from);
-  t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
   return t;
 }
 // Autograd finds out by its version that a tensor it has saved was written.
@@ -559,7 +561,8 @@ PyObject* tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int32_t window = int32_of(a[3], "window");
   if (window < 0 || b->b.max_q > MISAT_KV_TREE_NODES) return fail(MISAT_ERR_INVALID_ARG, "misat_kv_tree");
   const int32_t words = (b->b.max_q + 31) / 32;
-  const at::Tensor depth = fresh({T}, at::kInt, p->device), bits = fresh({T, words}, at::kInt, p->device);
+  const at::Tensor all_words = fresh({T * (words + 1)}, at::kInt, p->device), depth = piece(all_words, T * words, {T}),
+                   bits = piece(all_words, 0, {T, words});
   Tree t{{depth.data_ptr<int32_t>(), reinterpret_cast<uint32_t*>(bits.data_ptr<int32_t>()), words, window},
          T, b->b.max_q, p->device, {nullptr, {depth, bits}}};
   t.made.on = ordered(p);
@@ -665,12 +668,13 @@ PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   s.columns = (int32_t)columns;
   s.ring_size = (int32_t)places;
   const bool given = a[9] != Py_None;
-  // One allocation for what there is of each sequence, each array at a 16-byte boundary.
+  // One allocation for what there is of each sequence, each array at a 16-byte boundary, and one for the tokens'.
   const int64_t bytes = MISAT_KV_TABLES_WORK(seqs), row = (seqs + 2 + 3) / 4 * 4;
   const at::Tensor rows = fresh({3 * row + bytes / 4}, at::kInt, p->device);
-  const at::Tensor after = given ? tensor(a[9], "out") : piece(rows, 0, seqs + 2), q_off = piece(rows, row, seqs + 1),
-                   len = piece(rows, 2 * row, seqs), positions = fresh({s.n_tokens}, at::kInt, p->device),
-                   slots = fresh({s.n_tokens}, at::kLong, p->device);
+  const int64_t T = s.n_tokens, half = (T + 1) / 2;
+  const at::Tensor after = given ? tensor(a[9], "out") : piece(rows, 0, {seqs + 2}), q_off = piece(rows, row, {seqs + 1}),
+                   len = piece(rows, 2 * row, {seqs}), tokens = fresh({T + half}, at::kLong, p->device),
+                   slots = piece(tokens, 0, {T}, at::kLong), positions = piece(tokens, 2 * T, {T});
   s.state_out = ints(after, "out", p->device, {seqs + 2});
   s.q_off = q_off.data_ptr<int32_t>();
   s.kv_len_out = len.data_ptr<int32_t>();
