@@ -103,7 +103,7 @@ struct OffsetFinder {
       if (b < 0 && !beyond) {
         b = base + lo;
         from = first;
-        to = lo < 31 ? second : __ldcg(off + b + 1);
+        to = lo < 31 ? second : __ldcg(off + min(b + 1, n));  // (b = n: an item behind the last sequence)
       }
       if (!__any_sync(0xffffffffu, b < 0)) return min(b, n - 1);
       load(base + 31);

@@ -330,7 +330,7 @@ struct MarkFinder {
       if (b < 0 && !beyond) {
         b = base + lo;
         m = own;
-        to = lo < 31 ? next : __ldcg(&marks[b + 1].x);
+        to = lo < 31 ? next : __ldcg(&marks[min(b + 1, n)].x);
       }
       if (!__any_sync(0xffffffffu, b < 0)) return min(b, n - 1);
       load(base + 31);

@@ -369,3 +369,26 @@ def test_refused_arguments():
     with pytest.raises(ValueError):
         pool.append(batch, k, k, q=k, k_norm=each)
     pool.sync()
+
+
+@pytest.mark.parametrize("n", [1, 30, 31, 32, 33, 62, 63])
+def test_append_of_tokens_of_no_sequence_is_a_sticky_error(n):
+    """Tokens behind the last sequence, or before the first, are in none: nothing of them is written."""
+    m = misat()
+    s = Step([(1, 3 + b) for b in range(n)], 1, 16, BF16)
+    pool = s.pool(1)
+    norm = m.HeadNorm(torch.ones(16, device="cuda"))
+    x = rand((n + 5, 1, 16), BF16, 1)
+    for shift in (0, 5):
+        s.kb.zero_()
+        batch = pool.batch(s.q_off + shift, s.kv_len, s.table, n_tokens=n + 5, max_q=1)
+        q = torch.full_like(x, 7.0)
+        pool.append(batch, x, x, q=x, q_out=q, q_norm=norm, k_norm=norm)
+        with pytest.raises(m.MisatError) as e:
+            pool.sync()
+        assert e.value.code == m.ERR_INVALID_ARG
+        mine = slice(shift, shift + n)
+        rest = torch.ones(n + 5, dtype=torch.bool)
+        rest[mine] = False
+        assert (q[rest.cuda()] == 7).all() and not (q[mine] == 7).all(-1).any()
+        assert int((s.kb != 0).any(-1).sum()) == n
