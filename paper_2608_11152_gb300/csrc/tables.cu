@@ -31,6 +31,8 @@ constexpr int kFillCtas = 4;               // on an SM
 constexpr int kRun = 480;                  // tokens of a warp at a time: at most 31 blocks, one a lane
 constexpr int kGives = 4;                  // blocks given back of a lane at a time
 constexpr int kFillTokens = 4096;          // most tokens of a step that one CTA makes
+constexpr int kFillPlaces = 1 << 17;       // most places of a table whose blocks one CTA gives back, however many they are
+constexpr int kFillGives = 8192;           // most blocks that it gives back of a larger one
 
 struct TableArgs {
   int32_t n, n_tokens, max_q, columns, ring_size;
@@ -53,6 +55,7 @@ struct TableArgs {
   int4* marks;
   int32_t *give_off, *give_from;
   bool vec_rows;  // what is read and written of each sequence, at 16-byte boundaries
+  bool defer;     // a step of one CTA: many blocks given back are left to the second kernel
 };
 // Of a sequence: first new token, length after the step, blocks held before it, blocks taken before it.
 struct Mark {
@@ -141,12 +144,6 @@ __device__ __forceinline__ Place place_of(const TableArgs& a, int b, int col, in
   if (col < held) return {row, nullptr};
   return {a.ring + ring_place(a, ring_head, k), row};
 }
-// One block given back: the j-th of all.
-__device__ __forceinline__ void give(const TableArgs& a, int base, int b, int j, int from, int off) {
-  const int col = from + j - off;
-  if (col >= 0 && col < a.columns) a.ring[ring_place(a, base, j)] = __ldcg(a.table + (int64_t)b * a.stride + col);
-}
-
 // The last i with off[i] <= t, off in shared memory with off[n] > t.
 __device__ __forceinline__ int search(const int32_t* off, int n, int t) {
   int lo = 0, hi = n;
@@ -257,6 +254,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
     }
   }
   const int give_base = go ? ring_place(a, head, count) : 0, given = (int)total.give;
+  const bool later = FILL && a.defer && go && given > kFillGives;
   if (tid == 0) {
     a.q_off[a.n] = go ? a.n_tokens : 0;
     if (!go) set_error(a.err, sound ? MISAT_ERR_OOM : MISAT_ERR_INVALID_ARG);
@@ -267,11 +265,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
       s_give[a.n] = given;
     } else {
       a.marks[a.n] = make_int4(a.n_tokens, 0, 0, 0);
-      a.give_off[a.n] = given;
-      a.head[kOk] = go;
+    }
+    if (!FILL || a.defer) {
+      a.head[kOk] = FILL || go;
       a.head[kRingHead] = head;
       a.head[kGiveBase] = give_base;
-      a.head[kGiven] = given;
+      a.head[kGiven] = FILL && !later ? 0 : given;
+      if (!FILL || later) a.give_off[a.n] = given;
     }
   }
   if constexpr (FILL) {
@@ -290,11 +290,18 @@ __global__ void __launch_bounds__(kPlanThreads) k_table_plan(const __grid_consta
       a.positions[t] = pos;
       a.slots[t] = slot;
     }
-    if (go)
+    if (later) {
+      if (tid < a.n) {
+        a.give_off[tid] = s_give[tid];
+        a.give_from[tid] = s_from[tid];
+      }
+    } else if (go) {
+#pragma unroll 4
       for (int j = tid; j < given; j += kPlanThreads) {
         const int b = search(s_give, a.n, j);
-        give(a, give_base, b, j, s_from[b], s_give[b]);
+        a.ring[ring_place(a, give_base, j)] = __ldcg(a.table + (int64_t)b * a.stride + (s_from[b] + j - s_give[b]));
       }
+    }
   }
 }
 
@@ -471,9 +478,15 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
     return (all & 15) == 0;
   };
   a.vec_rows = whole({a.fresh, a.kv_len, a.shared, a.state, a.state_out, a.q_off, a.kv_len_out});
-  // A small step is one CTA's: 256 sequences of one token 4.2 us, as two kernels about 9.
+  // A small step is one CTA's: 256 sequences of one token 4.2 us, as two kernels about 9.  Where the table is so large that
+  // sequences that finish could give back more blocks than one CTA should move, a second kernel looks whether they do
+  // (256 sequences that hold up to 30,000 tokens: 7.0 us a step, all of them finished 8.2; of 65,000 blocks in a table below
+  // that size, all given back, one CTA takes 47).
   if (s->n <= kPlanThreads && s->n_tokens <= kFillTokens) {
+    a.defer = (int64_t)s->n * s->columns > kFillPlaces;
     launch_chained(k_table_plan<1, true>, 1, kPlanThreads, 0, st, a);
+    a.n_tokens = 0;
+    if (a.defer) launch_chained(k_table_fill, kv->num_sms, kThreads, 0, st, a);
     return launch_status();
   }
   if (s->n <= kPlanThreads) launch_chained(k_table_plan<1, false>, 1, kPlanThreads, 0, st, a);

@@ -250,3 +250,15 @@ def test_refused_arguments():
     assert f(t.pool._h, None, p, 1000, None) == m.ERR_INVALID_ARG
     for args in ((None, 1000), (p, 111), (p + 4, 900)):
         assert f(t.pool._h, s, *args, None) == m.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("each", [3, 16, 700, 5000])
+def test_many_blocks_given_back_by_a_small_step(each):
+    """Of a table with so many places that they are left to a second kernel where they are many."""
+    n = 60
+    held = [each if b % 3 else 5 for b in range(n)]
+    t = Tables(held, 5001, 40, seed=each)
+    kv = [0 if b % 3 else 70 for b in range(n)]
+    got = t.check([0 if b % 3 else 30 for b in range(n)], kv, [min(7, h) if b % 5 == 0 else 0 for b, h in enumerate(held)])
+    t.state = got.state.tolist()
+    t.check([1] * n, got.kv_len.tolist(), state=got.state)
