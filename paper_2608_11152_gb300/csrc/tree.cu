@@ -9,7 +9,7 @@
 // written, also where it has several rows in flight.
 //
 // Both are bound by latency: a few dependent reads a sequence, then one pass over the rows.  The plan of 64 trees of 16 to
-// 32 nodes takes 2.3 us, of 1,024 trees of 129 nodes 5.6; paths of 64 such trees (8 kv heads of 128) 3.4 us.  1,024 paths of
+// 32 nodes takes 2.1 us, of 1,024 trees of 129 nodes 4.9; paths of 64 such trees (8 kv heads of 128) 3.4 us.  1,024 paths of
 // up to 64 rows of 8 x 64 elements move 95 MB in 21.7 us, 0.64 of the copy rate: 128 bytes at a place.  Sixteen rows of a
 // column are in flight (8: 27.4 us, 24: 22.7, 32: 21.9).
 #include <algorithm>
@@ -20,7 +20,8 @@ using namespace misat;
 
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 128;    // of k_keep
+constexpr int kMaxNodes = 512;   // threads of k_tree: one a node up to here
 constexpr int kRoot = -1, kAbsent = -2;
 
 struct TreeArgs {
@@ -44,38 +45,37 @@ __device__ __forceinline__ Range load_range(const KvBatch& k, int b, int32_t* er
   return {begin, ok ? end - begin : 0, len};
 }
 
-__global__ void __launch_bounds__(kThreads) k_tree(const __grid_constant__ TreeArgs a) {
+__global__ void __launch_bounds__(kMaxNodes) k_tree(const __grid_constant__ TreeArgs a) {
   __shared__ int32_t up[MISAT_KV_TREE_NODES];
   chain_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0 &&
       (__ldcg(a.b.q_off) != 0 || __ldcg(a.b.q_off + a.b.n) != a.b.n_tokens))
     set_error(a.err, MISAT_ERR_INVALID_ARG);
   const Range s = load_range(a.b, blockIdx.x, a.err);
-  for (int i = threadIdx.x; i < s.n; i += kThreads) {
+  for (int i = (int)threadIdx.x; i < s.n; i += blockDim.x) {
     const int p = __ldcg(a.parent + s.begin + i);
     up[i] = p < i && p >= kAbsent ? p : kAbsent - 1;  // (neither a parent nor one of the two marks)
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < s.n; i += kThreads) {
-    // Up once for the depth, and to see that the line ends at the tokens before the tree.
-    int depth = 0, at = i, p;
-    while ((p = up[at]) >= 0) {
-      at = p;
-      ++depth;
-    }
-    const bool there = p == kRoot;
-    if (!there && !(p == kAbsent && at == i)) set_error(a.err, MISAT_ERR_INVALID_ARG);
-    a.depth[s.begin + i] = there ? depth : 0;
+  for (int i = (int)threadIdx.x; i < s.n; i += blockDim.x) {
+    // Up to the tokens before the tree, with the bits of the first `window` nodes.
     uint32_t* row = a.bits + (int64_t)(s.begin + i) * a.words;
-    int left = !there ? 0 : a.window > 0 ? min(a.window, depth + 1) : depth + 1;
-    at = i;
+    int at = i, nodes = 0;
+    const int most = a.window > 0 ? a.window : MISAT_KV_TREE_NODES;
     for (int w = a.words - 1; w >= 0; --w) {
       uint32_t word = 0;
-      for (; left > 0 && at >= w * 32; --left) {
+      for (; at >= w * 32 && nodes < most; ++nodes) {
         word |= 1u << (at & 31);
         at = up[at];
       }
       row[w] = word;
+    }
+    for (; at >= 0; ++nodes) at = up[at];
+    const bool there = at == kRoot;
+    a.depth[s.begin + i] = there ? nodes - 1 : 0;
+    if (!there) {
+      if (at != kAbsent || nodes > 1) set_error(a.err, MISAT_ERR_INVALID_ARG);
+      for (int w = 0; w < a.words; ++w) row[w] = 0;
     }
   }
 }
@@ -158,7 +158,8 @@ int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* pare
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!parents || !depth || !bits || batch->max_q == 0 || !on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
   const TreeArgs a{batch_view(batch), parents, depth, bits, words, window, kv->err};
-  launch_chained(k_tree, batch->n, kThreads, 0, static_cast<cudaStream_t>(cuda_stream), a);
+  const int threads = std::min((batch->max_q + 31) / 32 * 32, kMaxNodes);
+  launch_chained(k_tree, batch->n, threads, 0, static_cast<cudaStream_t>(cuda_stream), a);
   return launch_status();
 }
 
