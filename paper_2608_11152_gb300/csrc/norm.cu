@@ -390,6 +390,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
   S stages(part, s_mem);
   const int h = a.first + blockIdx.y * a.chunk + group - side * a.chunk;
   const bool mine = side < a.side && h < a.first + a.heads;
+  const bool works = __any_sync(0xffffffffu, mine);  // the warp has a head at all
   const bool q = h < a.hq, k = h < a.hq + a.hkv;
   const Heads& src = q ? a.x : k ? a.k : a.v;
   const int hh = q ? h : k ? h - a.hq : h - a.hq - a.hkv;
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
       s_slot[tid] = ok ? ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d : -1;
     }
     __syncthreads();
-    for (int base = 0; base < nt; base += a.side) {
+    for (int base = works ? 0 : nt; base < nt; base += a.side) {
       const int t = base + side;
       const bool ok = mine && t < nt;
       typename P::Raw raw;
@@ -497,6 +498,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(true).threads,
   S stages(part, s_mem);
   const int h = blockIdx.y * a.chunk + group - side * a.chunk;
   const bool mine = side < a.side && h < a.heads;
+  const bool works = __any_sync(0xffffffffu, mine);
   const int begin = blockIdx.x * a.per, end = (int)min((int64_t)begin + a.per, (int64_t)a.n_tokens);
   const T* x_in = static_cast<const T*>(a.x.p) + (int64_t)h * a.x.hs + (int64_t)(begin + side) * a.x.ts;
   const T* g_in = static_cast<const T*>(a.dy.p) + (int64_t)h * a.dy.hs + (int64_t)(begin + side) * a.dy.ts;
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(true).threads,
     __syncthreads();
     turns.fill(a, nt, s_pos);
     __syncthreads();
-    for (int base = 0; base < nt; base += a.side) {
+    for (int base = works ? 0 : nt; base < nt; base += a.side) {
       const int t = base + side;
       const bool ok = mine && t < nt;
       typename P::Raw raw_x, raw_g;
