@@ -146,12 +146,6 @@ struct Part {
         if (has(j) && has_second(j)) *reinterpret_cast<V*>(p + second(j)) = r.hi[j];
     }
   }
-  // Vectors that are not there become zeros, whatever the copy left: they add nothing to the sums.
-  __device__ __forceinline__ void clear_absent(Raw& r) const {
-    each([&](int v, int, bool there) {
-      if (!there) r.vec(v) = V{};
-    });
-  }
   // In 32 bits, and back.
   __device__ __forceinline__ void widen(const Raw& r, float (&x)[UPL][kElems]) const {
 #pragma unroll
@@ -342,7 +336,18 @@ struct Stages {
 
   __device__ __forceinline__ Stages(const P& part, void* smem)
       : part(part), smem(static_cast<const char*>(smem) + threadIdx.x * kVec),
-        base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * kVec) {}
+        base((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * kVec) {
+    // Vectors that are not there are zeros from the start, and no copy touches them: they add nothing to the sums.
+    if constexpr (WHOLE) {
+      char* mine = static_cast<char*>(smem) + threadIdx.x * kVec;
+      for (int i = 0; i < kDepth * TENSORS; ++i)
+        part.each([&](int v, int, bool there) {
+          if (!there) *reinterpret_cast<typename P::V*>(mine + (i * (P::kBytes / kVec) + v) * kThreads * kVec) = {};
+        });
+    } else {
+      for (int i = 0; i < TENSORS; ++i) part.each([&](int v, int, bool) { next[i].vec(v) = {}; });
+    }
+  }
   __device__ __forceinline__ uint32_t at(int stage, int tensor, int vec) const {
     return base + ((stage * TENSORS + tensor) * (P::kBytes / kVec) + vec) * kThreads * kVec;
   }
@@ -381,7 +386,8 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
     k_norm_rotate(const __grid_constant__ NormArgs a) {
   extern __shared__ __align__(16) float s_mem[];
   __shared__ int32_t s_pos[kMaxTile];
-  __shared__ int64_t s_slot[kMaxTile];  // element offset of the token's row of kv head 0, -1: skip
+  // Element offsets of a token's row in the queries' result and of its row of kv head 0 in the blocks, -1: skip.
+  __shared__ int64_t s_row[kMaxTile][2];
   using P = Part<T, VEC, HALF, UPL>;
   using S = Stages<P, T, VEC != 1, 1>;
   float* s_turn = s_mem + S::kSize / 4;
@@ -425,7 +431,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
     if (a.hkv == 0) {
       if (tid < nt) {
         s_pos[tid] = ahead_pos;
-        s_slot[tid] = 0;
+        s_row[tid][0] = (int64_t)(t0 + tid) * a.out.ts;
       }
       if (tid < a.tile && t0 + a.tile + tid < end) ahead_pos = __ldcg(a.positions + t0 + a.tile + tid);
     } else if (tid < 32) {
@@ -444,7 +450,8 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
     if (a.hkv > 0 && tid < nt) {  // (the block's number arrives meanwhile)
       const bool ok = blk >= 0 && blk < a.n_blocks;
       if (!ok) set_error(a.err, MISAT_ERR_INVALID_ARG);
-      s_slot[tid] = ok ? ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d : -1;
+      s_row[tid][0] = ok ? (int64_t)(t0 + tid) * a.out.ts : -1;
+      s_row[tid][1] = ok ? ((int64_t)blk * a.hkv * kBlockTokens + pos % kBlockTokens) * a.d : -1;
     }
     __syncthreads();
     for (int base = works ? 0 : nt; base < nt; base += a.side) {
@@ -460,11 +467,11 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
         stages.take(0, 0, raw);
         issue();
       }
-      part.clear_absent(raw);
       float x[UPL][P::kElems];
       part.widen(raw, x);
       const float sum = part.sum(dot(x, x));
-      if (!ok || s_slot[t] < 0) continue;
+      const int64_t row = s_row[t < nt ? t : 0][q ? 0 : 1];
+      if (!ok || row < 0) continue;
       if (k) {
         if (normed) {
           const float r = rsqrtf(fmaf(sum, a.inv_d, hw.eps));
@@ -479,7 +486,7 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(false).threads,
         part.template turn_all<false>(cs, cs + a.turns, x);
         part.narrow(x, raw);
       }
-      part.put(base_out + (q ? (int64_t)(t0 + t) * a.out.ts : s_slot[t]), raw);
+      part.put(base_out + row, raw);
     }
   }
 }
@@ -547,8 +554,6 @@ __global__ void __launch_bounds__(Part<T, VEC, HALF, UPL>::shape(true).threads,
         issue();
       }
       float x[UPL][P::kElems], g[UPL][P::kElems];
-      part.clear_absent(raw_x);
-      part.clear_absent(raw_g);
       part.widen(raw_x, x);
       part.widen(raw_g, g);
       const float* cs = s_turn + (ok ? t : 0) * 2 * a.turns;
