@@ -10,8 +10,8 @@
 // are worked out once for all heads of the CTA.  Squares, sums and products are in 32 bits, results are rounded once.
 //
 // Bound by memory where there are many tokens: 65,536 x 32 heads of 128 in bf16 forward 162 us for 1.07 GB (6.6 TB/s,
-// 0.97 of a plain copy), backward 243 us for 1.61 GB (0.97); by latency and issue where there are few: 64 tokens 2.8 us,
-// 5,003 tokens of 28 heads of 96 13.3 us (floor 7.9).  With the next token in registers instead of shared memory
+// 0.97 of a plain copy), backward 241 us for 1.61 GB (0.98); by latency and issue where there are few: 64 tokens 2.8 us,
+// 5,003 tokens of 28 heads of 96 12.4 us (floor 7.9).  With the next token in registers instead of shared memory
 // these two were 411 and 24.8 us.
 //
 // The weight's gradient is a sum over tokens (and heads): each CTA of a fixed grid writes the sum of its tokens, and a
@@ -684,8 +684,8 @@ Grid plan(NormArgs& a, int elem, bool half_layout, int vec, bool backward, int n
   // that would be many rounds: they then work on neighbouring rows at any time (65,536 x 32 heads of 128 in bf16: 192 us
   // with one wave of CTAs, 173 with 32 rounds a CTA, 166 with 24, 163 with 16; the append of 70,000 tokens, which looks up
   // their places: 280, 258, 256, 262).  A little more than one wave would be two (40,000 x 8 heads: 33.5 us with 17
-  // rounds, 38.3 with 16).  Element by element a CTA's first steps cost more than that gains (10,000 x 32 heads of 154:
-  // 100 us, 126 with 32 rounds).
+  // rounds, 38.3 with 16).  Element by element a CTA's first steps cost more than that gains (10,000 x 32 heads of 154
+  // when this was measured: 100 us, 126 with 32 rounds).
   const int rounds = (a.n_tokens - 1) / a.side + 1, most = std::max(1, num_sms * shape.ctas / g.y);
   a.per = (rounds - 1) / std::min(rounds, most) + 1;
   const int most_rounds = a.hkv ? 24 : 16;
