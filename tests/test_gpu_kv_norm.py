@@ -392,3 +392,22 @@ def test_append_of_tokens_of_no_sequence_is_a_sticky_error(n):
         rest[mine] = False
         assert (q[rest.cuda()] == 7).all() and not (q[mine] == 7).all(-1).any()
         assert int((s.kb != 0).any(-1).sum()) == n
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("heads,d,rot,half", [(9, 154, 106, False), (9, 154, 104, True), (33, 206, 206, False), (5, 252, 56, True),
+                                              (64, 36, 36, True), (48, 128, 128, True)])
+def test_vectors_of_two_elements(heads, d, rot, half, dtype):
+    m = misat()
+    x, dy, w, pos = made(333, heads, d, dtype, F32, True)
+    rope = m.Rope(rot, layout=m.ROPE_HALF if half else m.ROPE_INTERLEAVED)
+    within(rope, x, dy, w, pos, kref.frequencies(rot), half)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 50, 2.0 ** 20, 2.0 ** -20, 2.0 ** -50])
+@pytest.mark.parametrize("half", [True, False])
+def test_sizes_of_values(half, size):
+    """Squares stay inside 32 bits up to 2^59 an element; small heads are what eps leaves of them."""
+    m = misat()
+    x, dy, w, pos = made(50, 4, 64, BF16, F32, False)
+    within(m.Rope(64, layout=m.ROPE_HALF if half else m.ROPE_INTERLEAVED), x * size, dy, w, pos, kref.frequencies(64), half)

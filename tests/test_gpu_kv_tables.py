@@ -262,3 +262,37 @@ def test_many_blocks_given_back_by_a_small_step(each):
     got = t.check([0 if b % 3 else 30 for b in range(n)], kv, [min(7, h) if b % 5 == 0 else 0 for b, h in enumerate(held)])
     t.state = got.state.tolist()
     t.check([1] * n, got.kv_len.tolist(), state=got.state)
+
+
+@pytest.mark.parametrize("n", [100, 3000, 5000])
+@pytest.mark.parametrize("off", [0, 1])
+def test_arrays_at_any_boundary_and_lengths_in_place(n, off):
+    """By the library: every array of the sequences 4 bytes past a 16-byte boundary, and results over their inputs."""
+    m = misat()
+    new, kv, held = drawn(n, 7 * n + off, 3, 60)
+    t = Tables(held, 10, n + 20, seed=n)
+    r = random.Random(n)
+    shared = [r.randint(0, h) for h in held]
+    want = ref.tables(n, new, kv, t.state, t.table, t.ring, shared)
+
+    def at(values):
+        x = ints([0] * off + list(values) + [77])
+        return x, x.data_ptr() + 4 * off
+
+    T = sum(new)
+    arrays = {k: at(v) for k, v in dict(new_tokens=new, kv_len=kv, shared=shared, state=t.state, q_off=[5] * (n + 1),
+                                        positions=[5] * T).items()}
+    slots = torch.full((T + 1,), 5, dtype=torch.int64, device="cuda")
+    work = torch.empty(24 * n + 64, dtype=torch.uint8, device="cuda")
+    p = {k: v[1] for k, v in arrays.items()}
+    s = m.misat_kv_step(n=n, n_tokens=T, max_q=max(new), columns=10, table_stride=t.d_table.stride(0), ring_size=len(t.ring),
+                        block_table=t.d_table.data_ptr(), ring=t.d_ring.data_ptr(), state_out=p["state"],
+                        kv_len_out=p["kv_len"], slots=slots.data_ptr(), **p)
+    st = torch.cuda.current_stream().cuda_stream
+    assert m._lib.misat_kv_tables(t.pool._h, ctypes.byref(s), work.data_ptr(), work.numel(), st) == 0
+    t.pool.sync()
+    for name, w in zip(("state", "q_off", "kv_len", "positions"), want):
+        assert arrays[name][0].tolist() == [0] * off + w + [77], name
+    assert slots.tolist() == want[4] + [5]
+    assert t.d_table.tolist() == t.table and t.d_ring.tolist() == t.ring
+    assert arrays["new_tokens"][0].tolist()[off:-1] == new and arrays["shared"][0].tolist()[off:-1] == shared
