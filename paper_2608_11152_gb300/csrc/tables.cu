@@ -349,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid
   const int lane = threadIdx.x & 31;
   const int warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
   chain_wait();
-  const bool go = __ldcg(a.head + kOk) != 0;
+  const int4 plan = __ldcg(reinterpret_cast<const int4*>(a.head));  // in the order of Head
+  const bool go = plan.x != 0;
   const int64_t n = a.n_tokens;
   if (!go) {
     for (int64_t t = (int64_t)warp * 32 + lane; t < n; t += (int64_t)warps * 32) {
@@ -358,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, kFillCtas) k_table_fill(const __grid
     }
     return;
   }
-  const int head = __ldcg(a.head + kRingHead), base = __ldcg(a.head + kGiveBase), given = __ldcg(a.head + kGiven);
+  const int head = plan.y, base = plan.z, given = plan.w;
   // A warp's tokens are next to each other: only its first one is searched for.
   const int share = (int)max((n + warps - 1) / warps, (int64_t)32);
   const int stop = (int)min((int64_t)(warp + 1) * share, n);
