@@ -477,10 +477,17 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t bytes = 0;
   int rc = misat_norm_rotary_work(c.r->h, &w, c.code, (int32_t)c.T, (int32_t)c.H, (int32_t)c.D, &bytes);
   if (rc != MISAT_OK) return fail(rc, "misat_norm_rotary_backward");
-  const at::Tensor work = fresh({bytes / 4}, at::kFloat, c.r->device), dw = fresh(norm->w.sizes(), norm->w.scalar_type(), c.r->device);
+  // Little scratch (a small call) shares the gradient's allocation.
+  const at::IntArrayRef shape = norm->w.sizes();
+  const int64_t own = (norm->w.numel() * 4 + 15) / 16 * 4;
+  const bool together = bytes <= 64 * 1024;
+  const at::Tensor work = fresh({(together ? own : 0) + bytes / 4}, at::kFloat, c.r->device);
+  const at::Tensor dw = together ? piece(work, 0, shape, norm->w.scalar_type())
+                                 : fresh(shape, norm->w.scalar_type(), c.r->device);
+  float* const scratch = work.data_ptr<float>() + (together ? own : 0);
   rc = misat_norm_rotary_backward(c.r->h, &w, c.code, (int32_t)c.T, (int32_t)c.H, (int32_t)c.D, x.data_ptr(),
                                   x.stride(0), x.stride(1), g.data_ptr(), g.stride(0), g.stride(1), c.positions,
-                                  dx.data_ptr(), dx.stride(0), dx.stride(1), dw.data_ptr(), c.D, work.data_ptr(), bytes,
+                                  dx.data_ptr(), dx.stride(0), dx.stride(1), dw.data_ptr(), c.D, scratch, bytes,
                                   c10::cuda::getCurrentCUDAStream(c.r->device).stream());
   if (rc != MISAT_OK) return fail(rc, "misat_norm_rotary_backward");
   PyObject* o = a[5];
