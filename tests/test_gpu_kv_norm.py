@@ -336,17 +336,20 @@ def test_refused_arguments():
     long = rand((2, 1, 264), BF16, 1)
     with pytest.raises(m.MisatError):
         rope.norm_rotate(long, pos[:2], m.HeadNorm(torch.ones(264, device="cuda")))
-    # gradients' scratch
+    # gradients' scratch: of a call with so many tokens that it needs some
+    T = 4000
+    x, dy, w, pos = made(T, 2, 32, BF16, BF16, False)
     n = m.misat_head_norm(w.data_ptr(), 0, m.BF16, 1e-6, 0.0)
     size = ctypes.c_int64()
-    assert m._lib.misat_norm_rotary_work(rope._h, ctypes.byref(n), m.BF16, 4, 2, 32, ctypes.byref(size)) == 0
-    work = torch.empty(size.value + 16, dtype=torch.uint8, device="cuda")
+    assert m._lib.misat_norm_rotary_work(rope._h, ctypes.byref(n), m.BF16, T, 2, 32, ctypes.byref(size)) == 0
+    assert size.value > 0
+    work, dx, dw = torch.empty(size.value + 16, dtype=torch.uint8, device="cuda"), torch.empty_like(x), torch.empty_like(w)
     st = torch.cuda.current_stream().cuda_stream
 
-    def back(work, size, dw=w.clone().data_ptr(), norm=n):
-        return m._lib.misat_norm_rotary_backward(rope._h, ctypes.byref(norm), m.BF16, 4, 2, 32, x.data_ptr(), 64, 32,
-                                                 dy.data_ptr(), 64, 32, pos.data_ptr(), x.clone().data_ptr(), 64, 32, dw,
-                                                 32, work, size, st)
+    def back(work, size, dw=dw.data_ptr(), norm=n):
+        return m._lib.misat_norm_rotary_backward(rope._h, ctypes.byref(norm), m.BF16, T, 2, 32, x.data_ptr(), 64, 32,
+                                                 dy.data_ptr(), 64, 32, pos.data_ptr(), dx.data_ptr(), 64, 32, dw, 32, work,
+                                                 size, st)
 
     assert back(work.data_ptr(), size.value) == 0
     assert back(None, size.value) == m.ERR_INVALID_ARG
@@ -411,3 +414,20 @@ def test_sizes_of_values(half, size):
     m = misat()
     x, dy, w, pos = made(50, 4, 64, BF16, F32, False)
     within(m.Rope(64, layout=m.ROPE_HALF if half else m.ROPE_INTERLEAVED), x * size, dy, w, pos, kref.frequencies(64), half)
+
+
+@pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("heads,d", [(1, 128), (7, 64), (40, 128), (64, 96), (200, 128), (3, 13)])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 31, 63, 64, 65, 130, 500])
+def test_gradients_of_few_tokens(n, heads, d, each):
+    """Around the numbers of tokens up to which one cluster of CTAs adds the weight's gradient."""
+    m = misat()
+    x, dy, w, pos = made(n, heads, d, BF16, F32 if n % 2 else BF16, each)
+    rot = d // 4 * 2
+    rope = m.Rope(rot, layout=m.ROPE_HALF if n % 3 else m.ROPE_INTERLEAVED)
+    within(rope, x, dy, w, pos, kref.frequencies(rot), bool(n % 3))
+    norm = m.HeadNorm(w)
+    first = rope.norm_backward(x, dy, pos, norm)
+    for _ in range(3):
+        again = rope.norm_backward(x, dy, pos, norm)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
