@@ -511,3 +511,51 @@ def test_objects_of_another_kind_are_refused():
         with pytest.raises((ValueError, AttributeError)):
             call()
     pool.sync()
+
+
+def test_a_captured_step_is_replayed():
+    """Blocks, plan, append, attention and what is kept in one graph, whose lengths and tables go on from replay to replay."""
+    m = misat()
+    n, nodes, hq, hkv, d, dtype = 9, 6, 8, 2, 64, BF16
+    rope = m.Rope(d, layout=m.ROPE_INTERLEAVED)
+    norm = m.HeadNorm(rand((d,), BF16, 1) + 1)
+    x = rand((n * nodes, hq + 2 * hkv, d), dtype, 2)
+    par, path, many = ints(parents_of([nodes] * n, 3)), ints([[0, 2, 5]] * n), ints([b % 4 for b in range(n)])
+    new = ints([nodes] * n)
+
+    class Side:
+        def __init__(self):
+            self.kb, self.vb = (torch.zeros((200, hkv, 16, d), dtype=dtype, device="cuda") for _ in range(2))
+            self.pool = m.KvPool(self.kb, self.vb, n_q_heads=hq, rope=rope)
+            self.tables = m.KvTables(self.pool, torch.zeros((n, 15), dtype=torch.int32, device="cuda"),
+                                     torch.arange(200, dtype=torch.int32, device="cuda"))
+            self.state, self.lens = self.tables.initial(200), ints(list(range(n)))
+            first = self.tables.step(self.state, self.lens, ints([0] * n), n_tokens=n * (n - 1) // 2, max_q=n - 1, out=self.state)
+            self.pool.append(first, *(rand((first.n_tokens, hkv, d), dtype, 4) for _ in range(2)))
+
+        def step(self):
+            batch = self.tables.step(self.state, new, self.lens, n_tokens=n * nodes, max_q=nodes, out=self.state)
+            tree = self.pool.tree(batch, par)
+            q = self.pool.append(batch, x[:, hq:hq + hkv], x[:, hq + hkv:], q=x[:, :hq], q_norm=norm, k_norm=norm, tree=tree)
+            out, lse = self.pool.attend(batch, q, return_lse=True, tree=tree)
+            self.pool.keep(batch, path, many, out=self.lens)
+            return out, lse, batch.slots
+
+    eager, graphed = Side(), Side()
+    s = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        got = graphed.step()
+    for turn in range(25):
+        want = eager.step()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), turn
+        assert torch.equal(eager.lens, graphed.lens) and torch.equal(eager.state, graphed.state)
+        assert torch.equal(eager.tables.block_table, graphed.tables.block_table)
+        assert torch.equal(eager.kb, graphed.kb) and torch.equal(eager.vb, graphed.vb)
+    eager.pool.sync()
+    graphed.pool.sync()
+    assert eager.lens.tolist() == [b + 25 * (b % 4) for b in range(n)]
