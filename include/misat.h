@@ -714,7 +714,7 @@ int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_
  * a line of the tree these are the positions that the keys were rotated to.  The slots behind hold
  * what they held.  A path that does not rise or leaves the tree is a sticky error: that sequence is
  * left as it was.  No two sequences of a batch may share the blocks of their new tokens.
- * kv_len_out must not be kv_len.  [async]
+ * kv_len_out must not overlap kv_len, q_off, n_keep or path.  [async]
  * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES), CUDA; INVALID_ARG later. */
 int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path, int64_t path_stride,
                   const int32_t* n_keep, int32_t* kv_len_out, void* cuda_stream);

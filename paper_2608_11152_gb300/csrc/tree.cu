@@ -168,7 +168,15 @@ int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path
   if (!batch_ok(kv, batch) || batch->max_q > MISAT_KV_TREE_NODES || path_stride < 0) return MISAT_ERR_INVALID_ARG;
   if (batch->n == 0) return MISAT_OK;
   if (!batch->q_off || !batch->kv_len || (!batch->block_table && batch->table_stride > 0) ||
-      (!path && path_stride > 0) || !n_keep || !kv_len_out || kv_len_out == batch->kv_len || !on_device(kv->device))
+      (!path && path_stride > 0) || !n_keep || !kv_len_out || !on_device(kv->device))
+    return MISAT_ERR_INVALID_ARG;
+  // Several CTAs read what there is of a sequence, and one of them writes its length.
+  const auto apart = [&](const int32_t* p, int64_t count) {
+    const auto at = reinterpret_cast<uintptr_t>(p), out = reinterpret_cast<uintptr_t>(kv_len_out);
+    return at + 4 * (uint64_t)count <= out || out + 4 * (uint64_t)batch->n <= at;
+  };
+  const int64_t n = batch->n;
+  if (!apart(batch->kv_len, n) || !apart(batch->q_off, n + 1) || !apart(n_keep, n) || !apart(path, n * path_stride))
     return MISAT_ERR_INVALID_ARG;
   KeepArgs a{};
   a.b = batch_view(batch);

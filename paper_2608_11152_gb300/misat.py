@@ -818,8 +818,8 @@ class KvPool:
 
     def keep(self, batch, path, n_keep, out=None):
         """Move the keys and values of the accepted nodes of each tree, path[b, :n_keep[b]] (int32, rising), to the
-        slots behind the tokens before the tree; returns the lengths after it (int32 [n]; out must not be the
-        batch's kv_len)."""
+        slots behind the tokens before the tree; returns the lengths after it (int32 [n]; out must not
+        overlap the other tensors)."""
         return self._keep(self._state, batch._state, path, n_keep, out)
 
     def sync(self):

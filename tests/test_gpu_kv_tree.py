@@ -559,3 +559,25 @@ def test_a_captured_step_is_replayed():
     eager.pool.sync()
     graphed.pool.sync()
     assert eager.lens.tolist() == [b + 25 * (b % 4) for b in range(n)]
+
+
+def test_lengths_of_keep_stand_apart():
+    """Written by one of several CTAs that read the lengths, the counts and the paths: none of them may be its result."""
+    m = misat()
+    s = Step([(2, 5), (2, 7), (2, 3)], 2, 64, BF16)
+    pool = s.pool(4)
+    batch = s.batch(pool)
+    flat = ints([1, 0, 2, 0, 1, 2, 0, 0])
+    many, path = flat[:3], flat[3:6].view(3, 1)
+    before = s.kb.clone()
+    for out in (many, flat[1:4], flat[2:5], path[:, 0], flat[5:8], s.q_off[:3], s.q_off[1:], s.kv_len):
+        with pytest.raises(m.MisatError):
+            pool.keep(batch, path, many, out=out)
+    assert flat.tolist() == [1, 0, 2, 0, 1, 2, 0, 0] and torch.equal(s.kb, before)
+    assert s.kv_len.tolist() == [5, 7, 3] and s.q_off.tolist() == [0, 2, 4, 6]
+    path = ints([[0], [0], [0]])
+    # Lengths behind the counts in one tensor, and in front of them.
+    both = ints([0, 0, 0, 1, 0, 1, 0, 0, 0])
+    for out in (both[:3], both[6:]):
+        assert pool.keep(batch, path, both[3:6], out=out).tolist() == [4, 5, 2]
+    pool.sync()
