@@ -812,8 +812,8 @@ HeadWeight weight_of(const misat_head_norm* n) {
 
 bool sizes_ok(const misat_rope* r, const misat_head_norm* norm, int32_t dtype, int32_t n_tokens, int32_t n_heads,
               int32_t head_dim) {
-  return r && dtype >= MISAT_BF16 && dtype <= MISAT_F32 && n_tokens >= 0 && n_tokens <= kMaxTokens && n_heads >= 0 && n_heads <= 65535 &&
-         head_dim >= r->rot && head_dim <= kMaxHead && norm_ok(norm, dtype, n_heads, head_dim);
+  return r && dtype >= MISAT_BF16 && dtype <= MISAT_F32 && n_tokens >= 0 && n_tokens <= kMaxTokens && n_heads >= 0 &&
+         n_heads <= 65535 && head_dim >= r->rot && head_dim <= kMaxHead && norm_ok(norm, dtype, n_heads, head_dim);
 }
 NormArgs rotary_args(const misat_rope* r, const misat_head_norm* norm, int32_t n_tokens, int32_t n_heads,
                      int32_t head_dim) {
@@ -891,7 +891,8 @@ int misat_norm_rotary_backward(const misat_rope* r, const misat_head_norm* norm,
     return MISAT_ERR_INVALID_ARG;
   NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  SumArgs s{static_cast<const float*>(work), dweight, norm->head_stride ? dw_hs : 0, 0, (int32_t)part_size(a), head_dim, norm->dtype};
+  SumArgs s{static_cast<const float*>(work), dweight, norm->head_stride ? dw_hs : 0, 0, (int32_t)part_size(a), head_dim,
+            norm->dtype};
   if (!none) {
     a.x = {const_cast<void*>(x), x_ts, x_hs};
     a.dy = {const_cast<void*>(grad), g_ts, g_hs};
