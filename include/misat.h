@@ -701,9 +701,10 @@ int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_
 
 /* misat_kv_attend of a tree's nodes: a node sees the tokens before the tree (with a window those
  * at positions above its own less the window) and the nodes of its bits.  An absent node gets
- * zeros, and -infinity in lse, whatever its query holds.  kv_len below the new tokens leaves nodes
- * below position zero, which see nothing.  As there, what only some nodes see has to be finite for
- * all of them.  Errors as misat_kv_attend's.  [async] */
+ * zeros, and -infinity in lse; its query, and the key and value in its slot, may be anything.  kv_len
+ * below the new tokens leaves nodes below position zero, which see nothing.  As there, what only some
+ * nodes see has to be finite for all of them, and the weights are rounded to the pool's dtype for the
+ * product with v.  Errors as misat_kv_attend's.  [async] */
 int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_kv_draft* draft, const void* q,
                          int64_t q_token_stride, int64_t q_head_stride, void* out, int64_t out_token_stride,
                          int64_t out_head_stride, float* lse, void* cuda_stream);

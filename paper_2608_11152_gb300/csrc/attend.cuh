@@ -83,9 +83,10 @@ __device__ __forceinline__ uint32_t col_o(int st) { return 256 + st * DP; }
 template <bool APART>
 __device__ __forceinline__ uint32_t col_p(int st) { return APART ? 384 + st * 64 : col_s(st); }
 
-template <class T, int DP, bool APART>
+template <class T, int DP, bool TREE>
 struct Issuer {
   using L = Layout<DP>;
+  static constexpr bool APART = TREE && DP == 64;
   static constexpr bool kBf16 = std::is_same_v<T, __nv_bfloat16>;
   const AttendArgs& a;
   Control* c;
@@ -142,8 +143,36 @@ struct Issuer {
     };
     if (from > 0) zero(from / kBlockTokens * kBlockTokens, from);
     if (to < kKeys) zero(to, (to + kBlockTokens - 1) / kBlockTokens * kBlockTokens);
-    fence_async_shared();
-    __syncwarp();
+  }
+  // (TREE) The word that holds a node's own bit, of the nodes of key block j, four a lane; keys of no node count as
+  // there.  The bit's place in its word is the same for a lane's four.
+  __device__ __forceinline__ void own_words(const Segment& g, int j, uint32_t (&w)[4]) const {
+    const int before = g.s.len - g.s.n;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int key = j * kKeys + q * 32 + (int)(threadIdx.x & 31), i = key - before;
+      w[q] = i >= 0 && key < g.k.to ? __ldcg(a.bits + (int64_t)(g.s.begin + i) * a.words + (i >> 5)) : ~0u;
+    }
+  }
+  __device__ __forceinline__ bool absent(const Segment& g, const uint32_t (&w)[4], uint32_t (&gone)[4]) const {
+    const int bit = ((int)(threadIdx.x & 31) - (g.s.len - g.s.n)) & 31;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) gone[q] = __ballot_sync(0xffffffffu, !(w[q] >> bit & 1));
+    return (gone[0] | gone[1] | gone[2] | gone[3]) != 0;
+  }
+  // Slots of nodes that are not there lie between keys that are seen, and no one sees them: as above, their values may
+  // be anything.
+  __device__ __forceinline__ void clear_absent(int stage, const uint32_t (&gone)[4]) {
+    char* v = smem + L::kKv + stage * L::kStage;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (gone[q] == 0) continue;
+      for (int i = threadIdx.x & 31; i < 32 * (DP / 8); i += 32) {
+        const int row = i / (DP / 8), ch = i % (DP / 8);
+        if (gone[q] >> row & 1)
+          *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + (q * 32 + row) * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+    }
   }
   // Step x, by one thread.  The ring's next tile is the values of step x, then the keys of step x + 2;
   // in a pair the second stream uses the first one's.
@@ -229,22 +258,43 @@ struct Issuer {
       const Segment g = *p;
       const int n = g.steps();
       if (n == 0) continue;
+      // The first key block that reaches into the tree; its nodes' words are on their way meanwhile.
+      const int tree = TREE ? max(g.s.len - g.s.n, 0) / kKeys : 0;
+      uint32_t own[4], gone[4];
+      int known = -1;
+      bool any_gone = false;
+      if constexpr (TREE) own_words(g, max(tree, g.j0), own);
       for (int st = 0; st < (g.both() ? 2 : 1); ++st) {
         const int slot = qs.slot(g, st);
         if (!mbar_wait(smem_u32(&c->q_full[slot]), qs.phase(slot), &c->abort)) return;
       }
       tc_fence_after();
       // Steps in runs: one thread waits and issues without a vote or an election in between, which left the
-      // tensor cores idle; the warp meets where values have to be cleared, at the ends of the item's keys.
-      const int slot0 = qs.slot(g, 0), slot1 = qs.slot(g, 1), by = g.pair ? 2 : 1;
-      const int tail = ragged(g, g.j0 + g.nb - 1) ? n - (g.both() ? 2 : 1) : n;
+      // tensor cores idle; the warp meets where values may have to be cleared, at the ends of the item's keys and
+      // in the tree.
+      const int slot0 = qs.slot(g, 0), slot1 = qs.slot(g, 1), by = g.pair ? 2 : 1, each = g.both() ? 2 : 1;
+      int tail = ragged(g, g.j0 + g.nb - 1) ? n - each : n;
+      if (TREE) tail = min(tail, max(tree - g.j0, 0) * each);
 #pragma unroll 1
       for (int x = -2; x < n;) {
         int end = x < 0 ? 0 : x < tail ? tail : n;
-        if (x >= 0 && ragged(g, g.block(x))) {
-          end = x + by;
+        const int j = g.block(max(x, 0));
+        const bool in_tree = TREE && x >= 0 && j >= tree, ends = x >= 0 && ragged(g, j);
+        if constexpr (TREE) {
+          if (in_tree && j != known) {
+            any_gone = absent(g, own, gone);
+            own_words(g, j + 1, own);
+            known = j;
+          }
+        }
+        if (ends || in_tree) end = x + by;
+        if (ends || (in_tree && any_gone)) {
           if (!mbar_wait(MISAT_BAR(kv_full, ring.at), ring.phase, &c->abort)) return;
-          clear(g, ring.at, g.block(x));
+          if (ends) clear(g, ring.at, j);
+          if constexpr (TREE)
+            if (in_tree && any_gone) clear_absent(ring.at, gone);
+          fence_async_shared();
+          __syncwarp();
         }
         int state = 0;
         uint32_t lead;
@@ -810,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ld.run();
         if (*(volatile int*)&c->abort) ld.drain();
       } else if (warp == 9) {
-        Issuer<T, DP, TREE && DP == 64> is{a, c, smem, smem_u32(smem), smem_u32(smem) + L::kCtl, tmem};
+        Issuer<T, DP, TREE> is{a, c, smem, smem_u32(smem), smem_u32(smem) + L::kCtl, tmem};
         is.run();
         is.drain();
       } else if (warp == 8) {

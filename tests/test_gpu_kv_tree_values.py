@@ -1,0 +1,124 @@
+"""Trees with nodes that are not there, whose queries, keys and values hold anything."""
+
+import math
+import random
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests import kv_reference as kref  # noqa: E402
+from tests import kv_step_reference as ref  # noqa: E402
+from tests.test_gpu_kv import BF16, F16, Step, misat, rand  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def parents_with_gaps(new, seed, absent):
+    """Absent nodes anywhere in a tree, with nodes that are there behind them."""
+    r = random.Random(seed)
+    out = []
+    for n in new:
+        there = []
+        for i in range(n):
+            if r.random() < absent:
+                out.append(ref.ABSENT)
+            else:
+                out.append(r.choice(there + [ref.ROOT]))
+                there.append(i)
+    return out
+
+
+def slots_of(s):
+    """Block and place of each new token."""
+    seq = [b for b, n in enumerate(s.new) for _ in range(n)]
+    pos = [L - n + i for n, L in zip(s.new, s.lens) for i in range(n)]
+    seq, pos = torch.tensor(seq, device="cuda"), torch.tensor(pos, device="cuda")
+    return s.table[seq, pos // 16].long(), pos % 16
+
+
+def check(seqs, hq, hkv, d, dtype, absent, window=0, seed=1, fill=math.nan):
+    """The slots of absent nodes hold `fill`: results are those of the nodes that are there alone."""
+    s = Step(seqs, hkv, d, dtype, seed=seed)
+    parents = parents_with_gaps(s.new, seed, absent)
+    gone = torch.tensor(parents, device="cuda") == ref.ABSENT
+    blk, at = slots_of(s)
+    clean_k, clean_v = s.kb.clone(), s.vb.clone()
+    for x in (clean_k, clean_v):  # (for the reference, in which a product with zero counts)
+        x[blk[gone], :, at[gone]] = 0
+    for x in (s.kb, s.vb):
+        x[blk[gone], :, at[gone]] = fill
+    s.poison()
+    pool = s.pool(hq)
+    batch = s.batch(pool)
+    q = rand((s.T, hq, d), dtype, seed + 7, 1.5)
+    q[gone] = fill
+    tree = pool.tree(batch, ints(parents), window=window)
+    out, lse = pool.attend(batch, q, return_lse=True, tree=tree)
+    pool.sync()
+    depth, sees = ref.tree(s.new, parents, window)
+    o, ot, l, lt = ref.attend(q, clean_k, clean_v, s.new, s.lens, s.table, depth, sees, window)
+    kref.assert_within("out", out, o, ot)
+    kref.assert_within("lse", lse, l, lt)
+    assert (out[gone] == 0).all() and (lse[gone] == -math.inf).all()
+
+
+@pytest.mark.parametrize("fill", [math.nan, math.inf])
+@pytest.mark.parametrize("absent", [0.2, 0.9])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(4, 4, 64, BF16), (2, 2, 64, F16), (8, 1, 128, BF16), (28, 4, 64, F16), (6, 2, 72, F16),
+                                            (32, 2, 128, BF16), (3, 1, 8, BF16)])
+def test_slots_of_absent_nodes_hold_anything(hq, hkv, d, dtype, absent, fill):
+    """Trees that begin and end anywhere in a block of keys, one of them behind nothing."""
+    check([(1, 1), (5, 5), (12, 140), (33, 33), (32, 128), (17, 128 + 17), (3, 700), (64, 300), (0, 9), (127, 255)], hq, hkv, d,
+          dtype, absent, fill=fill)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(2, 1, 64), (8, 1, 128), (2, 2, 128)])
+@pytest.mark.parametrize("n,L", [(128, 256), (129, 130), (130, 500), (257, 257), (600, 641), (1024, 1100)])
+def test_absent_nodes_of_trees_longer_than_a_block(n, L, hq, hkv, d):
+    for absent in (0.01, 0.5, 0.99):
+        check([(n, L)], hq, hkv, d, BF16, absent, seed=n)
+
+
+@pytest.mark.parametrize("window", [1, 4, 100])
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (8, 1, 128)])
+def test_absent_nodes_under_a_window(hq, hkv, d, window):
+    check([(8, 8), (16, 40), (40, 41), (130, 700), (1, 1), (5, 300)], hq, hkv, d, BF16, 0.4, window, seed=4)
+
+
+def test_absent_nodes_behind_long_histories():
+    """Items in parts, of which some have none of the tree, and many sequences."""
+    check([(20, 30000)], 8, 1, 128, BF16, 0.5)
+    check([(250, 3250), (3, 50)], 8, 8, 64, F16, 0.5, seed=3)
+    r = random.Random(2)
+    seqs = [(r.choice([0, 1, 4, 16, 33]), 0) for _ in range(300)]
+    check([(n, n + r.choice([0, 1, 15, 130, r.randint(0, 900)])) for n, _ in seqs], 4, 1, 64, BF16, 0.3)
+    check([(n, n + r.choice([0, 1, 15, 130, r.randint(0, 900)])) for n, _ in seqs], 4, 2, 128, F16, 0.3)
+
+
+@pytest.mark.parametrize("normed", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_padding_rows_of_a_step_of_fixed_shape(d, normed):
+    """Append and attention of rows of which the absent ones hold NaN, and of the same with zeros there: the same bits."""
+    m = misat()
+    s = Step([(12, 40), (12, 12), (12, 300), (12, 139)], 2, d, BF16)
+    pool = s.pool(8, rope=m.Rope(d))
+    parents = parents_with_gaps(s.new, 5, 0.4)
+    gone = torch.tensor(parents, device="cuda") == ref.ABSENT
+    norm = m.HeadNorm(rand((d,), BF16, 2) + 1) if normed else None
+    batch = s.batch(pool)
+    tree = pool.tree(batch, ints(parents))
+    x = rand((s.T, 12, d), BF16, 3)
+    got = []
+    for fill in (0.0, math.nan):
+        x[gone] = fill
+        q = pool.append(batch, x[:, 8:10], x[:, 10:], q=x[:, :8], q_norm=norm, k_norm=norm, tree=tree)
+        got.append(pool.attend(batch, q, tree=tree, return_lse=True))
+    pool.sync()
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and not torch.isnan(a).any()
+    assert (got[0][0][gone] == 0).all() and not (got[0][0][~gone] == 0).all()
