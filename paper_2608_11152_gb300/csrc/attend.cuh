@@ -154,23 +154,25 @@ struct Issuer {
       w[q] = i >= 0 && key < g.k.to ? __ldcg(a.bits + (int64_t)(g.s.begin + i) * a.words + (i >> 5)) : ~0u;
     }
   }
-  __device__ __forceinline__ bool absent(const Segment& g, const uint32_t (&w)[4], uint32_t (&gone)[4]) const {
+  // A bit for each of a lane's four that is not there.
+  __device__ __forceinline__ uint32_t absent(const Segment& g, const uint32_t (&w)[4]) const {
     const int bit = ((int)(threadIdx.x & 31) - (g.s.len - g.s.n)) & 31;
+    uint32_t gone = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) gone[q] = __ballot_sync(0xffffffffu, !(w[q] >> bit & 1));
-    return (gone[0] | gone[1] | gone[2] | gone[3]) != 0;
+    for (int q = 0; q < 4; ++q) gone |= (~w[q] >> bit & 1) << q;
+    return gone;
   }
   // Slots of nodes that are not there lie between keys that are seen, and no one sees them: as above, their values may
   // be anything.
-  __device__ __forceinline__ void clear_absent(int stage, const uint32_t (&gone)[4]) {
+  __device__ __forceinline__ void clear_absent(int stage, uint32_t gone) {
     char* v = smem + L::kKv + stage * L::kStage;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (gone[q] == 0) continue;
-      for (int i = threadIdx.x & 31; i < 32 * (DP / 8); i += 32) {
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q, v += 32 * 128) {
+      const uint32_t rows = __ballot_sync(0xffffffffu, gone >> q & 1);
+#pragma unroll 1
+      for (int i = threadIdx.x & 31; rows && i < 32 * (DP / 8); i += 32) {
         const int row = i / (DP / 8), ch = i % (DP / 8);
-        if (gone[q] >> row & 1)
-          *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + (q * 32 + row) * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+        if (rows >> row & 1) *reinterpret_cast<uint4*>(v + (ch / 8) * L::kHalf + row * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
       }
     }
   }
@@ -260,9 +262,8 @@ struct Issuer {
       if (n == 0) continue;
       // The first key block that reaches into the tree; its nodes' words are on their way meanwhile.
       const int tree = TREE ? max(g.s.len - g.s.n, 0) / kKeys : 0;
-      uint32_t own[4], gone[4];
+      uint32_t own[4], gone = 0;
       int known = -1;
-      bool any_gone = false;
       if constexpr (TREE) own_words(g, max(tree, g.j0), own);
       for (int st = 0; st < (g.both() ? 2 : 1); ++st) {
         const int slot = qs.slot(g, st);
@@ -279,20 +280,25 @@ struct Issuer {
       for (int x = -2; x < n;) {
         int end = x < 0 ? 0 : x < tail ? tail : n;
         const int j = g.block(max(x, 0));
-        const bool in_tree = TREE && x >= 0 && j >= tree, ends = x >= 0 && ragged(g, j);
+        const bool ends = x >= 0 && ragged(g, j);
+        bool holes = false;
         if constexpr (TREE) {
-          if (in_tree && j != known) {
-            any_gone = absent(g, own, gone);
-            own_words(g, j + 1, own);
-            known = j;
+          if (x >= 0 && j >= tree) {
+            if (j != known) {
+              gone = absent(g, own);
+              own_words(g, j + 1, own);
+              known = j;
+            }
+            holes = __any_sync(0xffffffffu, gone != 0);
+            end = (j + 1 - g.j0) * each;
           }
         }
-        if (ends || in_tree) end = x + by;
-        if (ends || (in_tree && any_gone)) {
+        if (ends || holes) {
+          end = x + by;
           if (!mbar_wait(MISAT_BAR(kv_full, ring.at), ring.phase, &c->abort)) return;
           if (ends) clear(g, ring.at, j);
           if constexpr (TREE)
-            if (in_tree && any_gone) clear_absent(ring.at, gone);
+            if (holes) clear_absent(ring.at, gone);
           fence_async_shared();
           __syncwarp();
         }
