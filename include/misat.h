@@ -685,7 +685,9 @@ typedef struct misat_kv_draft {
 } misat_kv_draft;
 /* The plan of a step's trees: depth and bits as above, for misat_kv_append_norm and
  * misat_kv_attend_tree of every layer.  An absent node has depth 0 and no bits.  A number that is no
- * earlier node's that is there is a sticky error, and the node counts as absent.  [async]
+ * earlier node's that is there is a sticky error, and the node counts as absent; so do the tokens of a
+ * sequence whose offsets or length are malformed (kv_len below its new tokens among them), and those
+ * of no sequence.  [async]
  * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES, words), CUDA; INVALID_ARG later. */
 int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* parents, int32_t window, int32_t* depth,
                   uint32_t* bits, int32_t words, void* cuda_stream);

@@ -33,25 +33,43 @@ struct TreeArgs {
   int32_t* err;
 };
 
-// New tokens of sequence b and its place in the batch; n = 0 where it is malformed.
+// New tokens of sequence b and its place in the batch; n = 0 where it is malformed (its tokens are then [begin, end),
+// wherever that leads).
 struct Range {
-  int begin, n, len;
+  int begin, n, len, end;
 };
 __device__ __forceinline__ Range load_range(const KvBatch& k, int b, int32_t* err) {
   const int begin = __ldcg(k.q_off + b), end = __ldcg(k.q_off + b + 1), len = __ldcg(k.kv_len + b);
   const bool ok = begin >= 0 && end >= begin && end <= k.n_tokens && end - begin <= k.max_q && len >= end - begin &&
                   len <= kMaxLen && len <= k.stride * kBlockTokens;
   if (!ok && threadIdx.x == 0) set_error(err, MISAT_ERR_INVALID_ARG);
-  return {begin, ok ? end - begin : 0, len};
+  return {begin, ok ? end - begin : 0, len, end};
+}
+
+// Tokens [from, to) of the batch, as far as it has them: nodes that are not there.
+__device__ __forceinline__ void put_absent(const TreeArgs& a, int from, int to) {
+  to = min(to, a.b.n_tokens);
+  for (int64_t t = max(from, 0) + (int64_t)threadIdx.x; t < to; t += blockDim.x) {
+    a.depth[t] = 0;
+    for (int w = 0; w < a.words; ++w) a.bits[t * a.words + w] = 0;
+  }
 }
 
 __global__ void __launch_bounds__(kMaxNodes) k_tree(const __grid_constant__ TreeArgs a) {
   __shared__ int32_t up[MISAT_KV_TREE_NODES];
   chain_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0 &&
-      (__ldcg(a.b.q_off) != 0 || __ldcg(a.b.q_off + a.b.n) != a.b.n_tokens))
-    set_error(a.err, MISAT_ERR_INVALID_ARG);
+  // Every token of the batch gets a depth and bits: it is before the first sequence, behind the last, or between two
+  // neighbouring offsets, and absent where these are malformed.
+  if (blockIdx.x == 0) {
+    const int first = __ldcg(a.b.q_off), last = __ldcg(a.b.q_off + a.b.n);
+    if (first != 0 || last != a.b.n_tokens) {
+      if (threadIdx.x == 0) set_error(a.err, MISAT_ERR_INVALID_ARG);
+      put_absent(a, 0, first);
+      put_absent(a, last, a.b.n_tokens);
+    }
+  }
   const Range s = load_range(a.b, blockIdx.x, a.err);
+  if (s.n == 0) put_absent(a, s.begin, s.end);
   for (int i = (int)threadIdx.x; i < s.n; i += blockDim.x) {
     const int p = __ldcg(a.parent + s.begin + i);
     up[i] = p < i && p >= kAbsent ? p : kAbsent - 1;  // (neither a parent nor one of the two marks)

@@ -1,4 +1,4 @@
-"""Trees with nodes that are not there, whose queries, keys and values hold anything."""
+"""Trees with nodes that are not there, whose queries, keys and values hold anything, and plans of malformed batches."""
 
 import math
 import random
@@ -122,3 +122,64 @@ def test_padding_rows_of_a_step_of_fixed_shape(d, normed):
     for a, b in zip(*got):
         assert torch.equal(a, b) and not torch.isnan(a).any()
     assert (got[0][0][gone] == 0).all() and not (got[0][0][~gone] == 0).all()
+
+
+# ---- the plan of malformed batches ----
+
+BATCHES = {  # q_off, kv_len, and which node of its sequence each token is (None: of none)
+    "length below the new tokens": ([0, 3, 3, 5], [2, 4, 9], [None, None, None, 0, 1]),
+    "negative length": ([0, 3, 3, 5], [7, 4, -1], [0, 1, 2, None, None]),
+    "length past the table": ([0, 3, 3, 5], [7, 4, 2 ** 31 - 1], [0, 1, 2, None, None]),
+    "first offset": ([1, 3, 3, 5], [7, 4, 9], [None, 0, 1, 0, 1]),
+    "last offset": ([0, 3, 3, 4], [7, 4, 9], [0, 1, 2, 0, None]),
+    "no tokens": ([0, 0, 0, 0], [7, 4, 9], [None] * 5),
+    "offset past the batch": ([0, 3, 3, 9], [7, 4, 9], [0, 1, 2, None, None]),
+    "negative offset": ([-4, 3, 3, 5], [7, 4, 9], [None, None, None, 0, 1]),
+    "more than max_q": ([0, 0, 5, 5], [7, 9, 9], [None] * 5),
+}
+
+
+@pytest.mark.parametrize("words", [1, 2])
+@pytest.mark.parametrize("what", BATCHES)
+def test_plan_of_a_malformed_batch_is_written_whole(what, words):
+    """Nodes without a sequence are absent, not what their memory held before."""
+    m = misat()
+    q_off, kv_len, node = BATCHES[what]
+    s = Step([(3, 7), (0, 4), (2, 9)], 1, 64, BF16)
+    pool = s.pool(1)
+    batch = pool.batch(ints(q_off), ints(kv_len), s.table, n_tokens=5, max_q=4 if words == 1 else 33)
+    if what == "more than max_q" and words == 2:
+        batch = pool.batch(ints([0, 0, 34, 34]), ints([7, 99, 99]), torch.zeros((3, 9), dtype=torch.int32, device="cuda"),
+                           n_tokens=34, max_q=33)
+        node = [None] * 34
+    T = len(node)
+    parents = ints([ref.ROOT] * T)
+    depth = torch.full((T,), 77, dtype=torch.int32, device="cuda")
+    bits = torch.full((T, words), -1, dtype=torch.int32, device="cuda")
+    assert m._lib.misat_kv_tree(pool._h, batch._ref, parents.data_ptr(), 0, depth.data_ptr(), bits.data_ptr(), words,
+                                torch.cuda.current_stream().cuda_stream) == 0
+    with pytest.raises(m.MisatError) as e:
+        pool.sync()
+    assert e.value.code == m.ERR_INVALID_ARG
+    assert depth.tolist() == [0] * T
+    assert bits.tolist() == [[0 if i is None else 1 << i] + [0] * (words - 1) for i in node]
+
+
+def test_attention_by_the_plan_of_a_malformed_batch():
+    """A sequence that the plan refuses, though the attention takes its length, has no nodes."""
+    m = misat()
+    s = Step([(3, 7), (0, 4), (2, 9)], 1, 64, BF16)
+    pool = s.pool(2)
+    batch = s.batch(pool)
+    q = rand((5, 2, 64), BF16, 1)
+    want = pool.attend(batch, q, tree=pool.tree(batch, ints([-1] * 5)))
+    s.kv_len[0] = 2
+    junk = [torch.full((10,), -1, dtype=torch.int32, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk  # (the plan's memory comes from here)
+    tree = pool.tree(batch, ints([-1] * 5))
+    with pytest.raises(m.MisatError):
+        pool.sync()
+    out, lse = pool.attend(batch, q, return_lse=True, tree=tree)
+    pool.sync()
+    assert (out[:3] == 0).all() and (lse[:3] == -math.inf).all() and torch.equal(out[3:], want[3:])
