@@ -597,16 +597,20 @@ int misat_kv_attend(misat_kv* kv, const misat_kv_batch* batch, const void* q, in
  *   len = kv_len + new_tokens,  need = ceil(len / 16)
  * A row with fewer than `need` blocks gets the missing ones from the front of a ring of free
  * blocks; one with more gives those from max(need, shared) on to the ring's end (its first
- * `shared` blocks are another's, a prefix's, and are dropped without being given back).  Blocks
+ * `shared` blocks are another's, a prefix's, and are dropped without being given back).  `shared`
+ * says nothing else: new tokens go into the row's blocks, shared or not, so a sequence whose tokens
+ * end inside a shared block gets a block of its own first.  It is at most the number of blocks in the
+ * row, so the caller lowers it where a step leaves the row fewer; a row that holds no block and gets
+ * none (a finished sequence) may keep its number until the row is used again.  Blocks
  * are taken and given in the order of the sequences and of the places in a row, so the result
  * does not depend on timing; blocks given in a step can be taken from the next one on.
  * state: [n] blocks in each row, then the ring's front (a place in [0, ring_size)) and the number
  * of free blocks from there on.
  * A step that cannot be made changes nothing, but for q_off (zeros), positions and slots (-1) and
  * copies of what is not changed (state_out, kv_len_out): fewer free blocks than it takes (OOM),
- * more given than the ring has room for, a negative or longer count than allowed, a row with
- * fewer blocks than its kv_len tokens fill or too short for the step, new tokens whose sum is not
- * n_tokens (INVALID_ARG; all sticky, from misat_kv_sync). */
+ * more given than the ring has room for, a negative or longer count than allowed (`shared` above the
+ * row's blocks among them), a row with fewer blocks than its kv_len tokens fill or too short for
+ * the step, new tokens whose sum is not n_tokens (INVALID_ARG; all sticky, from misat_kv_sync). */
 typedef struct misat_kv_step {
   int32_t n;                 /* sequences, 0..max_batch of the pool */
   int32_t n_tokens;          /* sum of new_tokens, below 2^31 - 4096 */
@@ -616,7 +620,7 @@ typedef struct misat_kv_step {
   int32_t ring_size;         /* >= 1; as many as there are blocks always suffice */
   const int32_t* new_tokens; /* device [n], >= 0 */
   const int32_t* kv_len;     /* [n] tokens before the step (after it at most 2^30) */
-  const int32_t* shared;     /* [n] or NULL (none) */
+  const int32_t* shared;     /* [n] or NULL (none); see above */
   const int32_t* state;      /* [n + 2] */
   int32_t* block_table;      /* [n][table_stride], read and written */
   int32_t* ring;             /* [ring_size], read and written */

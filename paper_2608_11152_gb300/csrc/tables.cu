@@ -83,10 +83,13 @@ struct Row {
   }
 };
 __device__ __forceinline__ Row row_of(const TableArgs& a, int fresh, int before, int held, int shared) {
-  // A row holds blocks for the tokens that are there, and has room for those to come.
+  // A row holds blocks for the tokens that are there, and has room for those to come.  One without blocks that gets none (a
+  // finished sequence) shares none, whatever its number still says; where it gets some, a number left from before would
+  // keep them from being given back.
   const bool ok = fresh >= 0 && fresh <= a.max_q && before >= 0 && before <= kMaxLen && fresh <= kMaxLen - before &&
                   held >= 0 && held <= a.columns && (int64_t)before <= (int64_t)held * kBlockTokens && shared >= 0 &&
-                  shared <= held && (int64_t)before + fresh <= (int64_t)a.columns * kBlockTokens;
+                  (shared <= held || (held | before | fresh) == 0) &&
+                  (int64_t)before + fresh <= (int64_t)a.columns * kBlockTokens;
   if (!ok) return {0, 0, 0, 0, false};
   Row r{fresh, before + fresh, held, 0, true};
   r.from = max(r.need(), shared);

@@ -711,9 +711,11 @@ class KvTables:
 
     def step(self, state, new, kv_len, *, n_tokens, max_q, shared=None, out=None):
         """The step in which each sequence gets `new` tokens after its `kv_len` (int32 [n]; n_tokens is the sum of new,
-        max_q at least its largest): a KvStep.  shared: leading blocks of a row that are not given back (int32 [n]).
-        out: tensor for the state after the step; may be `state`.  Where it cannot be made (too few free blocks: ERR_OOM;
-        malformed numbers: ERR_INVALID_ARG), nothing changes and pool.sync() raises."""
+        max_q at least its largest): a KvStep.  shared: leading blocks of a row that are not given back (int32 [n]): at
+        most those in the row, where it has or gets any; lower it when a step leaves a row fewer.  New tokens are put into
+        a row's blocks whether they are shared or not.  out: tensor for the state after the step; may be `state`.  Where it
+        cannot be made (too few free blocks: ERR_OOM; malformed numbers: ERR_INVALID_ARG), nothing changes and
+        pool.sync() raises."""
         made = self._step(self.pool._state, self.block_table, self.free, state, new, kv_len, shared, n_tokens, max_q, out)
         return KvStep(self, made, new.shape[0], n_tokens, max_q)
 
