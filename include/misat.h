@@ -630,7 +630,9 @@ typedef struct misat_kv_step {
   int32_t* positions;        /* [n_tokens] position of each new token */
   int64_t* slots;            /* [n_tokens] its slot: 16 block + position % 16 */
 } misat_kv_step;
-/* work: device scratch of MISAT_KV_TABLES_WORK(n) bytes, 16-byte aligned, the call's own until it
+/* No array that is written overlaps another, but that a result of each sequence may be at the address
+ * of an input of each sequence (state_out at state, kv_len_out at kv_len).
+ * work: device scratch of MISAT_KV_TABLES_WORK(n) bytes, 16-byte aligned, the call's own until it
  * is finished.  Writes what a misat_kv_batch of this step takes.  [async]
  * Errors: INVALID_ARG, CUDA; OOM and INVALID_ARG later. */
 #define MISAT_KV_TABLES_WORK(n) (24 * (int64_t)(n) + 64)

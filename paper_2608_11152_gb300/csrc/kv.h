@@ -83,6 +83,16 @@ inline bool aligned16(const Heads& h, int elem) {
   return !h.p || ((reinterpret_cast<uintptr_t>(h.p) | (uintptr_t)(h.ts * elem) | (uintptr_t)(h.hs * elem)) & 15) == 0;
 }
 
+// An array of a call, of `count` elements of `size` bytes.  apart: no byte of one is the other's.
+struct Extent {
+  uintptr_t begin, end;
+  Extent(const void* p, int64_t count, int size = 4)
+      : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (p && count > 0 ? (uint64_t)count * size : 0)) {}
+};
+inline bool apart(const Extent& a, const Extent& b) {
+  return a.begin == a.end || b.begin == b.end || a.end <= b.begin || b.end <= a.begin;
+}
+
 // The handle's device is the current one.
 inline bool on_device(int device) {
   int d = -1;

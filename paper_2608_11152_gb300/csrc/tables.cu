@@ -452,6 +452,20 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
       (s->n_tokens > 0 && (!s->positions || !s->slots)) || !work || (reinterpret_cast<uintptr_t>(work) & 15) ||
       work_bytes < MISAT_KV_TABLES_WORK(s->n) || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
+  // What is written is no other array's, or a later part of the step would read numbers that are not the ones that it was
+  // worked out from, and leave the arrays by them.  A sequence's input is read by the thread that writes its results, before
+  // that: these may be in its place.
+  const int64_t n = s->n, T = s->n_tokens;
+  const Extent in[] = {{s->new_tokens, n}, {s->kv_len, n}, {s->shared, n}, {s->state, n + 2}};
+  const Extent out[] = {{s->state_out, n + 2}, {s->q_off, n + 1}, {s->kv_len_out, n},
+                        {s->block_table, n ? (n - 1) * s->table_stride + s->columns : 0}, {s->ring, s->ring_size},
+                        {s->positions, T}, {s->slots, T, 8}, {work, MISAT_KV_TABLES_WORK(n), 1}};
+  for (int i = 0; i < 8; ++i) {
+    for (const Extent& x : in)
+      if (!apart(out[i], x) && !(i < 3 && out[i].begin == x.begin)) return MISAT_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (!apart(out[i], out[j])) return MISAT_ERR_INVALID_ARG;
+  }
   TableArgs a{};
   a.n = s->n;
   a.n_tokens = s->n_tokens;
