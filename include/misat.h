@@ -693,7 +693,7 @@ typedef struct misat_kv_draft {
  * misat_kv_attend_tree of every layer.  An absent node has depth 0 and no bits.  A number that is no
  * earlier node's that is there is a sticky error, and the node counts as absent; so do the tokens of a
  * sequence whose offsets or length are malformed (kv_len below its new tokens among them), and those
- * of no sequence.  [async]
+ * of no sequence.  depth and bits overlap neither each other nor what is read.  [async]
  * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES, words), CUDA; INVALID_ARG later. */
 int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* parents, int32_t window, int32_t* depth,
                   uint32_t* bits, int32_t words, void* cuda_stream);
@@ -723,7 +723,7 @@ int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_
  * a line of the tree these are the positions that the keys were rotated to.  The slots behind hold
  * what they held.  A path that does not rise or leaves the tree is a sticky error: that sequence is
  * left as it was.  No two sequences of a batch may share the blocks of their new tokens.
- * kv_len_out must not overlap kv_len, q_off, n_keep or path.  [async]
+ * kv_len_out must not overlap kv_len, q_off, block_table, n_keep or path.  [async]
  * Errors: INVALID_ARG (max_q above MISAT_KV_TREE_NODES), CUDA; INVALID_ARG later. */
 int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path, int64_t path_stride,
                   const int32_t* n_keep, int32_t* kv_len_out, void* cuda_stream);

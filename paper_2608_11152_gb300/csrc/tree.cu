@@ -175,6 +175,12 @@ int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* pare
     return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!parents || !depth || !bits || batch->max_q == 0 || !on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
+  // A CTA reads its sequence's parents and lengths while others write.
+  const int64_t n = batch->n, T = batch->n_tokens;
+  const Extent d(depth, T), m(bits, T * words);
+  if (!apart(d, m)) return MISAT_ERR_INVALID_ARG;
+  for (const Extent& x : {Extent(batch->kv_len, n), Extent(batch->q_off, n + 1), Extent(parents, T)})
+    if (!apart(d, x) || !apart(m, x)) return MISAT_ERR_INVALID_ARG;
   const TreeArgs a{batch_view(batch), parents, depth, bits, words, window, kv->err};
   const int threads = std::min((batch->max_q + 31) / 32 * 32, kMaxNodes);
   launch_chained(k_tree, batch->n, threads, 0, static_cast<cudaStream_t>(cuda_stream), a);
@@ -188,14 +194,13 @@ int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path
   if (!batch->q_off || !batch->kv_len || (!batch->block_table && batch->table_stride > 0) ||
       (!path && path_stride > 0) || !n_keep || !kv_len_out || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
-  // Several CTAs read what there is of a sequence, and one of them writes its length.
-  const auto apart = [&](const int32_t* p, int64_t count) {
-    const auto at = reinterpret_cast<uintptr_t>(p), out = reinterpret_cast<uintptr_t>(kv_len_out);
-    return at + 4 * (uint64_t)count <= out || out + 4 * (uint64_t)batch->n <= at;
-  };
-  const int64_t n = batch->n;
-  if (!apart(batch->kv_len, n) || !apart(batch->q_off, n + 1) || !apart(n_keep, n) || !apart(path, n * path_stride))
-    return MISAT_ERR_INVALID_ARG;
+  // Several CTAs read what there is of a sequence, and one of them writes its length.  (The last row of several may be shorter
+  // than their distance.)
+  const int64_t n = batch->n, table = n == 1 ? batch->table_stride : (n - 1) * batch->table_stride + 1;
+  const Extent out(kv_len_out, n);
+  for (const Extent& x : {Extent(batch->kv_len, n), Extent(batch->q_off, n + 1), Extent(batch->block_table, table),
+                          Extent(n_keep, n), Extent(path, n * path_stride)})
+    if (!apart(out, x)) return MISAT_ERR_INVALID_ARG;
   KeepArgs a{};
   a.b = batch_view(batch);
   a.path = path;

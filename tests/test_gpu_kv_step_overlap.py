@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import kv_step_reference as ref  # noqa: E402
-from tests.test_gpu_kv import misat  # noqa: E402
+from tests.test_gpu_kv import BF16, Step, misat  # noqa: E402
 from tests.test_gpu_kv_tables import Tables, ints  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -97,3 +97,39 @@ def test_results_of_sequences_in_place_of_their_inputs(n):
     for got, w in zip((state, q_off, fresh, positions, slots), want):
         assert got.tolist() == w
     assert t.d_table.tolist() == t.table and t.d_ring.tolist() == t.ring
+
+
+def test_lengths_of_keep_are_not_in_the_table():
+    m = misat()
+    for seqs in ([(2, 5), (2, 20), (2, 3)], [(2, 40)]):
+        s = Step(seqs, 2, 64, BF16)
+        pool = s.pool(4)
+        batch = s.batch(pool)
+        n = len(seqs)
+        before = s.table.clone()
+        path, many = ints([[1]] * n), ints([1] * n)
+        for at in range(2):
+            with pytest.raises(m.MisatError):
+                pool.keep(batch, path, many, out=s.table.view(-1)[at:at + n])
+        pool.sync()
+        assert torch.equal(s.table, before)
+
+
+def test_plan_of_a_tree_stands_apart():
+    m = misat()
+    s = Step([(3, 20), (2, 5)], 2, 32, BF16)
+    pool = s.pool(4)
+    batch = s.batch(pool)
+    flat = ints([-1] * 20)
+    p = flat.data_ptr()
+    st = torch.cuda.current_stream().cuda_stream
+    f = m._lib.misat_kv_tree
+    off, lens = s.q_off.data_ptr(), s.kv_len.data_ptr()
+    for depth, bits in ((p, p + 40), (p + 16, p + 40), (p + 40, p), (p + 40, p + 16), (p + 40, p + 40), (p + 20, p + 36),
+                        (off, p + 40), (p + 40, off - 16), (lens - 4, p + 40), (p + 40, lens + 4)):
+        assert f(pool._h, batch._ref, p, 0, depth, bits, 1, st) == m.ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert (flat == -1).all()
+    assert f(pool._h, batch._ref, p, 0, p + 20, p + 40, 1, st) == 0
+    pool.sync()
+    assert flat[5:15].tolist() == [0] * 5 + [1, 2, 4, 1, 2]
