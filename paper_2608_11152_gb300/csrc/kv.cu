@@ -85,7 +85,7 @@ int misat_kv_attend_tree(misat_kv* kv, const misat_kv_batch* batch, const misat_
     return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!draft->depth || !draft->bits || draft->words == 0 ||
-      ((reinterpret_cast<uintptr_t>(draft->depth) | reinterpret_cast<uintptr_t>(draft->bits)) & 3) ||
+      !at_elements(draft->depth) || !at_elements(draft->bits) ||
       !attend_ok(kv, batch, q, q_ts, q_hs, out, o_ts, o_hs, lse))
     return MISAT_ERR_INVALID_ARG;
   launch_attend(kv, batch_view(batch), {const_cast<void*>(q), q_ts, q_hs}, {out, o_ts, o_hs}, lse, draft->window, draft,

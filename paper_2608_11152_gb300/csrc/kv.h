@@ -55,6 +55,9 @@ struct KvBatch {
 
 constexpr int kMaxLen = 1 << 30;  // tokens of a sequence
 
+// An array of numbers begins where its elements may: a caller's address may be any.
+inline bool at_elements(const void* p, int size = 4) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
+
 // Checks of the arguments that both pool calls share.  A tensor's pointer has to be aligned to its
 // elements; strides may be anything non-negative.
 inline bool heads_ok(const void* p, int64_t ts, int64_t hs, int elem) {
@@ -73,6 +76,7 @@ inline bool batch_ok(const misat_kv* kv, const misat_kv_batch* b) {
   if (!kv || !b || b->n < 0 || b->n > kv->max_batch || b->n_tokens < 0 || b->max_q < 0 || b->table_stride < 0)
     return false;
   if (b->n_tokens > 0 && b->n == 0) return false;
+  if (!at_elements(b->q_off) || !at_elements(b->kv_len) || !at_elements(b->block_table)) return false;
   return b->n_tokens == 0 || (b->q_off && b->kv_len && (b->block_table || b->table_stride == 0));
 }
 inline KvBatch batch_view(const misat_kv_batch* b) {

@@ -843,6 +843,7 @@ int misat_norm_rotary(const misat_rope* r, const misat_head_norm* norm, int32_t 
   if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
   const int elem = dtype == MISAT_F32 ? 4 : 2;
   if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions ||
+      !at_elements(positions) ||
       !in_place_ok(x, x_ts, x_hs, out, o_ts, o_hs, n_tokens, n_heads) || !on_device(r->device))
     return MISAT_ERR_INVALID_ARG;
   NormArgs a = rotary_args(r, norm, n_tokens, n_heads, head_dim);
@@ -885,6 +886,7 @@ int misat_norm_rotary_backward(const misat_rope* r, const misat_head_norm* norm,
   const bool none = n_tokens == 0 || n_heads == 0;
   if (!none && (!heads_ok(x, x_ts, x_hs, elem) || !heads_ok(grad, g_ts, g_hs, elem) ||
                 !result_ok(dx, dx_ts, dx_hs, elem, n_tokens, n_heads) || !positions ||
+                !at_elements(positions) ||
                 !in_place_ok(x, x_ts, x_hs, dx, dx_ts, dx_hs, n_tokens, n_heads) ||
                 !in_place_ok(grad, g_ts, g_hs, dx, dx_ts, dx_hs, n_tokens, n_heads) ||
                 (reinterpret_cast<uintptr_t>(work) & 15)))
@@ -922,7 +924,7 @@ int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_
       (k_norm && !norm_ok(k_norm, kv->dtype, kv->hkv, kv->d)))
     return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
-  if (!heads_ok(k, k_ts, k_hs, 2) || !heads_ok(v, v_ts, v_hs, 2) || (draft && !draft->depth))
+  if (!heads_ok(k, k_ts, k_hs, 2) || !heads_ok(v, v_ts, v_hs, 2) || (draft && (!draft->depth || !at_elements(draft->depth))))
     return MISAT_ERR_INVALID_ARG;
   if (q && (!heads_ok(q, q_ts, q_hs, 2) || !result_ok(q_out, qo_ts, qo_hs, 2, batch->n_tokens, kv->hq) ||
             !in_place_ok(q, q_ts, q_hs, q_out, qo_ts, qo_hs, batch->n_tokens, kv->hq)))

@@ -288,7 +288,8 @@ int misat_rotary(const misat_rope* r, int32_t dtype, int32_t n_tokens, int32_t n
     return MISAT_ERR_INVALID_ARG;
   if (n_tokens == 0 || n_heads == 0) return MISAT_OK;
   const int elem = dtype == MISAT_F32 ? 4 : 2;
-  if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions)
+  if (!heads_ok(x, x_ts, x_hs, elem) || !result_ok(out, o_ts, o_hs, elem, n_tokens, n_heads) || !positions ||
+      !at_elements(positions))
     return MISAT_ERR_INVALID_ARG;
   if (!in_place_ok(x, x_ts, x_hs, out, o_ts, o_hs, n_tokens, n_heads)) return MISAT_ERR_INVALID_ARG;
   if (!on_device(r->device)) return MISAT_ERR_INVALID_ARG;

@@ -452,6 +452,10 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
       (s->n_tokens > 0 && (!s->positions || !s->slots)) || !work || (reinterpret_cast<uintptr_t>(work) & 15) ||
       work_bytes < MISAT_KV_TABLES_WORK(s->n) || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
+  for (const void* x : std::initializer_list<const void*>{s->new_tokens, s->kv_len, s->shared, s->state, s->block_table, s->ring,
+                                                          s->state_out, s->q_off, s->kv_len_out, s->positions})
+    if (!at_elements(x)) return MISAT_ERR_INVALID_ARG;
+  if (!at_elements(s->slots, 8)) return MISAT_ERR_INVALID_ARG;
   // What is written is no other array's, or a later part of the step would read numbers that are not the ones that it was
   // worked out from, and leave the arrays by them.  A sequence's input is read by the thread that writes its results, before
   // that: these may be in its place.

@@ -175,6 +175,7 @@ int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* pare
     return MISAT_ERR_INVALID_ARG;
   if (batch->n_tokens == 0) return MISAT_OK;
   if (!parents || !depth || !bits || batch->max_q == 0 || !on_device(kv->device)) return MISAT_ERR_INVALID_ARG;
+  if (!at_elements(parents) || !at_elements(depth) || !at_elements(bits)) return MISAT_ERR_INVALID_ARG;
   // A CTA reads its sequence's parents and lengths while others write.
   const int64_t n = batch->n, T = batch->n_tokens;
   const Extent d(depth, T), m(bits, T * words);
@@ -194,6 +195,7 @@ int misat_kv_keep(misat_kv* kv, const misat_kv_batch* batch, const int32_t* path
   if (!batch->q_off || !batch->kv_len || (!batch->block_table && batch->table_stride > 0) ||
       (!path && path_stride > 0) || !n_keep || !kv_len_out || !on_device(kv->device))
     return MISAT_ERR_INVALID_ARG;
+  if (!at_elements(path) || !at_elements(n_keep) || !at_elements(kv_len_out)) return MISAT_ERR_INVALID_ARG;
   // Several CTAs read what there is of a sequence, and one of them writes its length.  (The last row of several may be shorter
   // than their distance.)
   const int64_t n = batch->n, table = n == 1 ? batch->table_stride : (n - 1) * batch->table_stride + 1;
