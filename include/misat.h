@@ -700,7 +700,9 @@ int misat_kv_tree(misat_kv* kv, const misat_kv_batch* batch, const int32_t* pare
 
 /* misat_kv_append with norms of the queries' and the keys' heads before the rotation (each NULL:
  * none), and with the positions of a tree's nodes (draft NULL: tokens in a row).  Nodes go into the
- * slots of their numbers, absent ones at depth 0.  Errors as misat_kv_append's.  [async] */
+ * slots of their numbers, absent ones at depth 0.  With the same norms, a token at a position gives the
+ * same bits as a node of a tree and in a row; with none, a node's rotated elements may differ from
+ * misat_kv_append's in the last bit (the turns are worked out another way, within the same bound).  Errors as misat_kv_append's.  [async] */
 int misat_kv_append_norm(misat_kv* kv, const misat_kv_batch* batch, const misat_head_norm* q_norm,
                          const misat_head_norm* k_norm, const misat_kv_draft* draft, const void* k,
                          int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,

@@ -1,4 +1,5 @@
-"""Trees with nodes that are not there, whose queries, keys and values hold anything, and plans of malformed batches."""
+"""Trees with nodes that are not there, whose queries, keys and values hold anything, plans of malformed batches, and nodes
+beside tokens in a row."""
 
 import math
 import random
@@ -183,3 +184,41 @@ def test_attention_by_the_plan_of_a_malformed_batch():
     out, lse = pool.attend(batch, q, return_lse=True, tree=tree)
     pool.sync()
     assert (out[:3] == 0).all() and (lse[:3] == -math.inf).all() and torch.equal(out[3:], want[3:])
+
+
+# ---- nodes and tokens in a row ----
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("hq,hkv,d,rot,half", [(4, 2, 64, 64, True), (7, 1, 72, 20, False), (32, 8, 128, 128, True), (3, 3, 24, 6, True),
+                                               (2, 1, 64, 64, False)])
+@pytest.mark.parametrize("normed", [("k_norm",), ("q_norm",), ("q_norm", "k_norm")])
+def test_a_node_is_cached_as_the_token_at_its_position(hq, hkv, d, rot, half, dtype, normed):
+    """Any tree's nodes, and each of them appended as a token in a row at the same position, with norms: the same bits."""
+    m = misat()
+    rope = m.Rope(rot, layout=m.ROPE_HALF if half else m.ROPE_INTERLEAVED)
+    norm = m.HeadNorm(rand((d,), dtype, 5) + 1)
+    kw = {name: norm for name in normed}
+    s = Step([(40, 31040), (300, 7300), (1, 1), (64, 80)], hkv, d, dtype)
+    pool = s.pool(hq, rope=rope)
+    batch = s.batch(pool)
+    r = random.Random(6)
+    parents = [r.randint(max(-1, i - 3), i - 1) for n in s.new for i in range(n)]
+    x = rand((s.T, hq + 2 * hkv, d), dtype, 3, 2.0)
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    got = pool.append(batch, k, v, q=q, tree=pool.tree(batch, ints(parents)), **kw)
+    blk, at = slots_of(s)
+    cached_k, cached_v = s.kb[blk, :, at], s.vb[blk, :, at]
+    depth, _ = ref.tree(s.new, parents)
+    first = [L - n for n, L in zip(s.new, s.lens) for _ in range(n)]
+    # a sequence for each node, whose one new token is at the node's position
+    lens = [p + e + 1 for p, e in zip(first, depth)]
+    table = torch.arange(s.T, dtype=torch.int32, device="cuda")[:, None].expand(s.T, max(lens) // 16 + 1).contiguous()
+    kb, vb = (torch.zeros((s.T, hkv, 16, d), dtype=dtype, device="cuda") for _ in range(2))
+    row = m.KvPool(kb, vb, n_q_heads=hq, rope=rope, max_batch=s.T)
+    want = row.append(row.batch(ints(list(range(s.T + 1))), ints(lens), table, n_tokens=s.T, max_q=1), k, v, q=q, **kw)
+    pool.sync()
+    row.sync()
+    t, place = torch.arange(s.T, device="cuda"), ints(lens).long() - 1
+    assert torch.equal(got, want)
+    assert torch.equal(cached_k, kb[t, :, place % 16]) and torch.equal(cached_v, vb[t, :, place % 16])
