@@ -665,14 +665,21 @@ class KvBatch:
     """The new tokens of n sequences (misat_kv_batch): made once for a step, used by every layer.  It serves
     every pool of the same heads on its device, and has to stay while a graph that holds a call with it is replayed."""
 
+    _c = None
+
     def __init__(self, pool, q_off, kv_len, block_table, n_tokens, max_q):
         self._state = _torch_calls().batch_state(pool._state, q_off, kv_len, block_table, int(n_tokens), int(max_q))
-        self._keep = (q_off, kv_len, block_table)
-        self.n, self.n_tokens = kv_len.shape[0], int(n_tokens)
-        stride = block_table.stride(0) if self.n > 1 else block_table.shape[1]
-        self._c = misat_kv_batch(self.n, self.n_tokens, int(max_q), q_off.data_ptr(), kv_len.data_ptr(),
-                                 block_table.data_ptr(), stride)
-        self._ref = C.addressof(self._c)  # for calls of the C functions
+        self.q_off, self.kv_len, self.block_table = q_off, kv_len, block_table
+        self.n, self.n_tokens, self.max_q = kv_len.shape[0], int(n_tokens), int(max_q)
+
+    @property
+    def _ref(self):
+        """The batch for calls of the C functions."""
+        if self._c is None:
+            stride = self.block_table.stride(0) if self.n > 1 else self.block_table.shape[1]
+            self._c = misat_kv_batch(self.n, self.n_tokens, self.max_q, self.q_off.data_ptr(), self.kv_len.data_ptr(),
+                                     self.block_table.data_ptr(), stride)
+        return C.addressof(self._c)
 
 
 class KvStep(KvBatch):
@@ -681,9 +688,8 @@ class KvStep(KvBatch):
 
     def __init__(self, tables, made, n, n_tokens, max_q):
         self.state, self.q_off, self.kv_len, self.positions, self.slots, self._state = made
-        self._keep = (self.q_off, self.kv_len, tables.block_table)
-        self.n, self.n_tokens, self.max_q = n, int(n_tokens), int(max_q)
         self.block_table = tables.block_table
+        self.n, self.n_tokens, self.max_q = n, int(n_tokens), int(max_q)
 
 
 class KvTables:

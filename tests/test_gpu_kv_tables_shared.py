@@ -56,3 +56,22 @@ def test_a_row_shortened_below_its_shared_blocks_is_refused():
         t.pool.sync()
     assert e.value.code == m.ERR_INVALID_ARG
     t.check([1, 1], [20, 23], [2, 0])
+
+
+def test_a_step_serves_the_library_s_calls_as_any_batch():
+    m = misat()
+    t = Tables([1, 0, 1], 6, 9)
+    made = t.step([5, 20, 3], [10, 0, 16])
+    plain = t.pool.batch(made.q_off, made.kv_len, t.d_table, n_tokens=28, max_q=20)
+    for name in ("n", "n_tokens", "max_q"):
+        assert getattr(made, name) == getattr(plain, name)
+    for name in ("q_off", "kv_len", "block_table"):
+        assert getattr(made, name).data_ptr() == getattr(plain, name).data_ptr()
+    x = torch.randn((28, 1, 8), device="cuda").to(t.kb.dtype)
+    t.pool.append(plain, x, x)
+    want = t.kb.clone()
+    t.kb.zero_()
+    st = torch.cuda.current_stream().cuda_stream
+    assert m._lib.misat_kv_append(t.pool._h, made._ref, x.data_ptr(), 8, 8, x.data_ptr(), 8, 8, None, 0, 0, None, 0, 0, st) == 0
+    t.pool.sync()
+    assert torch.equal(t.kb, want) and (want != 0).any()
