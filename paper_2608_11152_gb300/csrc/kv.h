@@ -90,12 +90,13 @@ inline bool aligned16(const Heads& h, int elem) {
 // An array of a call, of `count` elements of `size` bytes.  apart: no byte of one is the other's.
 struct Extent {
   uintptr_t begin, end;
-  Extent(const void* p, int64_t count, int size = 4)
-      : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (p && count > 0 ? (uint64_t)count * size : 0)) {}
+  Extent(const void* p, int64_t count, int size = 4) {
+    const bool empty = !p || count <= 0;
+    begin = empty ? UINTPTR_MAX : reinterpret_cast<uintptr_t>(p);
+    end = empty ? 0 : begin + (uint64_t)count * size;
+  }
 };
-inline bool apart(const Extent& a, const Extent& b) {
-  return a.begin == a.end || b.begin == b.end || a.end <= b.begin || b.end <= a.begin;
-}
+inline bool apart(const Extent& a, const Extent& b) { return (a.end <= b.begin) | (b.end <= a.begin); }
 
 // The handle's device is the current one.
 inline bool on_device(int device) {
