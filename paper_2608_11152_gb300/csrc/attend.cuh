@@ -35,7 +35,7 @@
 // Trees of drafted tokens (TREE): a node's keys are those before the tree and the ones of its bits, so a block that reaches
 // into the tree takes its mask from the node's words instead of from its position.  64 query heads' 63 nodes over
 // 130,941 tokens (8 kv heads of 64, f16) take 176 us, 96 sequences of 16 to 32 nodes over 512 to 16,000 tokens (8 kv heads of
-// 128) 509 against 505 for the same tokens in a row.
+// 128) 510 against 505 for the same tokens in a row (510 to 522 on different GPUs).
 #pragma once
 
 #include <algorithm>

@@ -10,7 +10,7 @@
 // are worked out once for all heads of the CTA.  Squares, sums and products are in 32 bits, results are rounded once.
 //
 // Bound by memory where there are many tokens: 65,536 x 32 heads of 128 in bf16 forward 162 us for 1.07 GB (6.6 TB/s,
-// 0.97 of a plain copy), backward 241 us for 1.61 GB (0.98); by latency and issue where there are few: 64 tokens 2.8 us,
+// 0.97 of a plain copy), backward 241 us for 1.61 GB (0.98); by latency and issue where there are few: 64 tokens 2.3 us,
 // 5,003 tokens of 28 heads of 96 12.4 us (floor 7.9).  With the next token in registers instead of shared memory
 // these two were 411 and 24.8 us.
 //
@@ -726,7 +726,8 @@ Grid plan(NormArgs& a, int elem, bool half_layout, int vec, bool backward, int n
   g.x = (rounds - 1) / a.per + 1;
   if (backward) {
     // The CTAs whose sums belong together are a cluster where few rounds are left for each: a call of 8 tokens of 32 heads
-    // takes 5.0 us from the host and 3.8 on the GPU, of 32 tokens (4 rounds) 5.9, as two kernels 7.3 and 4.2, 7.5 and 4.4.
+    // takes 4.5 to 5.7 us from the host (on different machines) and 3.8 in a graph, as two kernels 7.3 and 4.2; of 32 tokens,
+    // which are too many rounds, 6.3 to 7.2 and 4.4.
     const int most_x = kCluster / (a.wq.hs == 0 ? g.y : 1);
     a.fused = rounds <= most_x * kClusterRounds;
     if (a.fused) {

@@ -111,7 +111,7 @@ struct OffsetFinder {
   }
 };
 
-// VEC elements of T at p; VEC * sizeof(T) is 16 and p aligned to it, or VEC is 1.
+// VEC elements of T in one access, at an address that is a multiple of their size, at most 16 bytes.
 template <class T, int VEC>
 struct alignas(VEC * sizeof(T)) Vec {
   T e[VEC];

@@ -9,11 +9,11 @@
 // other part writes.  The sums over the sequences are scans by one CTA, which also finds out whether the step can be
 // made at all; a second kernel writes what the sums are the offsets of.
 //
-// Bound by latency.  256 sequences of one token: 4.2 us, one CTA with a launch, two trips to memory before its sums
+// Bound by latency.  256 sequences of one token: 4.1 us, one CTA with a launch, two trips to memory before its sums
 // and two behind them (20.8 us as two kernels with sums over the warps one after the other).  4,096 sequences with
-// 4.05 M tokens and 385,000 blocks given back: 25 us, of which the sums 7 and the 48 MB of positions and slots 8 at the
-// least; in the second kernel a warp has tokens next to each other, searches for its first one alone and looks up 31
-// blocks at a time, one a lane (four tokens a lane, each with its lookup: 30 us; a lookup for every token: 60).
+// 4.05 M tokens, 253,000 blocks taken and 417,000 given back: 25 us, of which the sums 7 and the 48 MB of positions and
+// slots 8 at the least; in the second kernel a warp has tokens next to each other, searches for its first one alone and
+// looks up 31 blocks at a time, one a lane (four tokens a lane, each with its lookup: 30 us; a lookup for every token: 60).
 #include <algorithm>
 #include <initializer_list>
 
@@ -499,10 +499,11 @@ int misat_kv_tables(misat_kv* kv, const misat_kv_step* s, void* work, int64_t wo
   a.give_off = a.give_from + (s->n + 3) / 4 * 4;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   a.vec_rows = (bits({a.fresh, a.kv_len, a.shared, a.state, a.state_out, a.q_off, a.kv_len_out}) & 15) == 0;
-  // A small step is one CTA's: 256 sequences of one token 4.2 us, as two kernels about 9.  Where the table is so large that
-  // sequences that finish could give back more blocks than one CTA should move, a second kernel looks whether they do
-  // (256 sequences that hold up to 30,000 tokens: 7.0 us a step, all of them finished 8.2; of 65,000 blocks in a table below
-  // that size, all given back, one CTA takes 47).
+  // A small step is one CTA's: 256 sequences of one token 3.4 us in a graph where none finishes, with a second kernel behind
+  // it 4.7.  How many blocks it gives back is not known here, and one CTA takes 0.6 us a thousand of them: 8 us for 8,192,
+  // 23 for 32,768, 43 for 65,536, 81 for 128,000, where the two kernels take 6.3 to 6.6.  So the size of the table decides: up
+  // to kFillPlaces places the step in which all of them come back at once takes at most 81 us, beyond that no step takes
+  // more than 10 and each pays the second launch.
   if (s->n <= kPlanThreads && s->n_tokens <= kFillTokens) {
     a.defer = (int64_t)s->n * s->columns > kFillPlaces;
     launch_chained(k_table_plan<1, true>, 1, kPlanThreads, 0, st, a);

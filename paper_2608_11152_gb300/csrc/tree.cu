@@ -9,7 +9,7 @@
 // written, also where it has several rows in flight.
 //
 // Both are bound by latency: a few dependent reads a sequence, then one pass over the rows.  The plan of 64 trees of 16 to
-// 32 nodes takes 2.1 us, of 1,024 trees of 129 nodes 4.9; paths of 64 such trees (8 kv heads of 128) 3.4 us.  1,024 paths of
+// 32 nodes takes 1.8 us, of 1,024 trees of 129 nodes 4.8; paths of 64 such trees (8 kv heads of 128) 3.3 us.  1,024 paths of
 // up to 64 rows of 8 x 64 elements move 95 MB in 21.7 us, 0.64 of the copy rate: 128 bytes at a place.  Sixteen rows of a
 // column are in flight (8: 27.4 us, 24: 22.7, 32: 21.9).
 #include <algorithm>

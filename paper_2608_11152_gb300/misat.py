@@ -654,7 +654,8 @@ class Rope:
 class HeadNorm:
     """Root-mean-square norm of each head (misat_head_norm): x / sqrt(mean x^2 + eps) * (offset + weight), for
     Rope.norm_rotate, Rope.norm_backward and KvPool.append.  weight: [head_dim] for all heads or [heads, head_dim], of the
-    heads' dtype or float32; the caller's tensor, read at every call."""
+    heads' dtype or float32; the caller's tensor, read at every call.  Finite elements beyond 2^59 in magnitude may make their
+    head zeros."""
 
     def __init__(self, weight, eps=1e-6, offset=0.0):
         self.weight, self.eps, self.offset = weight, float(eps), float(offset)
